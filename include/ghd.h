@@ -402,6 +402,82 @@ ghd_status ghd_spec_step(const ghd_spec_model *m, const int32_t *parent_dev, con
                          size_t ws_bytes, void *stream);
 size_t ghd_spec_workspace_bytes(const ghd_spec_model *m, int M, int kv_len);
 
+/* ---- the step's weights and cache in 4 bits --------------------------------
+ * The step's time is the bytes it streams: the weights of the linear layers and the
+ * committed cache (sections 2.1, 2.2.2).  Held in 4 bits both are a little more
+ * than a quarter of their fp16 size.  These calls take the place of
+ * ghd_linear_skinny, ghd_tree_attention / ghd_masked_attention and ghd_commit_path
+ * in a step whose weights and cache are held that way.
+ *
+ * Weights: codes 0..15 with a scale (fp16) and a zero point (a whole number) for
+ * every `group` columns of a row, group in {32, 64, 128}; the last group of a
+ * row may be short:  W[n, k] = (code[n, k] - zero[n, k / group]) * scale[n, k / group].
+ *
+ * Cache of one layer (ghd_kv, each of k and v of ghd_kv_q4_bytes, 16-byte
+ * aligned; capacity % 32 == 0, at most 2^24): every row of a head in groups of 32
+ * channels, a group x held as lo = min x, s = fp16((max x - lo) / 15) (one fp16 step less
+ * where lo + 15 s would not fit fp16) and codes rint((x - lo) / s), which stand for
+ * fp16(lo + code * s).  A group that holds an infinity or NaN reads as NaN.  Only these
+ * calls look inside; memory that was never appended to may hold anything.  Layout:
+ * csrc/q4.h.  Query heads share key heads: nh % nkv == 0, head h reads key head
+ * h / (nh / nkv).  nh, nkv <= 256, d in {64, 128}. */
+
+/* Bytes of the packed form; 0 for sizes that are not taken (K % 8 == 0, K <= 65536,
+ * N <= 2^20). */
+size_t ghd_weight_q4_bytes(int N, int K, int group);
+
+/* dst (packed) <- codes uint8 [N, K / 2] (two to a byte, the even column in the low
+ * four bits), scales fp16 [N, ceil(K / group)], zeros uint8 of the same shape or NULL
+ * (8 throughout), all row-major.  One-off, offline. */
+ghd_status ghd_pack_weight_q4(void *dst, const void *codes, const void *scales, const void *zeros,
+                              int N, int K, int group, void *stream);
+
+/* y = x W^T as ghd_linear_skinny, with Wq from ghd_pack_weight_q4: x fp16 [M, ldx],
+ * y float or fp16 (flags) [M, ldy].  Products and sums in 32 bits, scales applied to
+ * sums of x times whole numbers: nothing is rounded to fewer bits before y.  y must not
+ * meet x or Wq in memory. */
+ghd_status ghd_linear_q4(void *y, const void *x, const void *Wq, int M, int N, int K, int group,
+                         int64_t ldx, int64_t ldy, uint32_t flags, void *ws, size_t ws_bytes,
+                         void *stream);
+size_t ghd_linear_q4_workspace_bytes(int M, int N, int K);
+
+/* Bytes of each of k and v of one layer's cache; 0 for sizes that are not taken. */
+size_t ghd_kv_q4_bytes(int nkv, int capacity, int d);
+
+/* Rows kv_len .. kv_len + M - 1 of one layer's cache <- k, v fp16 [M, nkv, d] (rows
+ * ld_k, ld_v elements apart, even numbers; 4-byte aligned).  With rope_base > 0 keys
+ * are turned first, half-split pairs (j, j + d/2) by position * rope_base^(-2j/d), worked
+ * out in 64 bits, and rounded to fp16 as in the fp16 cache; with 0 they are taken
+ * as they are (rows of an fp16 cache).  parent_dev: positions are kv_len + depth (M <=
+ * GHD_MAX_M); NULL: kv_len + i, any M (a prompt).  q (optional, needs rope_base > 0): fp16
+ * [M, nh, d] at ld_q, turned the same way into q_out at ld_q_out, which may be q itself.
+ * Other rows stay as they are. */
+ghd_status ghd_kv_append_q4(const ghd_kv *kv, const void *k, const void *v, const void *q,
+                            void *q_out, const int32_t *parent_dev, int M, int kv_len, int nh, int nkv,
+                            int d, int capacity, int64_t ld_k, int64_t ld_v, int64_t ld_q,
+                            int64_t ld_q_out, float rope_base, void *stream);
+
+/* ghd_tree_attention and ghd_masked_attention over a 4-bit cache whose rows
+ * [0, kv_len + M) are there: q, out fp16 [M, nh, d].  An infinity or NaN in a row
+ * reaches the tokens that see the row and no others. */
+ghd_status ghd_tree_attention_q4(void *out, const void *q, const ghd_kv *kv,
+                                 const int32_t *parent_dev, int M, int kv_len, int nh, int nkv, int d,
+                                 int capacity, float scale, void *ws, size_t ws_bytes, void *stream);
+ghd_status ghd_masked_attention_q4(void *out, const void *q, const ghd_kv *kv,
+                                   const uint64_t *mask_dev, int M, int kv_len, int nh, int nkv, int d,
+                                   int capacity, float scale, void *ws, size_t ws_bytes, void *stream);
+size_t ghd_attention_q4_workspace_bytes(int M, int kv_len, int nh, int nkv, int d);
+
+/* ghd_commit_path for 4-bit caches: rows kv_len + path[j] -> kv_len + j in all L <= 48
+ * layers, codes and scales as they are.  res_dev as there. */
+ghd_status ghd_commit_path_q4(const ghd_kv *kv_host, int L, int nkv, int d, int capacity,
+                              const int32_t *res_dev, int M, int kv_len, void *stream);
+
+/* What rows [row0, row0 + rows) of all L layers stand for: k_out, v_out fp16
+ * [L, rows, nkv, d] (16-byte aligned). */
+ghd_status ghd_kv_read_q4(void *k_out, void *v_out, const ghd_kv *kv_host, int L, int nkv, int d,
+                          int capacity, int row0, int rows, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -102,6 +102,18 @@ def lib() -> C.CDLL:
             "ghd_draft_workspace_bytes": (sz, [i32, i32, i32, i32]),
             "ghd_spec_step": (C.c_int32, [vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]),
             "ghd_spec_workspace_bytes": (sz, [vp, i32, i32]),
+            "ghd_weight_q4_bytes": (sz, [i32, i32, i32]),
+            "ghd_pack_weight_q4": (C.c_int32, [vp, vp, vp, vp, i32, i32, i32, vp]),
+            "ghd_linear_q4": (C.c_int32, [vp, vp, vp, i32, i32, i32, i32, i64, i64, u32, vp, sz, vp]),
+            "ghd_linear_q4_workspace_bytes": (sz, [i32, i32, i32]),
+            "ghd_kv_q4_bytes": (sz, [i32, i32, i32]),
+            "ghd_kv_append_q4": (C.c_int32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i64, i64, i64, i64,
+                                             f32, vp]),
+            "ghd_tree_attention_q4": (C.c_int32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]),
+            "ghd_masked_attention_q4": (C.c_int32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]),
+            "ghd_attention_q4_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+            "ghd_commit_path_q4": (C.c_int32, [vp, i32, i32, i32, i32, vp, i32, i32, vp]),
+            "ghd_kv_read_q4": (C.c_int32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -120,7 +132,10 @@ EXPORTS = ["ghd_status_str", "ghd_last_hip_error", "ghd_tree_validate", "ghd_tre
            "ghd_accept_workspace_bytes", "ghd_accept_greedy_static", "ghd_verify_stack_argmax", "ghd_accept_path", "ghd_commit_path", "ghd_embed", "ghd_tree_build",
            "ghd_choose_width",
            "ghd_draft_tokens", "ghd_draft_workspace_bytes", "ghd_spec_step",
-           "ghd_spec_workspace_bytes"]
+           "ghd_spec_workspace_bytes",
+           "ghd_weight_q4_bytes", "ghd_pack_weight_q4", "ghd_linear_q4", "ghd_linear_q4_workspace_bytes",
+           "ghd_kv_q4_bytes", "ghd_kv_append_q4", "ghd_tree_attention_q4", "ghd_masked_attention_q4",
+           "ghd_attention_q4_workspace_bytes", "ghd_commit_path_q4", "ghd_kv_read_q4"]
 
 
 def status_str(status: int) -> str:
@@ -501,3 +516,147 @@ def ghd_spec_step(spec: SpecState, parent: torch.Tensor, rank: torch.Tensor, kv_
                                _ptr(_dev(rank, torch.int32)), M, kv_len, _ptr(_dev(tokens, torch.int32)),
                                _ptr(_dev(res, torch.int32)), _ptr(ws), ws.numel(), _stream()),
            "ghd_spec_step")
+
+
+# ---- weights and cache in 4 bits ------------------------------------------------
+def ghd_pack_weight_q4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], group: int
+                       ) -> torch.Tensor:
+    """codes uint8 [N, K / 2] (even column in the low four bits), scales fp16 [N, ceil(K / group)],
+    zeros uint8 of the same shape or None (8 throughout) -> packed bytes (uint8 tensor)."""
+    N, K = codes.shape[0], 2 * codes.shape[1]
+    shape = (N, -(-K // group))
+    if tuple(scales.shape) != shape or (zeros is not None and tuple(zeros.shape) != shape):
+        raise ValueError("scales and zeros must be %s" % (shape,))
+    out = torch.empty(lib().ghd_weight_q4_bytes(N, K, group), dtype=torch.uint8, device=codes.device)
+    _check(lib().ghd_pack_weight_q4(_ptr(out), _ptr(_dev(codes, torch.uint8)), _ptr(_dev(scales, torch.float16)),
+                                    None if zeros is None else _ptr(_dev(zeros, torch.uint8)), N, K, group,
+                                    _stream()), "ghd_pack_weight_q4")
+    return out
+
+
+def ghd_linear_q4_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib().ghd_linear_q4_workspace_bytes(M, N, K)
+
+
+def ghd_linear_q4(x: torch.Tensor, Wq: torch.Tensor, N: int, group: int, out_dtype=torch.float32,
+                  ws: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x fp16 [M, K] (rows may be apart), Wq from ghd_pack_weight_q4 with the same group."""
+    M, K = x.shape
+    if Wq.numel() != lib().ghd_weight_q4_bytes(N, K, group):
+        raise ValueError("Wq does not hold a [%d, %d] matrix in groups of %d" % (N, K, group))
+    if y is None:
+        y = torch.empty((M, N), dtype=out_dtype, device=x.device)
+    if ws is None:
+        ws = workspace(lib().ghd_linear_q4_workspace_bytes(M, N, K), x.device)
+    assert y.is_cuda and y.shape == (M, N) and y.stride(-1) == 1 and y.dtype in (torch.float16, torch.float32)
+    flags = GHD_OUT_F16 if y.dtype == torch.float16 else GHD_OUT_F32
+    _check(lib().ghd_linear_q4(_ptr(y), _ptr(_devs(x, torch.float16)), _ptr(_dev(Wq, torch.uint8)), M, N, K, group,
+                               x.stride(0), y.stride(0), flags, _ptr(ws), ws.numel(), _stream()), "ghd_linear_q4")
+    return y
+
+
+class KvQ4:
+    """The 4-bit caches of L layers: `capacity` rows (a multiple of 32) of nkv heads of d channels."""
+
+    def __init__(self, L: int, nkv: int, d: int, capacity: int, device="cuda"):
+        n = lib().ghd_kv_q4_bytes(nkv, capacity, d)
+        if n == 0:
+            raise ValueError("no 4-bit cache of %d heads of %d channels by %d rows" % (nkv, d, capacity))
+        self.L, self.nkv, self.d, self.capacity = L, nkv, d, capacity
+        self.k = torch.zeros((L, n), dtype=torch.uint8, device=device)
+        self.v = torch.zeros((L, n), dtype=torch.uint8, device=device)
+        self.kv = (KV * L)(*[KV(self.k[i].data_ptr(), self.v[i].data_ptr()) for i in range(L)])
+
+    def layer(self, i: int):
+        return C.byref(self.kv[i])
+
+
+def _heads(t: torch.Tensor, heads: int, d: int) -> torch.Tensor:
+    """A [M, heads, d] tensor whose rows may be apart but whose heads lie side by side."""
+    assert t.is_cuda and t.dtype == torch.float16 and t.shape[1:] == (heads, d), (t.device, t.dtype, t.shape)
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == d), t.stride()
+    return t
+
+
+def _row_step(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, kv_len: int,
+                     q: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None, rope_base: float = 0.0,
+                     q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Rows kv_len .. of a layer from k, v fp16 [M, nkv, d] (views into a fused row are fine), keys
+    turned where rope_base > 0: at kv_len + depth of parent, or at kv_len + i.  q fp16 [M, nh, d] is
+    turned likewise and returned."""
+    M, nkv, d = k.shape[0], cache.nkv, cache.d
+    _heads(k, nkv, d), _heads(v, nkv, d)
+    assert v.shape[0] == M and (parent is None or parent.numel() == M)
+    nh, ld_q, ld_qo = 0, 0, 0
+    if q is not None:
+        nh = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((M, nh, d), dtype=torch.float16, device=q.device)
+        assert q.shape[0] == M and q_out.shape[0] == M
+        ld_q, ld_qo = _row_step(_heads(q, nh, d)), _row_step(_heads(q_out, nh, d))
+    _check(lib().ghd_kv_append_q4(cache.layer(layer), _ptr(k), _ptr(v), _ptr(q), _ptr(q_out) if q is not None else None,
+                                  None if parent is None else _ptr(_dev(parent, torch.int32)), M, kv_len, nh, nkv, d,
+                                  cache.capacity, _row_step(k), _row_step(v), ld_q, ld_qo, rope_base, _stream()),
+           "ghd_kv_append_q4")
+    return q_out if q is not None else None
+
+
+def ghd_attention_q4_workspace_bytes(M: int, kv_len: int, nh: int, nkv: int, d: int) -> int:
+    return lib().ghd_attention_q4_workspace_bytes(M, kv_len, nh, nkv, d)
+
+
+def _attention_q4(fn, name, q, cache, layer, relation, kv_len, scale, ws, out):
+    M, nh, d = q.shape
+    assert d == cache.d
+    if out is None:
+        out = torch.empty_like(q)
+    if scale is None:
+        scale = 1.0 / (d ** 0.5)
+    if ws is None:
+        ws = workspace(lib().ghd_attention_q4_workspace_bytes(M, kv_len, nh, cache.nkv, d), q.device)
+    assert out.shape == q.shape
+    _check(fn(_ptr(_dev(out, torch.float16)), _ptr(_dev(q, torch.float16)), cache.layer(layer), relation, M, kv_len, nh,
+              cache.nkv, d, cache.capacity, scale, _ptr(ws), ws.numel(), _stream()), name)
+    return out
+
+
+def ghd_tree_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, parent: torch.Tensor, kv_len: int,
+                          scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q fp16 [M, nh, d] over the rows [0, kv_len + M) of a layer; returns fp16 [M, nh, d]."""
+    assert parent.numel() == q.shape[0]
+    return _attention_q4(lib().ghd_tree_attention_q4, "ghd_tree_attention_q4", q, cache, layer,
+                         _ptr(_dev(parent, torch.int32)), kv_len, scale, ws, out)
+
+
+def ghd_masked_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, mask: torch.Tensor, kv_len: int,
+                            scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """As ghd_tree_attention_q4 with the relation as int64 [M, 2] bit masks (ghd_masked_attention)."""
+    assert mask.shape == (q.shape[0], 2)
+    return _attention_q4(lib().ghd_masked_attention_q4, "ghd_masked_attention_q4", q, cache, layer,
+                         _ptr(_dev(mask, torch.int64)), kv_len, scale, ws, out)
+
+
+def ghd_commit_path_q4(cache: KvQ4, res: torch.Tensor, M: int, kv_len: int) -> None:
+    """ghd_commit_path for all layers of a 4-bit cache."""
+    _check(lib().ghd_commit_path_q4(cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, _ptr(_dev(res, torch.int32)),
+                                    M, kv_len, _stream()), "ghd_commit_path_q4")
+
+
+def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] = None,
+                   v: Optional[torch.Tensor] = None) -> tuple:
+    """What rows row0 .. row0 + rows - 1 of all layers stand for: fp16 [L, rows, nkv, d], keys and values."""
+    shape = (cache.L, rows, cache.nkv, cache.d)
+    if k is None:
+        k = torch.empty(shape, dtype=torch.float16, device=cache.k.device)
+    if v is None:
+        v = torch.empty(shape, dtype=torch.float16, device=cache.k.device)
+    assert k.shape == shape and v.shape == shape
+    _check(lib().ghd_kv_read_q4(_ptr(_dev(k, torch.float16)), _ptr(_dev(v, torch.float16)), cache.kv, cache.L, cache.nkv,
+                                cache.d, cache.capacity, row0, rows, _stream()), "ghd_kv_read_q4")
+    return k, v

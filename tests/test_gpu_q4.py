@@ -1,0 +1,410 @@
+"""The 4-bit operators on the GPU against plain forms in 64 bits (tests/q4_plain.py)."""
+import math
+import zlib
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_23219_amd import binding as B
+
+import q4_plain as P
+
+pytestmark = pytest.mark.gpu
+BASE = 10000.0
+
+
+def _rng(*key):
+    return np.random.default_rng([zlib.crc32(k.encode()) if isinstance(k, str) else int(k) for k in key])
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _close(got, want, tol):
+    err = np.abs(got.astype(np.float64) - want)
+    assert np.isfinite(got).all()
+    assert (err <= tol).all(), "off by %.3g where %.3g is allowed" % (err.flat[np.argmax(err - tol)], tol.flat[np.argmax(err - tol)])
+
+
+def _random_parent(rng, M, kind):
+    if kind == "chain":
+        return np.arange(-1, M - 1, dtype=np.int32)
+    return np.array([-1] + [rng.integers(0, i) for i in range(1, M)], np.int32)
+
+
+def _rows(rng, *shape):
+    return (rng.standard_normal(shape) * np.exp(0.5 * rng.standard_normal(shape[-2:])) + 0.5).astype(np.float16)
+
+
+# ---- linear ---------------------------------------------------------------------------
+def _weights(rng, N, K, group, zeros):
+    G = -(-K // group)
+    codes = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    scales = (rng.uniform(0.2, 1.0, (N, G)) * 0.01).astype(np.float16)
+    return codes, scales, rng.integers(0, 16, (N, G), dtype=np.uint8) if zeros else None
+
+
+LINEAR = [(1, 16, 8, 32), (1, 1, 128, 128), (2, 17, 136, 64), (3, 1003, 1288, 32), (5, 100, 4096, 128), (16, 256, 1032, 128),
+          (17, 130, 640, 64), (31, 65, 2048, 32), (33, 48, 264, 128), (64, 515, 1024, 64), (65, 31, 520, 32),
+          (100, 1000, 256, 128), (128, 77, 3000, 128), (128, 4099, 512, 64), (1, 20000, 512, 32), (7, 16400, 264, 64),
+          (40, 16390, 128, 128), (128, 16385, 136, 32), (16, 4096, 11008, 128), (48, 640, 13824, 32), (1, 48, 65536, 128),
+          (128, 33, 8192, 64)]
+
+
+@pytest.mark.parametrize("M,N,K,group", LINEAR)
+@pytest.mark.parametrize("zeros", [False, True])
+def test_linear(M, N, K, group, zeros):
+    print("q4 linear", M, N, K, group, zeros, flush=True)
+    rng = _rng(M, N, K, group, zeros)
+    codes, scales, z = _weights(rng, N, K, group, zeros)
+    pad = 8 * int(rng.integers(0, 3))
+    wide = rng.standard_normal((M, K + pad)).astype(np.float16)
+    Wq = B.ghd_pack_weight_q4(_dev(codes), _dev(scales), None if z is None else _dev(z), group)
+    x = _dev(wide)[:, :K]
+    W = P.unpack_weight(codes, scales, z, K, group)
+    for out16 in (False, True):
+        room = torch.full((M + 1, N + 5), 7.0, dtype=torch.float16 if out16 else torch.float32, device="cuda")
+        B.ghd_linear_q4(x, Wq, N, group, y=room[:M, :N])
+        got = room.cpu().numpy()
+        want, tol = P.linear(wide[:, :K], W, out16)
+        _close(got[:M, :N], want, tol)
+        assert (got[M] == 7).all() and (got[:, N:] == 7).all()       # nothing outside y is written
+
+
+def test_linear_same_bits_every_time_and_for_any_rows_beside():
+    """Sums are made in a fixed order: runs agree to the bit."""
+    rng = _rng("bits")
+    codes, scales, z = _weights(rng, 4096, 11008, 64, True)
+    Wq = B.ghd_pack_weight_q4(_dev(codes), _dev(scales), _dev(z), 64)
+    for M in (1, 16, 40, 128):
+        x = _dev(rng.standard_normal((M, 11008)).astype(np.float16))
+        first = B.ghd_linear_q4(x, Wq, 4096, 64)
+        for _ in range(3):
+            assert torch.equal(first, B.ghd_linear_q4(x, Wq, 4096, 64))
+
+
+def test_linear_keeps_infinities_and_nan_in_their_rows():
+    rng = _rng("inf")
+    codes, scales, _ = _weights(rng, 80, 264, 128, False)
+    Wq = B.ghd_pack_weight_q4(_dev(codes), _dev(scales), None, 128)
+    x = rng.standard_normal((20, 264)).astype(np.float16)
+    clean = B.ghd_linear_q4(_dev(x), Wq, 80, 128).cpu().numpy()
+    x[3, 7], x[17, 263] = np.inf, np.nan
+    got = B.ghd_linear_q4(_dev(x), Wq, 80, 128).cpu().numpy()
+    rest = [i for i in range(20) if i not in (3, 17)]
+    assert np.array_equal(got[rest], clean[rest])
+    assert not np.isfinite(got[3]).any() and np.isnan(got[17]).all()
+
+
+def test_linear_reads_nothing_behind_a_row():
+    """Columns from K on (here NaN) are no part of x."""
+    rng = _rng("behind")
+    codes, scales, _ = _weights(rng, 64, 136, 32, False)
+    Wq = B.ghd_pack_weight_q4(_dev(codes), _dev(scales), None, 32)
+    wide = np.full((4, 160), np.nan, np.float16)
+    wide[:, :136] = rng.standard_normal((4, 136))
+    want, tol = P.linear(wide[:, :136], P.unpack_weight(codes, scales, None, 136, 32), False)
+    _close(B.ghd_linear_q4(_dev(wide)[:, :136], Wq, 64, 32).cpu().numpy(), want, tol)
+
+
+# ---- cache ----------------------------------------------------------------------------
+def _filled(L, nkv, d, cap, byte=0xFF):
+    """A cache over memory that holds anything (0xFF: every lo and scale a NaN)."""
+    cache = B.KvQ4(L, nkv, d, cap)
+    cache.k.fill_(byte)
+    cache.v.fill_(byte)
+    return cache
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nkv,M,kv_len", [(1, 1, 0), (3, 1, 7), (2, 5, 30), (4, 8, 8), (2, 33, 61), (5, 128, 3), (1, 300, 1),
+                                          (3, 77, 51)])
+def test_rows_come_back_as_the_format_says(nkv, M, kv_len, d):
+    print("q4 rows", nkv, M, kv_len, d, flush=True)
+    rng = _rng(nkv, M, kv_len, d)
+    cap = -(-(kv_len + M + 3) // 32) * 32
+    cache = _filled(2, nkv, d, cap, 0)
+    before = _rows(rng, cap, nkv, d), _rows(rng, cap, nkv, d)
+    B.ghd_kv_append_q4(cache, 1, _dev(before[0]), _dev(before[1]), 0)
+    fused = _dev(_rows(rng, M, 2 * nkv + 1, d).reshape(M, -1))
+    k = fused[:, :nkv * d].view(M, nkv, d)
+    v = fused[:, (nkv + 1) * d:].view(M, nkv, d)
+    B.ghd_kv_append_q4(cache, 1, k, v, kv_len)
+    kr, vr = (t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, 0, cap))
+    for got, x, b in ((kr, k, before[0]), (vr, v, before[1])):
+        want = b.copy()
+        want[kv_len:kv_len + M] = x.cpu().numpy()
+        assert np.array_equal(got[1], P.held(want))      # the rows that were there too
+        assert (got[0] == 0).all()                       # the other layer
+    part_k, part_v = (t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, kv_len, M))
+    assert np.array_equal(part_k, kr[:, kv_len:kv_len + M]) and np.array_equal(part_v, vr[:, kv_len:kv_len + M])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M,kv_len,kind", [(1, 0, "chain"), (8, 100, "random"), (64, 2053, "random"), (128, 31, "chain"),
+                                           (200, 5, None), (9, 100000, None)])
+def test_turned_rows(M, kv_len, kind, d):
+    print("q4 turn", M, kv_len, kind, d, flush=True)
+    rng = _rng(M, kv_len, str(kind), d)
+    nkv, nh = 3, 6
+    cache = B.KvQ4(1, nkv, d, -(-(kv_len + M) // 32) * 32)
+    parent = None if kind is None else _random_parent(rng, M, kind)
+    pos = kv_len + (np.arange(M) if parent is None else P.depths(parent))
+    k, v, q = _rows(rng, M, nkv, d), _rows(rng, M, nkv, d), _rows(rng, M, nh, d)
+    q[:, :nkv] = k                                       # so that the turned keys come back as fp16 too
+    out = B.ghd_kv_append_q4(cache, 0, _dev(k), _dev(v), kv_len, q=_dev(q), parent=None if parent is None else _dev(parent),
+                             rope_base=BASE).cpu().numpy()
+    want = P.turn(q, pos, BASE)
+    # cosine and sine rounded to 32 bits, two products and a sum in 32 bits, the result to fp16
+    pair = np.abs(q.astype(np.float64))
+    pair = pair + np.roll(pair, d // 2, -1)
+    _close(out, want, 2.0 ** -11 * np.abs(want) + 2.0 ** -21 * pair + 2.0 ** -25)
+    kr, vr = (t.cpu().numpy()[0] for t in B.ghd_kv_read_q4(cache, kv_len, M))
+    assert np.array_equal(kr, P.held(out[:, :nkv]))      # what is held is the fp16 key, turned
+    assert np.array_equal(vr, P.held(v))
+
+
+def test_queries_turned_in_place_in_a_fused_row():
+    rng = _rng("place")
+    M, nh, nkv, d = 19, 8, 2, 128
+    fused = _dev(_rows(rng, M, nh + 2 * nkv, d).reshape(M, -1))
+    q, k, v = fused[:, :nh * d].view(M, nh, d), fused[:, nh * d:(nh + nkv) * d].view(M, nkv, d), fused[:, (nh + nkv) * d:].view(M, nkv, d)
+    a, b = B.KvQ4(1, nkv, d, 64), B.KvQ4(1, nkv, d, 64)
+    want = B.ghd_kv_append_q4(a, 0, k, v, 5, q=q.clone(), rope_base=BASE)
+    got = B.ghd_kv_append_q4(b, 0, k, v, 5, q=q, rope_base=BASE, q_out=q)
+    assert got.data_ptr() == q.data_ptr() and torch.equal(got, want)
+    assert torch.equal(a.k, b.k) and torch.equal(a.v, b.v)
+
+
+def test_edge_values_of_a_group():
+    """Constant groups, the widest range, subnormal numbers, signed zeros; an infinity or NaN makes
+    its own group NaN and no other."""
+    d = 128
+    x = np.zeros((8, 1, d), np.float16)
+    x[0] = 3.25
+    x[1, 0, :32] = np.linspace(-65504, 65504, 32)
+    x[1, 0, 32:64] = np.linspace(32768, 65504, 32)
+    x[2, 0] = np.arange(d) * 2.0 ** -24
+    x[3, 0, ::2] = -0.0
+    x[4, 0, 5] = 1
+    x[5, 0, 40], x[6, 0, 70], x[7, 0, 127] = np.inf, -np.inf, np.nan
+    cache = B.KvQ4(1, 1, d, 32)
+    B.ghd_kv_append_q4(cache, 0, _dev(x), _dev(x), 3)
+    want = P.held(x)
+    assert np.isfinite(want[:5]).all()
+    for got in B.ghd_kv_read_q4(cache, 3, 8):
+        got = got.cpu().numpy()[0]
+        nan = np.isnan(want)
+        assert np.array_equal(np.isnan(got), nan) and np.array_equal(got[~nan], want[~nan])
+        assert nan.sum() == 3 * 32
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("path", [[0], [0, 1, 2], [0, 3], [0, 1, 4, 7, 30, 31], [0, 2, 3, 5, 8, 9, 12, 20, 21, 33, 50],
+                                  list(range(0, 64, 2)), list(range(0, 40)) + [60, 63]])
+@pytest.mark.parametrize("kv_len", [0, 27])
+def test_commit_moves_the_accepted_rows_only(path, kv_len, d):
+    print("q4 commit", len(path), kv_len, d, flush=True)
+    rng = _rng(len(path), kv_len, d)
+    L, nkv, M = 3, 5, 64
+    cap = 96
+    cache = B.KvQ4(L, nkv, d, cap)
+    for l in range(L):
+        B.ghd_kv_append_q4(cache, l, _dev(_rows(rng, cap, nkv, d)), _dev(_rows(rng, cap, nkv, d)), 0)
+    before = [t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, 0, cap)]
+    B.ghd_commit_path_q4(cache, _dev(np.array([len(path), 9] + path, np.int32)), M, kv_len)
+    after = [t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, 0, cap)]
+    for b, a in zip(before, after):
+        want = b.copy()
+        for j, node in enumerate(path):
+            want[:, kv_len + j] = b[:, kv_len + node]
+        assert np.array_equal(a, want)
+
+
+def test_commit_with_a_corrupt_result_stays_in_the_tree():
+    rng = _rng("corrupt")
+    cache = B.KvQ4(1, 2, 64, 96)
+    B.ghd_kv_append_q4(cache, 0, _dev(_rows(rng, 96, 2, 64)), _dev(_rows(rng, 96, 2, 64)), 0)
+    before = [t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, 0, 96)]
+    B.ghd_commit_path_q4(cache, _dev(np.array([1000, 9] + [12345, -7] * 8, np.int32)), 16, 40)
+    after = [t.cpu().numpy() for t in B.ghd_kv_read_q4(cache, 0, 96)]
+    for b, a in zip(before, after):
+        assert np.array_equal(a[:, :40], b[:, :40]) and np.array_equal(a[:, 56:], b[:, 56:])
+
+
+# ---- attention ------------------------------------------------------------------------
+def _attend(M, nh, nkv, d, kv_len, see, rng, parent=None, scale=None, mend=None):
+    T = kv_len + M
+    cache = _filled(1, nkv, d, -(-T // 32) * 32 + 32)
+    k, v = _rows(rng, T, nkv, d), _rows(rng, T, nkv, d)
+    q = rng.standard_normal((M, nh, d)).astype(np.float16)
+    B.ghd_kv_append_q4(cache, 0, _dev(k), _dev(v), 0)
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    if parent is not None:
+        got = B.ghd_tree_attention_q4(_dev(q), cache, 0, _dev(parent), kv_len, scale=scale)
+    else:
+        got = B.ghd_masked_attention_q4(_dev(q), cache, 0, _dev(P.mask_words(see)), kv_len, scale=scale)
+    want, tol = P.attention(q, P.held(k), P.held(v), see, kv_len, scale)
+    _close(got.cpu().numpy(), want, tol)
+
+
+ATTENTION = [(1, 1, 1, 0), (1, 4, 4, 1), (1, 8, 2, 30), (1, 32, 4, 31), (1, 8, 1, 4000), (2, 6, 3, 32), (5, 5, 5, 95), (7, 40, 5, 129),
+             (16, 4, 4, 0), (16, 4, 2, 500), (17, 3, 3, 64), (31, 8, 1, 33), (33, 4, 4, 1000), (37, 20, 4, 777), (64, 2, 2, 2048),
+             (64, 16, 2, 13), (65, 2, 1, 63), (96, 2, 2, 40), (100, 10, 5, 1), (128, 2, 2, 0), (128, 3, 3, 300), (128, 16, 1, 129)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M,nh,nkv,kv_len", ATTENTION)
+def test_tree_attention(M, nh, nkv, kv_len, d):
+    for kind in ("chain", "random"):
+        print("q4 tree attention", M, nh, nkv, kv_len, d, kind, flush=True)
+        rng = _rng(M, nh, nkv, kv_len, d, kind)
+        parent = _random_parent(rng, M, kind)
+        _attend(M, nh, nkv, d, kv_len, P.sees_of_parent(parent), rng, parent)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M,nh,nkv,kv_len", ATTENTION)
+def test_masked_attention(M, nh, nkv, kv_len, d):
+    """Any relation; some rows see no drafted token, with nothing committed no key at all: zeros."""
+    print("q4 masked attention", M, nh, nkv, kv_len, d, flush=True)
+    rng = _rng(M, nh, nkv, kv_len, d, "mask")
+    see = rng.random((M, M)) < 0.3
+    see[::3] = False
+    _attend(M, nh, nkv, d, kv_len, see, rng)
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 2.0, 1e-3])
+def test_attention_scales(scale):
+    rng = _rng("scale", int(scale * 1000) + 500)
+    parent = _random_parent(rng, 12, "random")
+    _attend(12, 4, 2, 128, 200, P.sees_of_parent(parent), rng, parent, scale=scale)
+
+
+def test_mask_bits_behind_the_last_token_say_nothing():
+    rng = _rng("bits behind")
+    M, kv = 20, 10
+    cache = _filled(1, 2, 64, 64)
+    B.ghd_kv_append_q4(cache, 0, _dev(_rows(rng, kv + M, 2, 64)), _dev(_rows(rng, kv + M, 2, 64)), 0)
+    q = _dev(rng.standard_normal((M, 2, 64)).astype(np.float16))
+    words = P.mask_words(np.eye(M, dtype=bool))
+    want = B.ghd_masked_attention_q4(q, cache, 0, _dev(words), kv)
+    words[:, 1] = -1
+    words[:, 0] |= np.int64(-1) << np.int64(M)
+    assert torch.equal(B.ghd_masked_attention_q4(q, cache, 0, _dev(words), kv), want)
+    assert torch.isfinite(want).all()
+
+
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("M,kv_len", [(9, 40), (70, 3)])
+def test_nan_in_a_drafted_row_reaches_those_who_see_it(where, value, M, kv_len):
+    print("q4 nan", where, value, M, kv_len, flush=True)
+    d, nh, nkv, bad = 128, 4, 2, 5
+    rng = _rng(where, M)
+    see = np.tril(rng.random((M, M)) < 0.4) | np.eye(M, dtype=bool)
+    T = kv_len + M
+    k, v = _rows(rng, T, nkv, d), _rows(rng, T, nkv, d)
+    q = _dev(rng.standard_normal((M, nh, d)).astype(np.float16))
+    outs = []
+    for spoil in (False, True):
+        if spoil:
+            (k if where == "k" else v)[kv_len + bad, 1, 33] = value
+        cache = _filled(1, nkv, d, -(-T // 32) * 32)
+        B.ghd_kv_append_q4(cache, 0, _dev(k), _dev(v), 0)
+        outs.append(B.ghd_masked_attention_q4(q, cache, 0, _dev(P.mask_words(see)), kv_len).cpu().numpy())
+    hit = np.zeros((M, nh, d), bool)
+    hit[see[:, bad], 2:] = True                          # the query heads of key head 1
+    if where == "v":
+        hit[..., :32] = hit[..., 64:] = False            # the group of channel 33
+    assert np.isnan(outs[1][hit]).all()
+    assert np.array_equal(outs[1][~hit], outs[0][~hit])
+
+
+def test_attention_same_bits_every_time_and_on_another_stream():
+    rng = _rng("runs")
+    M, nh, nkv, d, kv = 24, 16, 4, 128, 3000
+    cache = B.KvQ4(1, nkv, d, 3072)
+    B.ghd_kv_append_q4(cache, 0, _dev(_rows(rng, kv + M, nkv, d)), _dev(_rows(rng, kv + M, nkv, d)), 0)
+    q, parent = _dev(rng.standard_normal((M, nh, d)).astype(np.float16)), _dev(_random_parent(rng, M, "random"))
+    first = B.ghd_tree_attention_q4(q, cache, 0, parent, kv)
+    for _ in range(4):
+        assert torch.equal(first, B.ghd_tree_attention_q4(q, cache, 0, parent, kv))
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        again = B.ghd_tree_attention_q4(q, cache, 0, parent, kv)
+    torch.cuda.current_stream().wait_stream(other)
+    assert torch.equal(first, again)
+
+
+def test_heads_more_than_4_gib_apart():
+    """Offsets inside a long cache pass 32 bits."""
+    rng = _rng("far")
+    nkv, d, cap, M, kv = 3, 128, 1 << 24, 6, 50
+    n = B.lib().ghd_kv_q4_bytes(nkv, cap, d)
+    assert n * 2 // 3 > 1 << 31
+    cache = B.KvQ4.__new__(B.KvQ4)
+    cache.L, cache.nkv, cache.d, cache.capacity = 1, nkv, d, cap
+    cache.k, cache.v = (torch.empty((1, n), dtype=torch.uint8, device="cuda") for _ in range(2))
+    cache.kv = (B.KV * 1)(B.KV(cache.k.data_ptr(), cache.v.data_ptr()))
+    k, v = _rows(rng, kv + M, nkv, d), _rows(rng, kv + M, nkv, d)
+    q, parent = rng.standard_normal((M, nkv, d)).astype(np.float16), _random_parent(rng, M, "random")
+    B.ghd_kv_append_q4(cache, 0, _dev(k), _dev(v), 0)
+    got = B.ghd_tree_attention_q4(_dev(q), cache, 0, _dev(parent), kv).cpu().numpy()
+    want, tol = P.attention(q, P.held(k), P.held(v), P.sees_of_parent(parent), kv, 1 / math.sqrt(d))
+    _close(got, want, tol)
+    # and rows far behind in a head
+    at = cap - 40
+    B.ghd_kv_append_q4(cache, 0, _dev(k[:40]), _dev(v[:40]), at)
+    res = _dev(np.array([3, 0, 0, 11, 39], np.int32))
+    B.ghd_commit_path_q4(cache, res, 40, at)
+    kr, vr = (t.cpu().numpy()[0] for t in B.ghd_kv_read_q4(cache, at, 40))
+    for got, x in ((kr, k), (vr, v)):
+        want = P.held(x[:40]).copy()
+        want[1], want[2] = want[11].copy(), want[39].copy()
+        assert np.array_equal(got, want)
+
+
+# ---- together -------------------------------------------------------------------------
+def test_a_captured_step_replays_like_the_eager_one():
+    """Linear, append, attention and commit in a graph, replayed with other work in between."""
+    rng = _rng("graph")
+    M, nh, nkv, d, kv, group = 12, 8, 2, 64, 333, 64
+    H, N = nh * d, (nh + 2 * nkv) * d
+    codes, scales, z = _weights(rng, N, H, group, True)
+    Wq = B.ghd_pack_weight_q4(_dev(codes), _dev(scales), _dev(z), group)
+    cache = B.KvQ4(1, nkv, d, 384)
+    B.ghd_kv_append_q4(cache, 0, _dev(_rows(rng, kv, nkv, d)), _dev(_rows(rng, kv, nkv, d)), 0)
+    x, parent = _dev(rng.standard_normal((M, H)).astype(np.float16)), _dev(_random_parent(rng, M, "random"))
+    res = _dev(np.array([3, 0, 0, 5, 9], np.int32))
+    y = torch.empty((M, N), dtype=torch.float16, device="cuda")
+    q2, out = (torch.empty((M, nh, d), dtype=torch.float16, device="cuda") for _ in range(2))
+    ws = B.workspace(max(B.ghd_linear_q4_workspace_bytes(M, N, H), B.ghd_attention_q4_workspace_bytes(M, kv, nh, nkv, d)))
+
+    def step():
+        B.ghd_linear_q4(x, Wq, N, group, ws=ws, y=y)
+        q, k, v = y[:, :H].view(M, nh, d), y[:, H:H + nkv * d].view(M, nkv, d), y[:, H + nkv * d:].view(M, nkv, d)
+        B.ghd_kv_append_q4(cache, 0, k, v, kv, q=q, parent=parent, rope_base=BASE, q_out=q2)
+        B.ghd_tree_attention_q4(q2, cache, 0, parent, kv, ws=ws, out=out)
+        B.ghd_commit_path_q4(cache, res, M, kv)
+
+    step()
+    want = [t.clone() for t in (y, q2, out, cache.k, cache.v)]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        for t in (y, q2, out):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip((y, q2, out, cache.k, cache.v), want):
+            assert torch.equal(t, w)
