@@ -117,7 +117,7 @@ struct Q4Linear {
     bool out16;
 };
 size_t q4_linear_bytes(int M, int N, int K);
-ghd_status launch_q4_linear(Q4Linear a, void* ws, hipStream_t st);
+ghd_status launch_q4_linear(const Q4Linear& a, void* ws, hipStream_t st);
 ghd_status launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int N, int K, int group,
                           hipStream_t st);
 
