@@ -42,38 +42,46 @@ static inline size_t q4_weight_bytes(int N, int K, int group)
 
 #ifdef __HIPCC__
 // ---- codes to numbers --------------------------------------------------------------------
-__device__ __forceinline__ half2_ q4_bits(uint32_t word, uint32_t mask)
-{
-    return __builtin_bit_cast(half2_, (word & mask) | 0x64006400u);
-}
+// Masks and 1024.0 are kept in registers: as literals they make an AND and an OR of 8 bytes each out of one instruction.
+struct Q4Bits {
+    uint32_t low, high, k1024;
+    __device__ __forceinline__ Q4Bits() : low(0x000f000fu), high(0x00f000f0u), k1024(0x64006400u)
+    {
+        asm("" : "+s"(low), "+s"(high), "+v"(k1024));
+    }
+    __device__ __forceinline__ half2_ operator()(uint32_t word, uint32_t mask) const
+    {
+        return __builtin_bit_cast(half2_, (word & mask) | k1024);
+    }
+};
 __device__ __forceinline__ half2_ pair_of(half_t x) { return (half2_){x, x}; }
 __device__ __forceinline__ half8 join(half2_ a, half2_ b, half2_ c, half2_ d)
 {
     return (half8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // the codes of a word, less a zero point, exactly: off = -(1024 + zero) (fp16 holds whole numbers up to 2048)
-__device__ __forceinline__ half8 q4_codes(uint32_t w, half2_ off)
+__device__ __forceinline__ half8 q4_codes(const Q4Bits& bits, uint32_t w, half2_ off)
 {
     const half2_ off16 = off + pair_of((half_t)960.f);         // -(64 + zero)
     const half2_ sixteenth = pair_of((half_t)0.0625f);
     const uint32_t v = w >> 8;
-    return join(q4_bits(w, 0x000f000fu) + off, __builtin_elementwise_fma(q4_bits(w, 0x00f000f0u), sixteenth, off16),
-                q4_bits(v, 0x000f000fu) + off, __builtin_elementwise_fma(q4_bits(v, 0x00f000f0u), sixteenth, off16));
+    return join(bits(w, bits.low) + off, __builtin_elementwise_fma(bits(w, bits.high), sixteenth, off16),
+                bits(v, bits.low) + off, __builtin_elementwise_fma(bits(v, bits.high), sixteenth, off16));
 }
 // fp16(lo + code * scale) of the codes of a word, pair by pair
-__device__ __forceinline__ half8 q4_values(uint32_t w, const half2_ lo[4], const half2_ scale[4])
+__device__ __forceinline__ half8 q4_values(const Q4Bits& bits, uint32_t w, const half2_ lo[4], const half2_ scale[4])
 {
-    const half8 c = q4_codes(w, pair_of((half_t)-1024.f));
+    const half8 c = q4_codes(bits, w, pair_of((half_t)-1024.f));
     half2_ r[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p)
         r[p] = __builtin_elementwise_fma((half2_){c[2 * p], c[2 * p + 1]}, scale[p], lo[p]);
     return join(r[0], r[1], r[2], r[3]);
 }
-__device__ __forceinline__ half8 q4_values(uint32_t w, half2_ lo, half2_ scale)
+__device__ __forceinline__ half8 q4_values(const Q4Bits& bits, uint32_t w, half2_ lo, half2_ scale)
 {
     const half2_ l[4] = {lo, lo, lo, lo}, s[4] = {scale, scale, scale, scale};
-    return q4_values(w, l, s);
+    return q4_values(bits, w, l, s);
 }
 #endif
 

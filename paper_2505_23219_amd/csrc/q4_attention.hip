@@ -70,6 +70,7 @@ __global__ __launch_bounds__(kQ4Waves * 64) void k_q4_attention(const Q4Attn a, 
             if (in) q[s][mt] = *(const half8*)(qr + 8 * s);
         }
     }
+    const Q4Bits bits;
     const float c = a.scale * 1.4426950408889634f;
     floatx4 o[CT][MT];
     float m[MT], l[MT];
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(kQ4Waves * 64) void k_q4_attention(const Q4Attn a, 
             for (int mt = 0; mt < MT; ++mt) s[h][mt] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const half8 ka = q4_values(kw[h][k], pair_of(km[h][0]), pair_of(km[h][1]));
+                const half8 ka = q4_values(bits, kw[h][k], pair_of(km[h][0]), pair_of(km[h][1]));
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
                     s[h][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, q[k][mt], s[h][mt], 0, 0, 0);
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(kQ4Waves * 64) void k_q4_attention(const Q4Attn a, 
                 lo[e] = (half2_){vlo[ct / 2][2 * e], vlo[ct / 2][2 * e + 1]};
                 sc[e] = (half2_){vs[ct / 2][2 * e], vs[ct / 2][2 * e + 1]};
             }
-            const half8 va = q4_values(vw[ct / 4][ct % 4], lo, sc);
+            const half8 va = q4_values(bits, vw[ct / 4][ct % 4], lo, sc);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
                 o[ct][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, p[mt], o[ct][mt], 0, 0, 0);

@@ -338,13 +338,14 @@ __global__ __launch_bounds__(256) void k_q4_read(const Q4Layers a, int nkv, int 
     const size_t out0 = (size_t)layer * rows * nkv * D + (size_t)head * D;
     const int64_t step = (int64_t)nkv * D;
     const char* kt = a.k[layer] + tile;
+    const Q4Bits bits;
 #pragma unroll
     for (int u = 0; u < D / 64; ++u) {                                   // 8 rows of D / 8 words
         const int e = lane + 64 * u, key = e / (D / 8), w = e % (D / 8), row = first + key;
         const uint32_t word = *(const uint32_t*)(kt + (in_tile + key) * (D / 2) + w * 4);
         const half2_ m = *(const half2_*)(kt + q4_codes_bytes(D) + ((in_tile + key) * (D / 32) + w / 4) * 4);
         if (row >= 0 && row < rows)
-            *(half8*)(ko + out0 + row * step + w * 8) = q4_values(word, pair_of(m[0]), pair_of(m[1]));
+            *(half8*)(ko + out0 + row * step + w * 8) = q4_values(bits, word, pair_of(m[0]), pair_of(m[1]));
     }
     const char* vt = a.v[layer] + tile;
     constexpr int kHalves = 128 / D, kKeys = 8 / kHalves;
@@ -357,8 +358,8 @@ __global__ __launch_bounds__(256) void k_q4_read(const Q4Layers a, int nkv, int 
         l2[p] = (half2_){lo[2 * p], lo[2 * p + 1]};
         s2[p] = (half2_){s[2 * p], s[2 * p + 1]};
     }
-    const half8 x0 = q4_values(((const uint32_t*)vt)[q4_v_word(c, octet % 4)], l2, s2);
-    const half8 x1 = q4_values(((const uint32_t*)vt)[q4_v_word(c + 1, octet % 4)], l2, s2);
+    const half8 x0 = q4_values(bits, ((const uint32_t*)vt)[q4_v_word(c, octet % 4)], l2, s2);
+    const half8 x1 = q4_values(bits, ((const uint32_t*)vt)[q4_v_word(c + 1, octet % 4)], l2, s2);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int row = first + j;
