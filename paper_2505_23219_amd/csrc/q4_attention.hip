@@ -3,14 +3,16 @@
 // out[i, h] = softmax over the keys that node i sees of (scale q . K^) applied to V^, where K^ and V^ are the fp16
 // numbers that the codes stand for (q4.h).  A key head's query rows - M nodes by nh / nkv heads - are the columns of
 // S^T = K^ q^T and O^T = V^T P^T, so softmax statistics are a lane's own and the probabilities come out as the operand of
-// the second product.  A wavefront takes 32 keys at a time by itself: 32 bytes of codes a lane, turned into fp16 operands in
-// registers; running maximum and sum in 32 bits, probabilities rounded to fp16 (they are at most 1).
+// the second product.  Running maximum and sum are kept in 32 bits; probabilities are rounded to fp16, relative to a maximum
+// that lags by up to 2^8 (fp16 holds that as exactly, and sums are rescaled seldom).
+//
+// Up to 16 query rows a wavefront takes 32 keys at a time by itself, codes straight into operand registers: what counts is
+// that the cache streams.  Above, the wavefronts of a workgroup have 16 rows each and share the conversion of the codes, which
+// takes longer than the products of 16 rows: each converts a piece of the keys to come into LDS, as operands.
 #include "q4.h"
 #include "attention_impl.h"
 
 namespace ghd {
-
-constexpr int kQ4Waves = 4;
 
 typedef uint32_t word2 __attribute__((ext_vector_type(2)));
 typedef uint32_t word4 __attribute__((ext_vector_type(4)));
@@ -19,6 +21,7 @@ typedef uint32_t word4 __attribute__((ext_vector_type(4)));
 // before that are committed, and seen
 __device__ __forceinline__ uint32_t q4_mask32(uint64_t lo, uint64_t hi, int base)
 {
+    if (base <= -32) return ~0u;
     if (base < 0) return (uint32_t)(lo << -base) | ((1u << -base) - 1u);
     if (base >= 128) return 0;
     if (base >= 64) return (uint32_t)(hi >> (base - 64));
@@ -32,321 +35,582 @@ __device__ __forceinline__ bool q4_sees(const uint64_t* mask, int node, int M)
     return (mask[2 * node] & lo) | (mask[2 * node + 1] & hi);
 }
 
-template <int D, int MT>
-__global__ __launch_bounds__(kQ4Waves * 64) void k_q4_attention(const Q4Attn a, int splits, int blocks)
+// The masks of all nodes to LDS; the workgroup's barrier is the caller's.
+__device__ __forceinline__ void q4_masks(const Q4Attn& a, uint64_t* s_mask)
 {
-    constexpr int CT = D / 16, KS = D / 32;
-    __shared__ uint64_t s_mask[2 * GHD_MAX_M];
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x % splits, block = blockIdx.x / splits % blocks, head = blockIdx.x / splits / blocks;
-    const int rep = a.nh / a.nkv, R = a.M * rep, total = a.kv_len + a.M;
-    const int ntiles = (total + kQ4Tile - 1) / kQ4Tile;
-    const int t0 = (int)((int64_t)ntiles * split / splits), t1 = (int)((int64_t)ntiles * (split + 1) / splits);
-    if (t1 * kQ4Tile > a.kv_len) {                     // masks are looked at
-        if (a.mask) {
-            if ((int)threadIdx.x < 2 * a.M) {
-                const int w = threadIdx.x & 1, left = a.M - 64 * w;      // bits of this word that mean something
-                const uint64_t m = a.mask[threadIdx.x];
-                s_mask[threadIdx.x] = left >= 64 ? m : left <= 0 ? 0 : m & ((1ull << left) - 1);
-            }
-        } else if (threadIdx.x < 64) {
-            store_masks(tree_nodes<2, true>(a.parent[min(lane, a.M - 1)], a.parent[min(lane + 64, a.M - 1)], a.M, lane),
-                        a.M, lane, s_mask);
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (a.mask) {
+        for (int e = tid; e < 2 * a.M; e += blockDim.x) {
+            const int left = a.M - 64 * (e & 1);                   // bits of this word that mean something
+            s_mask[e] = left >= 64 ? a.mask[e] : left <= 0 ? 0 : a.mask[e] & ((1ull << left) - 1);
         }
-        __syncthreads();
-    }
-    half8 q[KS][MT];
-    int node[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int row = block * 16 * MT + mt * 16 + col;
-        const bool in = row < R;
-        node[mt] = in ? row / rep : 0;
-        const half_t* qr = a.q + ((size_t)node[mt] * a.nh + head * rep + (in ? row - node[mt] * rep : 0)) * D + g * (D / 4);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            q[s][mt] = (half8){0, 0, 0, 0, 0, 0, 0, 0};
-            if (in) q[s][mt] = *(const half8*)(qr + 8 * s);
-        }
-    }
-    const Q4Bits bits;
-    const float c = a.scale * 1.4426950408889634f;
-    floatx4 o[CT][MT];
-    float m[MT], l[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        m[mt] = -INFINITY;
-        l[mt] = 0.f;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[ct][mt] = (floatx4){0.f, 0.f, 0.f, 0.f};
-    }
-    const char* kh = a.k + q4_tile_at(head, 0, a.tiles, D);
-    const char* vh = a.v + q4_tile_at(head, 0, a.tiles, D);
-    for (int t = t0 + wave; t < t1; t += kQ4Waves) {
-        const char* kt = kh + (size_t)t * q4_tile_bytes(D);
-        const char* vt = vh + (size_t)t * q4_tile_bytes(D);
-        // K: operand row r of half h is key 8 (r / 4) + 4 h + r % 4, so that a lane's 8 scores of a column are
-        // those of keys 8 g .. 8 g + 7, the probabilities it holds in the second product
-        uint32_t kw[2][KS];
-        half2_ km[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int key = 8 * (col >> 2) + 4 * h + (col & 3);
-            if constexpr (D == 128) {
-                const word4 w = *(const word4*)(kt + key * 64 + g * 16);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[h][s] = w[s];
-                km[h] = *(const half2_*)(kt + q4_codes_bytes(D) + (key * 4 + g) * 4);
-            } else {
-                const word2 w = *(const word2*)(kt + key * 32 + g * 8);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[h][s] = w[s];
-                km[h] = *(const half2_*)(kt + q4_codes_bytes(D) + (key * 2 + (g >> 1)) * 4);
-            }
-        }
-        word4 vw[CT / 4];
-        half8 vlo[CT / 2], vs[CT / 2];
-#pragma unroll
-        for (int i = 0; i < CT / 4; ++i) vw[i] = *(const word4*)(vt + ((i * 4 + g) * 16 + col) * 16);
-#pragma unroll
-        for (int i = 0; i < CT / 2; ++i) {
-            vlo[i] = *(const half8*)(vt + q4_codes_bytes(D) + i * 128 + g * 16);
-            vs[i] = *(const half8*)(vt + q4_codes_bytes(D) + i * 128 + 64 + g * 16);
-        }
-        floatx4 s[2][MT];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[h][mt] = (floatx4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const half8 ka = q4_values(bits, kw[h][k], pair_of(km[h][0]), pair_of(km[h][1]));
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    s[h][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, q[k][mt], s[h][mt], 0, 0, 0);
-            }
-        }
-        const int base = t * kQ4Tile - a.kv_len;
-        const bool masked = base + kQ4Tile > 0;
-        uint32_t see[MT];
-        uint32_t nan_keys = 0;       // keys of this lane (bit 8 i + key) whose lo or scale of group i is no number
-        if (masked) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                see[mt] = q4_mask32(s_mask[2 * node[mt]], s_mask[2 * node[mt] + 1], base) >> 8 * g & 255u;
-            // Values of rows that are not there may be anything, and 0 times anything is no 0: they count as 0, and so
-            // does what reads as NaN (a NaN was appended), which only reaches the rows that see it, below.
-#pragma unroll
-            for (int i = 0; i < CT / 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool there = t * kQ4Tile + 8 * g + e < total;
-                    const bool number = (__builtin_bit_cast(uint16_t, (half_t)vlo[i][e]) & 0x7c00u) != 0x7c00u &&
-                                        (__builtin_bit_cast(uint16_t, (half_t)vs[i][e]) & 0x7c00u) != 0x7c00u;
-                    if (there && !number) nan_keys |= 1u << (8 * i + e);
-                    if (!there || !number) vlo[i][e] = vs[i][e] = 0;
-                }
-        }
-        half8 p[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float v[8], top = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = s[e >> 2][mt][e & 3] * c;
-                if (masked && !(see[mt] >> e & 1)) v[e] = -INFINITY;
-                top = fmaxf(top, v[e]);
-            }
-            top = max_over_groups(top);
-            if (top > m[mt]) {       // (the same in the four lanes of a column)
-                const float r = __builtin_amdgcn_exp2f(m[mt] - top);
-                l[mt] *= r;
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) o[ct][mt] *= r;
-                m[mt] = top;
-            }
-            const float off = m[mt] == -INFINITY ? 0.f : m[mt];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = __builtin_amdgcn_exp2f(v[e] - off);
-                l[mt] += x;
-                p[mt][e] = (half_t)x;
-            }
-        }
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            half2_ lo[4], sc[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lo[e] = (half2_){vlo[ct / 2][2 * e], vlo[ct / 2][2 * e + 1]};
-                sc[e] = (half2_){vs[ct / 2][2 * e], vs[ct / 2][2 * e + 1]};
-            }
-            const half8 va = q4_values(bits, vw[ct / 4][ct % 4], lo, sc);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                o[ct][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, p[mt], o[ct][mt], 0, 0, 0);
-        }
-        if (masked && __ballot(nan_keys != 0)) {
-            // how many keys with a NaN in this channel's group a row sees: a product of ones
-#pragma unroll
-            for (int i = 0; i < CT / 2; ++i) {
-                half8 bad;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bad[e] = nan_keys >> (8 * i + e) & 1 ? (half_t)1.f : (half_t)0.f;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    half8 sees;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sees[e] = see[mt] >> e & 1 ? (half_t)1.f : (half_t)0.f;
-                    const floatx4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, sees, (floatx4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n[e] > 0.f) o[2 * i][mt][e] = o[2 * i + 1][mt][e] = NAN;
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) l[mt] = sum_over_groups(l[mt]);
-    // The wavefronts' states meet in LDS, one after the other into the first one's registers.
-    floatx4* so = (floatx4*)lds;                                // [CT][MT][64]
-    float* sm = (float*)(lds + (size_t)CT * MT * 64 * 16);      // [MT][16][2]
-    for (int w = 1; w < kQ4Waves; ++w) {
-        __syncthreads();
-        if (wave == w) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (g == 0) {
-                    sm[(mt * 16 + col) * 2] = m[mt];
-                    sm[(mt * 16 + col) * 2 + 1] = l[mt];
-                }
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) so[(ct * MT + mt) * 64 + lane] = o[ct][mt];
-            }
-        }
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const float mo = sm[(mt * 16 + col) * 2], lo = sm[(mt * 16 + col) * 2 + 1];
-                const float mn = fmaxf(m[mt], mo), off = mn == -INFINITY ? 0.f : mn;
-                const float f0 = __builtin_amdgcn_exp2f(m[mt] - off), f1 = __builtin_amdgcn_exp2f(mo - off);
-                m[mt] = mn;
-                l[mt] = l[mt] * f0 + lo * f1;
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) o[ct][mt] = o[ct][mt] * f0 + so[(ct * MT + mt) * 64 + lane] * f1;
-            }
-        }
-    }
-    if (wave != 0) return;
-    if (splits > 1) {
-        const size_t unit = blockIdx.x;
-        floatx4* po = (floatx4*)a.o_part + unit * (CT * MT * 64);
-        float* pm = a.ml_part + unit * (MT * 32);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            if (g == 0) {
-                pm[(mt * 16 + col) * 2] = m[mt];
-                pm[(mt * 16 + col) * 2 + 1] = l[mt];
-            }
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) po[(ct * MT + mt) * 64 + lane] = o[ct][mt];
-        }
-        return;
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int row = block * 16 * MT + mt * 16 + col;
-        if (row >= R) continue;
-        // a row that sees no key gives zeros
-        const bool none = a.kv_len == 0 && a.mask && !q4_sees(a.mask, node[mt], a.M);
-        const float r = 1.f / l[mt];
-        half_t* dst = a.out + ((size_t)node[mt] * a.nh + head * rep + row - node[mt] * rep) * D + 4 * g;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            half4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = none ? (half_t)0.f : (half_t)(o[ct][mt][e] * r);
-            *(half4*)(dst + ct * 16) = y;
-        }
+    } else if (tid < 64) {
+        store_masks(tree_nodes<2, true>(a.parent[min(lane, a.M - 1)], a.parent[min(lane + 64, a.M - 1)], a.M, lane), a.M, lane, s_mask);
     }
 }
 
-// Parts of a head's keys to its rows.  A wavefront takes one fragment of 16 channels by 16 rows.
-template <int D, int MT>
-__global__ __launch_bounds__(256) void k_q4_join(const Q4Attn a, int splits, int blocks, int items)
-{
-    constexpr int CT = D / 16;
-    const int lane = threadIdx.x & 63, item = blockIdx.x * 4 + (threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    if (item >= items) return;
-    const int frag = item % (CT * MT), hb = item / (CT * MT), mt = frag % MT, ct = frag / MT;
-    const int block = hb % blocks, head = hb / blocks;
-    const size_t unit0 = (size_t)hb * splits;
-    float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, a.ml_part[(unit0 + s) * (MT * 32) + (mt * 16 + col) * 2]);
-    const float off = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-        const float* pm = a.ml_part + (unit0 + s) * (MT * 32) + (mt * 16 + col) * 2;
-        const float f = __builtin_amdgcn_exp2f(pm[0] - off);
-        l += pm[1] * f;
-        o += ((const floatx4*)a.o_part)[(unit0 + s) * (CT * MT * 64) + frag * 64 + lane] * f;
+// 16 keys of a tile (half h), as a lane (g, col) has them: operand row r is key 8 (r / 4) + 4 h + r % 4, so that a lane's 8
+// scores of a column are those of keys 8 g .. 8 g + 7, the probabilities it holds in the second product.  Its channels, D / 4
+// from g D / 4 on, are the k-steps' in turn.
+template <int D>
+struct Q4RawK {
+    uint32_t w[D / 32];
+    half2_ m;
+    __device__ __forceinline__ void load(const char* tile, int h, int col, int g)
+    {
+        const int key = 8 * (col >> 2) + 4 * h + (col & 3);
+        if constexpr (D == 128) {
+            const word4 v = *(const word4*)(tile + key * 64 + g * 16);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) w[s] = v[s];
+            m = *(const half2_*)(tile + q4_codes_bytes(D) + (key * 4 + g) * 4);
+        } else {
+            const word2 v = *(const word2*)(tile + key * 32 + g * 8);
+            w[0] = v[0];
+            w[1] = v[1];
+            m = *(const half2_*)(tile + q4_codes_bytes(D) + (key * 2 + (g >> 1)) * 4);
+        }
     }
-    const int rep = a.nh / a.nkv, row = block * 16 * MT + mt * 16 + col;
-    if (row >= a.M * rep) return;
+    __device__ __forceinline__ half8 operand(const Q4Bits& bits, int s) const
+    {
+        return q4_values(bits, w[s], pair_of(m[0]), pair_of(m[1]));
+    }
+};
+
+struct Q4Pairs {
+    half2_ lo[4], s[4];                // of a lane's 8 keys
+    __device__ __forceinline__ void set(half8 l, half8 sc)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            lo[e] = (half2_){l[2 * e], l[2 * e + 1]};
+            s[e] = (half2_){sc[2 * e], sc[2 * e + 1]};
+        }
+    }
+};
+
+// Values of rows that are not there may be anything, and 0 times anything is no 0: they count as 0.  So does what reads as NaN
+// (a NaN was appended), which only reaches the rows that see it (q4_poison); returned: which of the 8 keys those are.
+__device__ __forceinline__ uint32_t q4_clean(half8& lo, half8& s, int key0, int total)
+{
+    word4 l = __builtin_bit_cast(word4, lo), c = __builtin_bit_cast(word4, s);
+    const int there = total - key0;                            // so many of the 8 keys, from the first on
+    uint32_t bad = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t in = (there > 2 * p ? 0xffffu : 0u) | (there > 2 * p + 1 ? 0xffff0000u : 0u);
+        // an exponent of all ones, plus one, carries into the sign
+        const uint32_t odd = (((l[p] & 0x7c007c00u) + 0x04000400u) | ((c[p] & 0x7c007c00u) + 0x04000400u)) & 0x80008000u & in;
+        const uint32_t keep = in & ~((odd >> 15) * 0xffffu);
+        l[p] &= keep;
+        c[p] &= keep;
+        bad |= (odd >> 15 & 1u) << 2 * p | odd >> 31 << (2 * p + 1);
+    }
+    lo = __builtin_bit_cast(half8, l);
+    s = __builtin_bit_cast(half8, c);
+    return bad;
+}
+
+// A row tile's state over the keys so far.
+template <int D>
+struct Q4State {
+    floatx4 o[D / 16], l;              // l: the sum of the (rounded) probabilities, by a product with ones; four times the same
+    float m;
+    __device__ __forceinline__ Q4State() : l((floatx4){0.f, 0.f, 0.f, 0.f}), m(-INFINITY)
+    {
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) o[ct] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    }
+    // scores (of this lane's 8 keys) to probabilities; c, what makes powers of two of them, is not negative
+    template <bool MASKED>
+    __device__ __forceinline__ half8 probabilities(const floatx4 (&s)[2], float c, uint32_t see)
+    {
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = s[e >> 2][e & 3];
+            top = fmaxf(top, MASKED && !(see >> e & 1) ? -INFINITY : v);
+        }
+        top = max_over_groups(top);
+        top = top == -INFINITY ? top : top * c;
+        if (__ballot(top > m + 8.f)) {
+            const float now = fmaxf(m, top), r = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            l *= r;
+#pragma unroll
+            for (int ct = 0; ct < D / 16; ++ct) o[ct] *= r;
+            m = now;
+        }
+        const float off = m == -INFINITY ? 0.f : -m;
+        half2_ p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            floatx2 x;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                x[u] = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][2 * (e & 1) + u], c, off));
+                if (MASKED && !(see >> (2 * e + u) & 1)) x[u] = 0.f;
+            }
+            p[e] = __builtin_convertvector(x, half2_);
+        }
+        const half8 all = join(p[0], p[1], p[2], p[3]);
+        const half_t one = (half_t)1.f;
+        l = __builtin_amdgcn_mfma_f32_16x16x32_f16((half8){one, one, one, one, one, one, one, one}, all, l, 0, 0, 0);
+        return all;
+    }
+    // NaN in the channels of group i for rows that see one of the keys with a NaN there: how many they see is a product of ones
+    __device__ __forceinline__ void poison(int i, uint32_t bad, uint32_t see)
+    {
+        half8 b, v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            b[e] = bad >> e & 1 ? (half_t)1.f : (half_t)0.f;
+            v[e] = see >> e & 1 ? (half_t)1.f : (half_t)0.f;
+        }
+        const floatx4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, v, (floatx4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n[e] > 0.f) o[2 * i][e] = o[2 * i + 1][e] = NAN;
+    }
+};
+
+// What a launch works on: a head's rows in blocks, its keys in parts.
+struct Q4Item {
+    int head, block, split, rep, R, total;
+    __device__ __forceinline__ Q4Item(const Q4Attn& a, int splits, int blocks)
+    {
+        split = blockIdx.x % splits;
+        block = blockIdx.x / splits % blocks;
+        head = blockIdx.x / splits / blocks;
+        rep = a.nh / a.nkv;
+        R = a.M * rep;
+        total = a.kv_len + a.M;
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void q4_queries(const Q4Attn& a, const Q4Item& it, int row, int g, half8 (&q)[D / 32])
+{
+    const int node = row / it.rep;
+    const half_t* p = a.q + ((size_t)node * a.nh + it.head * it.rep + row - node * it.rep) * D + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+        q[s] = (half8){0, 0, 0, 0, 0, 0, 0, 0};
+        if (row < it.R) q[s] = *(const half8*)(p + 8 * s);
+        if (a.scale < 0.f) q[s] = -q[s];
+    }
+}
+
+// the four channels of tile ct of a row, the sums divided by l; a row that sees no key gives zeros
+template <int D>
+__device__ __forceinline__ void q4_out(const Q4Attn& a, int head, int rep, int row, int ct, int g, floatx4 o, float l)
+{
     const int node = row / rep;
     const bool none = a.kv_len == 0 && a.mask && !q4_sees(a.mask, node, a.M);
+    const float r = 1.f / l;
     half4 y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = none ? (half_t)0.f : (half_t)(o[e] / l);
+    for (int e = 0; e < 4; ++e) y[e] = none ? (half_t)0.f : (half_t)(o[e] * r);
     *(half4*)(a.out + ((size_t)node * a.nh + head * rep + row - node * rep) * D + ct * 16 + 4 * g) = y;
 }
 
-struct Q4AttnCut {
-    int mt, blocks, splits;
+// ---- up to 16 rows -----------------------------------------------------------------------
+constexpr int kQ4KeyWaves = 4;
+
+// a tile of 32 keys, as a wavefront has it on its way
+template <int D>
+struct Q4Tile {
+    Q4RawK<D> k[2];
+    word4 v[D / 64];
+    half8 lo, s;                       // of the lane's 8 keys and group col % (D / 32): the four (two) lanes side by side have all
+    __device__ __forceinline__ void load(const char* kt, const char* vt, int col, int g)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) k[h].load(kt, h, col, g);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) v[i] = *(const word4*)(vt + ((i * 4 + g) * 16 + col) * 16);
+        const char* m = vt + q4_codes_bytes(D) + col % (D / 32) * 128 + g * 16;
+        lo = *(const half8*)m;
+        s = *(const half8*)(m + 64);
+    }
 };
+
+// x of the lane that has group i, among the lanes side by side that have all
+template <int D, int I>
+__device__ __forceinline__ half8 q4_of_group(half8 x)
+{
+    constexpr int kCtrl = D == 128 ? I * 0x55 : I ? 0xF5 : 0xA0;
+    word4 w = __builtin_bit_cast(word4, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[e], kCtrl, 0xf, 0xf, true);
+    return __builtin_bit_cast(half8, w);
+}
+
+template <int D, bool MASKED>
+__device__ __forceinline__ void q4_tile(const Q4Attn& a, const Q4Bits& bits, Q4State<D>& st, const half8 (&q)[D / 32], Q4Tile<D>& t,
+                                        float c, int tile, int total, int g, const uint64_t* mask)
+{
+    floatx4 s[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k[h].operand(bits, k), q[k], s[h], 0, 0, 0);
+    }
+    uint32_t see = 0, bad = 0;
+    if constexpr (MASKED) {
+        see = q4_mask32(mask[0], mask[1], tile * kQ4Tile - a.kv_len) >> 8 * g & 255u;
+        bad = q4_clean(t.lo, t.s, tile * kQ4Tile + 8 * g, total);
+    }
+    const half8 p = st.template probabilities<MASKED>(s, c, see);
+    auto group = [&](auto I) {
+        constexpr int i = decltype(I)::value;
+        Q4Pairs m;
+        m.set(q4_of_group<D, i>(t.lo), q4_of_group<D, i>(t.s));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int ct = 2 * i + e;
+            st.o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q4_values(bits, t.v[ct / 4][ct % 4], m.lo, m.s), p, st.o[ct], 0, 0, 0);
+        }
+        if constexpr (MASKED) {
+            constexpr int kCtrl = D == 128 ? i * 0x55 : i ? 0xF5 : 0xA0;
+            const uint32_t b = (uint32_t)__builtin_amdgcn_mov_dpp((int)bad, kCtrl, 0xf, 0xf, true);
+            if (__ballot(b != 0)) st.poison(i, b, see);
+        }
+    };
+    group(std::integral_constant<int, 0>());
+    group(std::integral_constant<int, 1>());
+    if constexpr (D == 128) {
+        group(std::integral_constant<int, 2>());
+        group(std::integral_constant<int, 3>());
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const Q4Attn a, int splits)
+{
+    constexpr int CT = D / 16;
+    __shared__ uint64_t s_mask[2 * GHD_MAX_M];
+    __shared__ floatx4 s_o[kQ4KeyWaves][CT][64];
+    __shared__ floatx2 s_ml[kQ4KeyWaves][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const Q4Item it(a, splits, 1);
+    const int ntiles = (it.total + kQ4Tile - 1) / kQ4Tile, plain = a.kv_len / kQ4Tile;     // tiles whose keys all see
+    const int t0 = (int)((int64_t)ntiles * it.split / splits), t1 = (int)((int64_t)ntiles * (it.split + 1) / splits);
+    const char* kh = a.k + q4_tile_at(it.head, 0, a.tiles, D);
+    const char* vh = a.v + q4_tile_at(it.head, 0, a.tiles, D);
+    auto load = [&](Q4Tile<D>& t, int tile) {
+        const size_t at = (size_t)min(tile, t1 - 1) * q4_tile_bytes(D);
+        t.load(kh + at, vh + at, col, g);
+    };
+    Q4Tile<D> tile[2];
+    load(tile[0], t0 + wave);
+    half8 q[D / 32];
+    q4_queries<D>(a, it, col, g, q);
+    if (t1 > plain) {
+        q4_masks(a, s_mask);
+        __syncthreads();
+    }
+    const Q4Bits bits;
+    const float c = fabsf(a.scale) * 1.4426950408889634f;
+    Q4State<D> st;
+    const int t_plain = min(t1, plain);
+    int t = t0 + wave;
+    // (two tiles in turn: a copy of the one on its way would have to wait for it)
+    for (; t < t_plain; t += 2 * kQ4KeyWaves) {
+        load(tile[1], t + kQ4KeyWaves);
+        q4_tile<D, false>(a, bits, st, q, tile[0], c, t, it.total, g, nullptr);
+        if (t + kQ4KeyWaves >= t_plain) {
+            tile[0] = tile[1];
+            t += kQ4KeyWaves;
+            break;
+        }
+        load(tile[0], t + 2 * kQ4KeyWaves);
+        q4_tile<D, false>(a, bits, st, q, tile[1], c, t + kQ4KeyWaves, it.total, g, nullptr);
+    }
+    const uint64_t* mask = s_mask + 2 * (col < it.R ? col / it.rep : 0);
+    for (; t < t1; t += kQ4KeyWaves) {                       // the few that reach into the drafted rows
+        q4_tile<D, true>(a, bits, st, q, tile[0], c, t, it.total, g, mask);
+        load(tile[0], t + kQ4KeyWaves);
+    }
+    // the wavefronts' states meet in LDS; each finishes its share of the channel tiles
+    if (g == 0) s_ml[wave][col] = (floatx2){st.m, st.l[0]};
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) s_o[wave][ct][lane] = st.o[ct];
+    __syncthreads();
+    float m = -INFINITY, l = 0.f, f[kQ4KeyWaves];
+#pragma unroll
+    for (int w = 0; w < kQ4KeyWaves; ++w) m = fmaxf(m, s_ml[w][col][0]);
+    const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < kQ4KeyWaves; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(s_ml[w][col][0] - off);
+        l += s_ml[w][col][1] * f[w];
+    }
+    if (splits > 1 && wave == 0 && g == 0) ((floatx2*)a.ml_part)[(size_t)blockIdx.x * 16 + col] = (floatx2){m, l};
+#pragma unroll
+    for (int j = 0; j < CT / kQ4KeyWaves; ++j) {
+        const int ct = wave * (CT / kQ4KeyWaves) + j;
+        floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kQ4KeyWaves; ++w) o += s_o[w][ct][lane] * f[w];
+        if (splits > 1) ((floatx4*)a.o_part)[((size_t)blockIdx.x * CT + ct) * 64 + lane] = o;
+        else if (col < it.R) q4_out<D>(a, it.head, it.rep, col, ct, g, o, l);
+    }
+}
+
+// ---- more rows ---------------------------------------------------------------------------
+// NR wavefronts of 16 rows.  A stage is 32 keys (64 for eight wavefronts), two buffers of it in LDS as operands; a stage's
+// pieces - 16 keys of K, or 64 channels of 32 keys of V - are converted by a wavefront each (two wavefronts: two each).  Codes
+// of the stage after the next are requested before a stage's products, converted after the next one's.
+template <int D, int NR>
+__global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a, int splits, int blocks)
+{
+    constexpr int CT = D / 16, KS = D / 32, TS = NR == 8 ? 2 : 1;             // tiles a stage
+    constexpr int kKPieces = 2 * TS, kVPieces = D / 64 * TS, kPieces = kKPieces + kVPieces;
+    constexpr int kTileFrags = 2 * KS + CT, kBuf = TS * kTileFrags * 1024;
+    __shared__ uint64_t s_mask[2 * GHD_MAX_M];
+    __shared__ uint8_t s_bad[2][TS][KS][4];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const Q4Item it(a, splits, blocks);
+    const int ntiles = (it.total + kQ4Tile - 1) / kQ4Tile, nstages = (ntiles + TS - 1) / TS;
+    const int s0 = (int)((int64_t)nstages * it.split / splits), s1 = (int)((int64_t)nstages * (it.split + 1) / splits);
+    const char* kh = a.k + q4_tile_at(it.head, 0, a.tiles, D);
+    const char* vh = a.v + q4_tile_at(it.head, 0, a.tiles, D);
+    // A piece as it is requested, the same way for both kinds (a choice between requests ends in copies, which wait for them):
+    // codes; of K the row's (lo, scale), twice, of V lo and scale of group col % 2 of two.
+    static_assert(kPieces <= NR, "a piece a wavefront");
+    const bool of_k = wave < kKPieces;
+    const int vp = wave - kKPieces, part = of_k ? wave % 2 : vp % (D / 64), of_tile = of_k ? wave / 2 : vp / (D / 64);
+    const char* piece_head = of_k ? kh : vh;
+    const int key = 8 * (col >> 2) + 4 * part + (col & 3);                    // (of K)
+    const int off_codes = of_k ? key * (D / 2) + (D == 128 ? g : g >> 1) * 16 : ((part * 4 + g) * 16 + col) * 16;
+    const int off_lo = q4_codes_bytes(D) + (of_k ? key * (D / 8) & ~15 : (2 * part + (col & 1)) * 128 + g * 16);
+    const int off_scale = of_k ? off_lo : off_lo + 64;
+    word4 raw[3];
+    auto load = [&](int stage) {
+        const char* at = piece_head + (size_t)min(min(stage, s1 - 1) * TS + of_tile, ntiles - 1) * q4_tile_bytes(D);
+        raw[0] = *(const word4*)(at + off_codes);
+        raw[1] = *(const word4*)(at + off_lo);
+        raw[2] = *(const word4*)(at + off_scale);
+    };
+    const Q4Bits bits;
+    auto convert = [&](int stage, int buf) {
+        char* to = lds + buf * kBuf + of_tile * kTileFrags * 1024 + lane * 16;
+        if (of_k) {
+            uint32_t m = raw[1][0];
+#pragma unroll
+            for (int e = 1; e < 4; ++e)
+                if ((D == 128 ? g : (key & 1) * 2 + (g >> 1)) == e) m = raw[1][e];
+            const half2_ ms = __builtin_bit_cast(half2_, m);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const uint32_t w = D == 128 ? raw[0][s] : g & 1 ? raw[0][(2 + s) & 3] : raw[0][s];
+                *(half8*)(to + (part * KS + s) * 1024) = q4_values(bits, w, pair_of(ms[0]), pair_of(ms[1]));
+            }
+        } else if (vp < kVPieces) {
+            half8 lo = __builtin_bit_cast(half8, raw[1]), sc = __builtin_bit_cast(half8, raw[2]);
+            if ((stage + 1) * TS * kQ4Tile > a.kv_len) {
+                const uint32_t bad = q4_clean(lo, sc, (stage * TS + of_tile) * kQ4Tile + 8 * g, it.total);
+                if (col < 2) s_bad[buf][of_tile][2 * part + col][g] = (uint8_t)bad;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                Q4Pairs m;
+                if (u == 0) m.set(q4_of_group<64, 0>(lo), q4_of_group<64, 0>(sc));
+                else m.set(q4_of_group<64, 1>(lo), q4_of_group<64, 1>(sc));
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    *(half8*)(to + (2 * KS + 4 * part + 2 * u + x) * 1024) = q4_values(bits, raw[0][2 * u + x], m.lo, m.s);
+            }
+        }
+    };
+    load(s0);
+    const int row0 = it.block * NR * 16 + wave * 16, row = row0 + col;
+    half8 q[KS];
+    q4_queries<D>(a, it, row, g, q);
+    if (s1 * TS * kQ4Tile > a.kv_len) q4_masks(a, s_mask);
+    convert(s0, 0);
+    load(s0 + 1);
+    __syncthreads();
+    const float c = fabsf(a.scale) * 1.4426950408889634f;
+    const uint64_t* mask = s_mask + 2 * (row < it.R ? row / it.rep : 0);
+    Q4State<D> st;
+    auto work = [&](auto MASKED, int stage) {
+        constexpr bool masked = decltype(MASKED)::value;
+        const int buf = (stage - s0) & 1;
+        if (row0 < it.R) {
+#pragma unroll
+            for (int tile = 0; tile < TS; ++tile) {
+                const char* base = lds + buf * kBuf + tile * kTileFrags * 1024 + lane * 16;
+                floatx4 s[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+                        s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const half8*)(base + (h * KS + k) * 1024), q[k], s[h], 0, 0, 0);
+                }
+                uint32_t see = 0;
+                if (masked) see = q4_mask32(mask[0], mask[1], (stage * TS + tile) * kQ4Tile - a.kv_len) >> 8 * g & 255u;
+                const half8 p = st.template probabilities<masked>(s, c, see);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    st.o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const half8*)(base + (2 * KS + ct) * 1024), p, st.o[ct], 0, 0, 0);
+                if (masked)
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        const uint32_t bad = s_bad[buf][tile][i][g];
+                        if (__ballot(bad != 0)) st.poison(i, bad, see);
+                    }
+            }
+        }
+        if (stage + 1 < s1) {
+            convert(stage + 1, buf ^ 1);
+            load(stage + 2);
+        }
+        __syncthreads();
+    };
+    int stage = s0;
+    for (; stage < min(s1, a.kv_len / (TS * kQ4Tile)); ++stage) work(std::false_type(), stage);     // all rows see all keys
+    for (; stage < s1; ++stage) work(std::true_type(), stage);
+    if (splits > 1) {
+        const size_t unit = (size_t)blockIdx.x * NR + wave;
+        if (g == 0) ((floatx2*)a.ml_part)[unit * 16 + col] = (floatx2){st.m, st.l[0]};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) ((floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane] = st.o[ct];
+        return;
+    }
+    if (row < it.R)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) q4_out<D>(a, it.head, it.rep, row, ct, g, st.o[ct], st.l[0]);
+}
+
+// ---- parts of a head's keys to its rows ----------------------------------------------------
+// Four wavefronts take the parts of one fragment - 16 channels by 16 rows - in turn, eight requests at a time.
+template <int D>
+__global__ __launch_bounds__(256) void k_q4_join(const Q4Attn a, int splits, int blocks, int row_tiles)
+{
+    constexpr int CT = D / 16, kAt = 8;
+    __shared__ floatx4 s_o[4][64];
+    __shared__ floatx2 s_ml[4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int ct = blockIdx.x % CT, rt = blockIdx.x / CT % row_tiles, hb = blockIdx.x / CT / row_tiles;
+    const int block = hb % blocks, head = hb / blocks, rep = a.nh / a.nkv, row = (block * row_tiles + rt) * 16 + col;
+    if ((block * row_tiles + rt) * 16 >= a.M * rep) return;
+    float m = -INFINITY, l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = wave; p0 < splits; p0 += 4 * kAt) {
+        floatx2 ml[kAt];
+        floatx4 v[kAt];
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < kAt; ++j) {
+            const size_t unit = ((size_t)hb * splits + min(p0 + 4 * j, splits - 1)) * row_tiles + rt;
+            ml[j] = ((const floatx2*)a.ml_part)[unit * 16 + col];
+            v[j] = ((const floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane];
+        }
+#pragma unroll
+        for (int j = 0; j < kAt; ++j)
+            if (p0 + 4 * j < splits) top = fmaxf(top, ml[j][0]);
+        const float off = top == -INFINITY ? 0.f : top, r = __builtin_amdgcn_exp2f(m - off);
+        l *= r;
+        o *= r;
+#pragma unroll
+        for (int j = 0; j < kAt; ++j)
+            if (p0 + 4 * j < splits) {
+                const float f = __builtin_amdgcn_exp2f(ml[j][0] - off);
+                l += ml[j][1] * f;
+                o += v[j] * f;
+            }
+        m = top;
+    }
+    s_o[wave][lane] = o;
+    if (g == 0) s_ml[wave][col] = (floatx2){m, l};
+    __syncthreads();
+    if (wave != 0 || row >= a.M * rep) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, s_ml[w][col][0]);
+    const float off = top == -INFINITY ? 0.f : top;
+    l = 0.f;
+    o = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ml[w][col][0] - off);
+        l += s_ml[w][col][1] * f;
+        o += s_o[w][lane] * f;
+    }
+    q4_out<D>(a, head, rep, row, ct, g, o, l);
+}
+
+// ---- how a call is divided -----------------------------------------------------------------
+struct Q4AttnCut {
+    int rows, blocks, splits;    // wavefronts of 16 rows in a workgroup, blocks of rows, parts of the keys
+};
+// Parts of the keys cost a launch that joins them (3 us) and what they write: as many as make 256 workgroups, one a compute unit
+// (64 rows of 32 heads over 2112 keys: 4, 8, 16 parts 23.0, 18.3, 20.4 us), and where each then has long to go twice as many or,
+// of the wavefronts that wait for the cache most, three times (128 rows of 40 heads over 8320 keys: 6 parts 48.4, 12 45.5;
+// 1 token of 40 heads over 32000: 6 48.9, 12 44.7, 19 43.7).  No parts where a workgroup is through sooner than a second launch
+// (8 tokens of 8 heads over 308 keys: 1 part 7.4, 2 9.4).
 static Q4AttnCut q4_attn_cut(int M, int kv_len, int nh, int nkv)
 {
     Q4AttnCut c;
-    const int R = M * (nh / nkv), rt = ceil_div(R, 16), ntiles = ceil_div(kv_len + M, kQ4Tile);
-    c.mt = rt <= 1 ? 1 : 2;
-    c.blocks = ceil_div(rt, c.mt);
-    const int items = nkv * c.blocks;
-    c.splits = std::max(1, std::min(ceil_div(ntiles, kQ4Waves), 512 / items));
+    const int rt = ceil_div(M * (nh / nkv), 16), ntiles = ceil_div(kv_len + M, kQ4Tile);
+    c.rows = rt <= 1 ? 1 : rt <= 4 ? 4 : 8;
+    c.blocks = ceil_div(rt, c.rows);
+    // what a workgroup takes at a time, in tiles, and after how many of those a part more pays
+    const int step = c.rows == 1 ? kQ4KeyWaves : c.rows == 8 ? 2 : 1, turns = ceil_div(ntiles, step), items = nkv * c.blocks;
+    const int far = c.rows == 1 ? 64 : 16;
+    c.splits = 256 / std::min(items, 256);
+    if (ntiles / c.splits > far) c.splits = (c.rows == 1 ? 768 : 512) / std::min(items, 512);
+    c.splits = std::max(1, std::min(c.splits, turns <= (c.rows == 1 ? 6 : 4) ? 1 : c.rows == 1 ? turns : (turns + 1) / 2));
     return c;
 }
+
+static size_t q4_attn_units(const Q4AttnCut& c, int nkv) { return (size_t)nkv * c.blocks * c.splits * c.rows; }
 
 size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
 {
     const Q4AttnCut c = q4_attn_cut(M, kv_len, nh, nkv);
     if (c.splits == 1) return 256;
-    const size_t units = (size_t)nkv * c.blocks * c.splits;
-    return align_up(units * c.mt * 16 * d * 4, 256) + align_up(units * c.mt * 32 * 4, 256);
+    const size_t units = q4_attn_units(c, nkv);
+    return align_up(units * 16 * d * 4, 256) + align_up(units * 128, 256);
 }
 
-template <int D, int MT>
+template <int D, int NR>
+static ghd_status q4_rows_of(const Q4Attn& a, const Q4AttnCut& c, hipStream_t st)
+{
+    const size_t lds = (size_t)2 * (NR == 8 ? 2 : 1) * (D / 8) * 1024;
+    const ghd_status s = launch_resident_checked((const void*)k_q4_attention_rows<D, NR>, NR * 64, lds, nullptr);
+    if (s) return s;
+    hipLaunchKernelGGL((k_q4_attention_rows<D, NR>), dim3(a.nkv * c.blocks * c.splits), dim3(NR * 64), lds, st, a, c.splits, c.blocks);
+    return check_launch();
+}
+
+template <int D>
 static ghd_status q4_attention_of(const Q4Attn& a, const Q4AttnCut& c, hipStream_t st)
 {
-    const size_t lds = (size_t)(D / 16) * MT * 64 * 16 + MT * 128;
-    hipLaunchKernelGGL((k_q4_attention<D, MT>), dim3(a.nkv * c.blocks * c.splits), dim3(kQ4Waves * 64), lds, st, a, c.splits,
-                       c.blocks);
-    if (c.splits > 1) {
-        const int items = a.nkv * c.blocks * (D / 16) * MT;
-        hipLaunchKernelGGL((k_q4_join<D, MT>), dim3(ceil_div(items, 4)), dim3(256), 0, st, a, c.splits, c.blocks, items);
+    ghd_status s;
+    if (c.rows == 1) {
+        hipLaunchKernelGGL(k_q4_attention_keys<D>, dim3(a.nkv * c.splits), dim3(kQ4KeyWaves * 64), 0, st, a, c.splits);
+        s = check_launch();
+    } else if (c.rows == 4) {
+        s = q4_rows_of<D, 4>(a, c, st);
+    } else {
+        s = q4_rows_of<D, 8>(a, c, st);
     }
+    if (s || c.splits == 1) return s;
+    hipLaunchKernelGGL(k_q4_join<D>, dim3(a.nkv * c.blocks * c.rows * (D / 16)), dim3(256), 0, st, a, c.splits, c.blocks, c.rows);
     return check_launch();
 }
 
 ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, hipStream_t st)
 {
     const Q4AttnCut c = q4_attn_cut(a.M, a.kv_len, a.nh, a.nkv);
-    const size_t units = (size_t)a.nkv * c.blocks * c.splits;
     a.o_part = (float*)ws;
-    a.ml_part = (float*)((char*)ws + align_up(units * c.mt * 16 * d * 4, 256));
-    if (d == 128) return c.mt == 1 ? q4_attention_of<128, 1>(a, c, st) : q4_attention_of<128, 2>(a, c, st);
-    return c.mt == 1 ? q4_attention_of<64, 1>(a, c, st) : q4_attention_of<64, 2>(a, c, st);
+    a.ml_part = (float*)((char*)ws + align_up(q4_attn_units(c, a.nkv) * 16 * d * 4, 256));
+    return d == 128 ? q4_attention_of<128>(a, c, st) : q4_attention_of<64>(a, c, st);
 }
 
 }  // namespace ghd
