@@ -541,17 +541,25 @@ def ghd_linear_q4_workspace_bytes(M: int, N: int, K: int) -> int:
 def ghd_linear_q4(x: torch.Tensor, Wq: torch.Tensor, N: int, group: int, out_dtype=torch.float32,
                   ws: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x fp16 [M, K] (rows may be apart), Wq from ghd_pack_weight_q4 with the same group."""
+    L = _lib or lib()
     M, K = x.shape
-    if Wq.numel() != lib().ghd_weight_q4_bytes(N, K, group):
+    if Wq.numel() != L.ghd_weight_q4_bytes(N, K, group):
         raise ValueError("Wq does not hold a [%d, %d] matrix in groups of %d" % (N, K, group))
     if y is None:
         y = torch.empty((M, N), dtype=out_dtype, device=x.device)
     if ws is None:
-        ws = workspace(lib().ghd_linear_q4_workspace_bytes(M, N, K), x.device)
-    assert y.is_cuda and y.shape == (M, N) and y.stride(-1) == 1 and y.dtype in (torch.float16, torch.float32)
-    flags = GHD_OUT_F16 if y.dtype == torch.float16 else GHD_OUT_F32
-    _check(lib().ghd_linear_q4(_ptr(y), _ptr(_devs(x, torch.float16)), _ptr(_dev(Wq, torch.uint8)), M, N, K, group,
-                               x.stride(0), y.stride(0), flags, _ptr(ws), ws.numel(), _stream()), "ghd_linear_q4")
+        ws = workspace(L.ghd_linear_q4_workspace_bytes(M, N, K), x.device)
+    ldx, one = x.stride()
+    ldy, also = y.stride()
+    half = y.dtype is torch.float16
+    assert x.is_cuda and x.dtype is torch.float16 and one == 1, (x.device, x.dtype, x.stride())
+    assert y.is_cuda and y.shape == (M, N) and also == 1 and (half or y.dtype is torch.float32), (y.shape, y.dtype)
+    assert Wq.is_cuda and Wq.dtype is torch.uint8 and Wq.is_contiguous()
+    st = L.ghd_linear_q4(y.data_ptr(), x.data_ptr(), Wq.data_ptr(), M, N, K, group, ldx if M > 1 else max(ldx, K),
+                         ldy if M > 1 else max(ldy, N), GHD_OUT_F16 if half else GHD_OUT_F32, ws.data_ptr(), ws.numel(),
+                         _stream())
+    if st:
+        _check(st, "ghd_linear_q4")
     return y
 
 
@@ -566,20 +574,15 @@ class KvQ4:
         self.k = torch.zeros((L, n), dtype=torch.uint8, device=device)
         self.v = torch.zeros((L, n), dtype=torch.uint8, device=device)
         self.kv = (KV * L)(*[KV(self.k[i].data_ptr(), self.v[i].data_ptr()) for i in range(L)])
-
-    def layer(self, i: int):
-        return C.byref(self.kv[i])
+        self.layers = [C.byref(kv) for kv in self.kv]
 
 
-def _heads(t: torch.Tensor, heads: int, d: int) -> torch.Tensor:
-    """A [M, heads, d] tensor whose rows may be apart but whose heads lie side by side."""
-    assert t.is_cuda and t.dtype == torch.float16 and t.shape[1:] == (heads, d), (t.device, t.dtype, t.shape)
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == d), t.stride()
-    return t
-
-
-def _row_step(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+def _row_step(t: torch.Tensor, M: int, heads: int, d: int) -> int:
+    """How far the rows of a [M, heads, d] tensor whose heads lie side by side are apart."""
+    step, head, one = t.stride()
+    assert t.is_cuda and t.dtype is torch.float16 and t.shape == (M, heads, d), (t.device, t.dtype, t.shape)
+    assert one == 1 and (heads == 1 or head == d), t.stride()
+    return step if M > 1 else heads * d
 
 
 def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, kv_len: int,
@@ -589,19 +592,21 @@ def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, 
     turned where rope_base > 0: at kv_len + depth of parent, or at kv_len + i.  q fp16 [M, nh, d] is
     turned likewise and returned."""
     M, nkv, d = k.shape[0], cache.nkv, cache.d
-    _heads(k, nkv, d), _heads(v, nkv, d)
-    assert v.shape[0] == M and (parent is None or parent.numel() == M)
-    nh, ld_q, ld_qo = 0, 0, 0
+    ld_k, ld_v = _row_step(k, M, nkv, d), _row_step(v, M, nkv, d)
+    nh, ld_q, ld_qo, q_ptr, qo_ptr, tree = 0, 0, 0, None, None, None
     if q is not None:
         nh = q.shape[1]
         if q_out is None:
             q_out = torch.empty((M, nh, d), dtype=torch.float16, device=q.device)
-        assert q.shape[0] == M and q_out.shape[0] == M
-        ld_q, ld_qo = _row_step(_heads(q, nh, d)), _row_step(_heads(q_out, nh, d))
-    _check(lib().ghd_kv_append_q4(cache.layer(layer), _ptr(k), _ptr(v), _ptr(q), _ptr(q_out) if q is not None else None,
-                                  None if parent is None else _ptr(_dev(parent, torch.int32)), M, kv_len, nh, nkv, d,
-                                  cache.capacity, _row_step(k), _row_step(v), ld_q, ld_qo, rope_base, _stream()),
-           "ghd_kv_append_q4")
+        ld_q, ld_qo = _row_step(q, M, nh, d), _row_step(q_out, M, nh, d)
+        q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
+    if parent is not None:
+        assert parent.numel() == M
+        tree = _dev(parent, torch.int32).data_ptr()
+    st = (_lib or lib()).ghd_kv_append_q4(cache.layers[layer], k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, tree, M, kv_len, nh,
+                                          nkv, d, cache.capacity, ld_k, ld_v, ld_q, ld_qo, rope_base, _stream())
+    if st:
+        _check(st, "ghd_kv_append_q4")
     return q_out if q is not None else None
 
 
@@ -619,7 +624,7 @@ def _attention_q4(fn, name, q, cache, layer, relation, kv_len, scale, ws, out):
     if ws is None:
         ws = workspace(lib().ghd_attention_q4_workspace_bytes(M, kv_len, nh, cache.nkv, d), q.device)
     assert out.shape == q.shape
-    _check(fn(_ptr(_dev(out, torch.float16)), _ptr(_dev(q, torch.float16)), cache.layer(layer), relation, M, kv_len, nh,
+    _check(fn(_ptr(_dev(out, torch.float16)), _ptr(_dev(q, torch.float16)), cache.layers[layer], relation, M, kv_len, nh,
               cache.nkv, d, cache.capacity, scale, _ptr(ws), ws.numel(), _stream()), name)
     return out
 

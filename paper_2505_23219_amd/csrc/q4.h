@@ -94,8 +94,9 @@ struct Q4Append {
     int64_t ld_k, ld_v, ld_q, ld_qo;
     int M, kv_len, nkv, nq, tiles;   // nq: query heads to be turned (0 without q)
     float rope_base;                 // 0: rows as they are
+    double log2_step;                // of the angles of neighbouring channels (the launch's)
 };
-ghd_status launch_q4_append(const Q4Append& a, int d, hipStream_t st);
+ghd_status launch_q4_append(Q4Append a, int d, hipStream_t st);
 ghd_status launch_q4_commit(void* const* k, void* const* v, int L, int nkv, int d, int cap, int kv_len, int M,
                             const int32_t* res, hipStream_t st);
 ghd_status launch_q4_read(void* const* k, void* const* v, int L, int nkv, int d, int cap, int row0, int rows, half_t* ko,

@@ -12,208 +12,217 @@
 namespace ghd {
 
 typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+typedef word4 word4_at4 __attribute__((aligned(4)));       // rows of the caller's may begin at any word
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x)
 {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
 }
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;   // exchanges inside 16 lanes
-
-// over 16 lanes (each has two of a group's 32 channels)
-template <class Op>
-__device__ __forceinline__ uint32_t over16(uint32_t x, Op op)
-{
-    x = op(x, dpp<kXor1>(x));
-    x = op(x, dpp<kXor2>(x));
-    x = op(x, dpp<kMirror8>(x));
-    return op(x, dpp<kMirror16>(x));
-}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kXor8 = 0x128;   // exchanges inside 4, 4 and 16 lanes (the last turns 16 by 8)
 
 struct Group {
     half_t lo, s;
-    uint32_t c0, c1;       // this lane's two codes
+    uint32_t codes;        // of this lane's 8 channels, as a word of q4.h
 };
 
-// x: this lane's two channels of a group that 16 lanes hold
-__device__ __forceinline__ Group quantise(half2_ x)
+// x: this lane's 8 channels of a group that four lanes side by side hold
+__device__ __forceinline__ Group quantise(half8 x)
 {
 #pragma clang fp contract(off)
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
-    // (min x, min -x) of the two channels, then of the 16 lanes
-    const half2_ m = {x[0] < x[1] ? x[0] : x[1], x[0] < x[1] ? -x[1] : -x[0]};
-    const half2_ r = __builtin_bit_cast(half2_, over16(__builtin_bit_cast(uint32_t, m), [](uint32_t a, uint32_t b) {
-        return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(half2_, a), __builtin_bit_cast(half2_, b)));
-    }));
-    const bool odd = (bits & 0x7c00u) == 0x7c00u || (bits & 0x7c000000u) == 0x7c000000u;
-    const uint32_t bad = over16((uint32_t)odd, [](uint32_t a, uint32_t b) { return a | b; });
+    const word4 bits = __builtin_bit_cast(word4, x);
+    half2_ least = {x[0], x[1]}, most = least;
+    uint32_t odd = 0;      // an infinity or NaN: an exponent of all ones, plus one, carries into the sign
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const half2_ v = {x[2 * p], x[2 * p + 1]};
+        least = __builtin_elementwise_min(least, v);
+        most = __builtin_elementwise_max(most, v);
+        odd |= (bits[p] & 0x7c007c00u) + 0x04000400u;
+    }
+    odd &= 0x80008000u;
+    // (min x, min -x), of the lane, then of the four
+    half2_ m = {__builtin_elementwise_min(least[0], least[1]), -__builtin_elementwise_max(most[0], most[1])};
+    m = __builtin_elementwise_min(m, __builtin_bit_cast(half2_, dpp<kXor1>(__builtin_bit_cast(uint32_t, m))));
+    m = __builtin_elementwise_min(m, __builtin_bit_cast(half2_, dpp<kXor2>(__builtin_bit_cast(uint32_t, m))));
+    odd |= dpp<kXor1>(odd);
+    odd |= dpp<kXor2>(odd);
     Group g;
-    g.lo = r[0];
-    const float lo = (float)r[0];
-    g.s = (half_t)((-(float)r[1] - lo) / 15.f);
+    g.lo = m[0];
+    const float lo = (float)m[0];
+    g.s = (half_t)((-(float)m[1] - lo) / 15.f);
     // rounded up, the scale of the widest ranges would make the largest code stand for more than fp16 holds
     if (lo + 15.f * (float)g.s >= 65520.f)
         g.s = __builtin_bit_cast(half_t, (uint16_t)(__builtin_bit_cast(uint16_t, g.s) - 1));
     const float s = (float)g.s;
-    auto code = [&](half_t v) { return s > 0.f ? (uint32_t)fminf(fmaxf(rintf(((float)v - lo) / s), 0.f), 15.f) : 0u; };
-    g.c0 = code(x[0]);
-    g.c1 = code(x[1]);
-    if (bad) {             // a group with an infinity or NaN in it reads as NaN
+    // (x - lo) / s by a reciprocal, which is off by less than 1e-5; where a quotient is that near to the middle of two codes for any
+    // lane, by divisions (a division is ten instructions, and there are 16 a lane and row)
+    float code[8];
+    const float r = __builtin_amdgcn_rcpf(s);
+    bool near = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float t = ((float)x[j] - lo) * r;
+        code[j] = rintf(t);
+        near = near || fabsf(t - code[j]) > 0.49998f;
+    }
+    if (__ballot(near && s > 0.f))
+#pragma unroll
+        for (int j = 0; j < 8; ++j) code[j] = rintf(((float)x[j] - lo) / s);
+    g.codes = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g.codes |= (uint32_t)fminf(code[j], 15.f) << (4 * (j / 2) + 16 * (j % 2));
+    if (!(s > 0.f)) g.codes = 0;
+    if (odd) {             // a group with an infinity or NaN in it reads as NaN
         g.s = __builtin_bit_cast(half_t, (uint16_t)0x7e00);
-        g.c0 = g.c1 = 0;
+        g.codes = 0;
     }
     return g;
 }
 
-// ---- append ------------------------------------------------------------------------------
-// Bound: for a tree's rows latency (one launch, rows read, reduced over lanes and written); for a prompt the bytes.
-// Rows are read 4 bytes a lane, two channels and, of keys and queries, the two they turn with half a row
-// away; 16 lanes hold a group.  A wavefront has one octet and a run of heads, whose cosines it works out once: heads
-// 0 .. nkv - 1 are keys and values, nkv .. nkv + nq - 1 queries.
-template <int D>
-__global__ __launch_bounds__(256) void k_q4_append(const Q4Append a, int chunks, int per_chunk, int units)
+// A word of every lane (key k = lane / 8) has 8 channels; afterwards lane 8 c + i has channel c's 8 keys.  Key bit 0 changes
+// places with the half a code is in, bit 1 with its lowest and bit 2 with its next place among four.
+__device__ __forceinline__ uint32_t keys_of_channel(uint32_t w, int lane)
 {
-    const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= units) return;
-    const int octet = a.kv_len / 8 + unit / chunks, head0 = unit % chunks * per_chunk;
-    const int head1 = min(head0 + per_chunk, a.nkv + a.nq);
-    const int row0 = octet * 8 - a.kv_len;                    // input row of the octet's first key (may be negative)
-    constexpr int kLanes = D / 4, kSets = 64 / kLanes, kRows = 8 / kSets;   // lanes a row of turned pairs; rows a lane
-    const int i = lane % kLanes, set = lane / kLanes;         // channels 2 i, 2 i + 1 and D / 2 further
-    float cs[kRows][2], sn[kRows][2];
-    const bool turn = a.rope_base > 0.f;
-    if (turn) {
-        int up0 = 0, up1 = 0;
-        if (a.parent) {
-            up0 = a.parent[min(lane, a.M - 1)];
-            up1 = a.parent[min(lane + 64, a.M - 1)];
-        }
-        const TreeNodes<2> t = tree_nodes<2, false>(up0, up1, a.parent ? a.M : 0, lane);
-#pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            const int row = row0 + set * kRows + j, in = min(max(row, 0), a.M - 1);
-            const int depth = t.depth(a.parent ? in : 0);
-            const int at = a.kv_len + (a.parent ? depth : in);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const double freq = exp2(-2.0 / D * log2((double)a.rope_base) * (2 * i + e));
-                double s, c;
-                sincos((double)at * freq, &s, &c);
-                cs[j][e] = (float)c;
-                sn[j][e] = (float)s;
-            }
-        }
-    }
-    auto rotate = [&](half2_& lo, half2_& hi, int j) {
-#pragma clang fp contract(off)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float x = (float)lo[e], y = (float)hi[e];
-            lo[e] = (half_t)(x * cs[j][e] - y * sn[j][e]);
-            hi[e] = (half_t)(y * cs[j][e] + x * sn[j][e]);
+    uint32_t other = dpp<kXor8>(w);
+    w = lane & 8 ? other >> 16 | (w & 0xffff0000u) : (w & 0xffffu) | other << 16;
+    other = (uint32_t)__shfl_xor((int)w, 16);
+    w = lane & 16 ? (other >> 4 & 0x0f0f0f0fu) | (w & 0xf0f0f0f0u) : (w & 0x0f0f0f0fu) | (other & 0x0f0f0f0fu) << 4;
+    other = (uint32_t)__shfl_xor((int)w, 32);
+    return lane & 32 ? (other >> 8 & 0x00ff00ffu) | (w & 0xff00ff00u) : (w & 0x00ff00ffu) | (other & 0x00ff00ffu) << 8;
+}
+
+// ---- append ------------------------------------------------------------------------------
+// A wavefront takes the octet of a head (of two heads of 64 channels) at a time: lane 8 k + i has of key k channels 8 i .. + 7 and
+// those half a row further, which turn with them: two 16-byte requests, and a word of K codes, each.  The workgroup's
+// four wavefronts have one octet, whose cosines and sines, worked out in 64 bits, they share through LDS (worked out by every
+// wavefront for itself the smallest call took 9 us, 4096 rows of 32 + 8 heads 47).
+// Bound: for a tree's rows latency - parents, cosines, rows, one behind the other; for a prompt the bytes.
+template <int D>
+__global__ __launch_bounds__(256) void k_q4_append(const Q4Append a, int chunks, int per_chunk)
+{
+    constexpr int kHeads = 128 / D, kHalf = D / 2;
+    __shared__ float2 s_turn[8][kHalf];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, key = lane >> 3;
+    const int i = D == 128 ? lane & 7 : lane & 3, second = D == 128 ? 0 : lane >> 2 & 1;     // (the second of two heads)
+    const int octet = a.kv_len / 8 + blockIdx.x / chunks, row0 = octet * 8 - a.kv_len;       // row0: input row of the first key
+    const int kv_items = (a.nkv + kHeads - 1) / kHeads, items = kv_items + (a.nq + kHeads - 1) / kHeads;
+    const int first = blockIdx.x % chunks * per_chunk, end = min(first + per_chunk, items);
+    const int row = row0 + key, row_in = min(max(row, 0), a.M - 1);
+    const bool in = row >= 0 && row < a.M;
+    struct Rows {
+        half8 x[2], v[2];
+    };
+    auto load = [&](Rows& r, int item) {
+        item = min(item, end - 1);
+        const bool is_q = item >= kv_items;
+        const int head = min((is_q ? item - kv_items : item) * kHeads + second, (is_q ? a.nq : a.nkv) - 1);
+        const half_t* x = (is_q ? a.q + (int64_t)row_in * a.ld_q : a.kx + (int64_t)row_in * a.ld_k) + head * D + 8 * i;
+        r.x[0] = __builtin_bit_cast(half8, *(const word4_at4*)x);
+        r.x[1] = __builtin_bit_cast(half8, *(const word4_at4*)(x + kHalf));
+        if (!is_q) {
+            const half_t* v = a.vx + (int64_t)row_in * a.ld_v + head * D + 8 * i;
+            r.v[0] = __builtin_bit_cast(half8, *(const word4_at4*)v);
+            r.v[1] = __builtin_bit_cast(half8, *(const word4_at4*)(v + kHalf));
         }
     };
-    for (int head = head0; head < head1; ++head) {
-        if (head >= a.nkv) {                                  // a query head
-            const int h = head - a.nkv;
-#pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                const int row = row0 + set * kRows + j;
-                if (row < 0 || row >= a.M) continue;
-                const half_t* src = a.q + (size_t)row * a.ld_q + h * D + 2 * i;
-                half_t* dst = a.q_out + (size_t)row * a.ld_qo + h * D + 2 * i;
-                half2_ lo = *(const half2_*)src, hi = *(const half2_*)(src + D / 2);
-                rotate(lo, hi, j);
-                *(half2_*)dst = lo;
-                *(half2_*)(dst + D / 2) = hi;
-            }
-            continue;
+    Rows r;
+    load(r, first + wave);
+    const bool turn = a.rope_base > 0.f;
+    float2 cs[8];
+    if (turn) {
+        int depth = 0;
+        if (a.parent) {
+            const TreeNodes<2> t =
+                tree_nodes<2, false>(a.parent[min(lane, a.M - 1)], a.parent[min(lane + 64, a.M - 1)], a.M, lane);
+            depth = t.depth(min(max(row0 + (lane & 7), 0), a.M - 1));          // lane k: of the octet's key k
         }
-        const size_t tile = q4_tile_at(head, octet / 4, a.tiles, D);
+        // entry (key, j) by thread; a wavefront's entries are of one key, or of two
+#pragma unroll
+        for (int e = tid; e < 8 * kHalf; e += 256) {
+            const int k = e / kHalf, j = e % kHalf, from = row0 + k;
+            const int at = a.kv_len + (a.parent ? __shfl(depth, k) : from);
+            if (from < 0 || from >= a.M) continue;
+            double s, c;
+            sincos((double)at * exp2(a.log2_step * j), &s, &c);
+            s_turn[k][j] = make_float2((float)c, (float)s);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) cs[j] = s_turn[key][8 * i + j];
+    }
+    auto rotate = [&](Rows& w) {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = (float)w.x[0][j], y = (float)w.x[1][j];
+            w.x[0][j] = (half_t)(x * cs[j].x - y * cs[j].y);
+            w.x[1][j] = (half_t)(y * cs[j].x + x * cs[j].y);
+        }
+    };
+    auto store = [&](Rows& w, int item) {
+        const bool is_q = item >= kv_items;
+        const int head = (is_q ? item - kv_items : item) * kHeads + second;
+        if (turn) rotate(w);
+        if (is_q) {
+            if (!in || head >= a.nq) return;
+            half_t* to = a.q_out + (int64_t)row * a.ld_qo + head * D + 8 * i;
+            *(word4_at4*)to = __builtin_bit_cast(word4, w.x[0]);
+            *(word4_at4*)(to + kHalf) = __builtin_bit_cast(word4, w.x[1]);
+            return;
+        }
+        const bool there = head < a.nkv;
+        const size_t tile = q4_tile_at(min(head, a.nkv - 1), octet / 4, a.tiles, D);
         const int in_tile = octet % 4 * 8;
-        {   // keys
-            char* kt = a.k + tile;
-            half2_ x[kRows][2];
+        char *kt = a.k + tile, *vt = a.v + tile;
+        half_t* meta = (half_t*)(vt + q4_codes_bytes(D));
+        uint32_t held = 0;                                       // codes of rows that are not this call's
 #pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                const int row = min(max(row0 + set * kRows + j, 0), a.M - 1);
-                const half_t* src = a.kx + (size_t)row * a.ld_k + head * D + 2 * i;
-                x[j][0] = *(const half2_*)src;
-                x[j][1] = *(const half2_*)(src + D / 2);
+        for (int k = 0; k < 8; ++k)
+            if (row0 + k < 0 || row0 + k >= a.M) held |= 15u << (4 * (k / 2) + 16 * (k % 2));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = u * kHalf + 8 * i;
+            const Group gk = quantise(w.x[u]);
+            if (in && there) {
+                *(uint32_t*)(kt + (in_tile + key) * (D / 2) + c / 2) = gk.codes;
+                if ((i & 3) == 0) *(half2_*)(kt + q4_codes_bytes(D) + ((in_tile + key) * (D / 32) + c / 32) * 4) = (half2_){gk.lo, gk.s};
             }
-#pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                const int row = row0 + set * kRows + j, key = in_tile + set * kRows + j;
-                const bool in = row >= 0 && row < a.M;
-                if (turn) rotate(x[j][0], x[j][1], j);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const Group g = quantise(x[j][u]);
-                    uint32_t w = (g.c0 | g.c1 << 16) << 4 * (i & 3);      // a word: four lanes
-                    w |= dpp<kXor1>(w);
-                    w |= dpp<kXor2>(w);
-                    const int c = 2 * i + u * (D / 2);
-                    if (in && (i & 3) == 0) *(uint32_t*)(kt + key * (D / 2) + c / 2) = w;
-                    if (in && (i & 15) == 0)
-                        *(half2_*)(kt + q4_codes_bytes(D) + (key * (D / 32) + c / 32) * 4) = (half2_){g.lo, g.s};
-                }
+            const Group gv = quantise(w.v[u]);
+            if (in && there && (i & 3) == 0) {
+                meta[c / 32 * 64 + in_tile + key] = gv.lo;
+                meta[c / 32 * 64 + 32 + in_tile + key] = gv.s;
+            }
+            uint32_t word = keys_of_channel(gv.codes, lane);     // now of channel u kHalf + 8 i + key
+            uint32_t* to = (uint32_t*)vt + q4_v_word(c + key, octet % 4);
+            if (there) {
+                if (held) word = (word & ~held) | (*to & held);
+                *to = word;
             }
         }
-        {   // values: 64 lanes hold a row of 128 channels, or two halves of the octet of 64
-            char* vt = a.v + tile;
-            constexpr int kHalves = 128 / D, kKeys = 8 / kHalves;
-            const int c = 2 * (lane % (D / 2)), k0 = lane / (D / 2) * kKeys;
-            half2_ x[kKeys];
-#pragma unroll
-            for (int j = 0; j < kKeys; ++j) {
-                const int row = min(max(row0 + k0 + j, 0), a.M - 1);
-                x[j] = *(const half2_*)(a.vx + (size_t)row * a.ld_v + head * D + c);
-            }
-            uint32_t w0 = 0, w1 = 0, held = 0;                // words of channels c, c + 1; bits of rows that are held already
-            half_t* meta = (half_t*)(vt + q4_codes_bytes(D)) + c / 32 * 64;
-#pragma unroll
-            for (int j = 0; j < kKeys; ++j) {
-                const int k = k0 + j, row = row0 + k, at = 4 * (k / 2) + 16 * (k % 2);
-                const Group g = quantise(x[j]);
-                if (row >= 0 && row < a.M) {
-                    w0 |= g.c0 << at;
-                    w1 |= g.c1 << at;
-                    if ((lane & 15) == 0) {
-                        meta[in_tile + k] = g.lo;
-                        meta[32 + in_tile + k] = g.s;
-                    }
-                } else {
-                    held |= 15u << at;
-                }
-            }
-            if constexpr (kHalves == 2) {
-                w0 |= (uint32_t)__shfl_xor((int)w0, 32);
-                w1 |= (uint32_t)__shfl_xor((int)w1, 32);
-                held |= (uint32_t)__shfl_xor((int)held, 32);
-            }
-            if (k0 == 0) {
-                uint32_t* p0 = (uint32_t*)vt + q4_v_word(c, octet % 4);
-                uint32_t* p1 = (uint32_t*)vt + q4_v_word(c + 1, octet % 4);
-                if (held) {
-                    w0 |= *p0 & held;
-                    w1 |= *p1 & held;
-                }
-                *p0 = w0;
-                *p1 = w1;
-            }
-        }
+    };
+    // (two in turn: a copy of the one on its way would have to wait for it)
+    Rows next;
+    for (int item = first + wave; item < end; item += 8) {
+        load(next, item + 4);
+        store(r, item);
+        if (item + 4 >= end) break;
+        load(r, item + 8);
+        store(next, item + 4);
     }
 }
 
-ghd_status launch_q4_append(const Q4Append& a, int d, hipStream_t st)
+ghd_status launch_q4_append(Q4Append a, int d, hipStream_t st)
 {
-    const int octets = (a.kv_len + a.M - 1) / 8 - a.kv_len / 8 + 1, heads = a.nkv + a.nq;
-    // one head a wavefront where that is at most 4096 wavefronts; above that, runs of heads, which share cosines
-    const int per = (int)std::min<int64_t>(heads, std::max<int64_t>(1, (int64_t)octets * heads / 4096));
-    const int chunks = ceil_div(heads, per), units = octets * chunks;
-    const dim3 grid(ceil_div(units, 4));
-    if (d == 128) hipLaunchKernelGGL(k_q4_append<128>, grid, dim3(256), 0, st, a, chunks, per, units);
-    else hipLaunchKernelGGL(k_q4_append<64>, grid, dim3(256), 0, st, a, chunks, per, units);
+    a.log2_step = -2.0 / d * log2((double)(a.rope_base > 0.f ? a.rope_base : 1.f));
+    const int heads = 128 / d, octets = (a.kv_len + a.M - 1) / 8 - a.kv_len / 8 + 1;
+    const int items = ceil_div(a.nkv, heads) + ceil_div(a.nq, heads);
+    // an item a wavefront where that is at most 1024 workgroups; above that runs of them, which share cosines
+    const int per = (int)std::min<int64_t>(align_up(items, 4), 4 * std::max<int64_t>(1, (int64_t)octets * items / 4096));
+    const int chunks = ceil_div(items, per);
+    const dim3 grid(octets * chunks);
+    if (d == 128) hipLaunchKernelGGL(k_q4_append<128>, grid, dim3(256), 0, st, a, chunks, per);
+    else hipLaunchKernelGGL(k_q4_append<64>, grid, dim3(256), 0, st, a, chunks, per);
     return check_launch();
 }
 

@@ -1,4 +1,5 @@
 """The 4-bit operators on the GPU against plain forms in 64 bits (tests/q4_plain.py)."""
+import ctypes
 import math
 import zlib
 
@@ -350,6 +351,7 @@ def test_heads_more_than_4_gib_apart():
     cache.L, cache.nkv, cache.d, cache.capacity = 1, nkv, d, cap
     cache.k, cache.v = (torch.empty((1, n), dtype=torch.uint8, device="cuda") for _ in range(2))
     cache.kv = (B.KV * 1)(B.KV(cache.k.data_ptr(), cache.v.data_ptr()))
+    cache.layers = [ctypes.byref(cache.kv[0])]
     k, v = _rows(rng, kv + M, nkv, d), _rows(rng, kv + M, nkv, d)
     q, parent = rng.standard_normal((M, nkv, d)).astype(np.float16), _random_parent(rng, M, "random")
     B.ghd_kv_append_q4(cache, 0, _dev(k), _dev(v), 0)
