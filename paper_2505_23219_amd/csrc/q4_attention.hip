@@ -359,19 +359,25 @@ __global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const
 }
 
 // ---- more rows ---------------------------------------------------------------------------
-// NR wavefronts of 16 rows.  A stage is 32 keys (64 for eight wavefronts), two buffers of it in LDS as operands; a stage's
-// pieces - 16 keys of K, or 64 channels of 32 keys of V - are converted by a wavefront each (two wavefronts: two each).  Codes
-// of the stage after the next are requested before a stage's products, converted after the next one's.
-template <int D, int NR>
-__global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a, int splits, int blocks)
+// KG groups of NR wavefronts of 16 rows; the groups take stages of the keys in turn and meet at the end.  A stage is 32 keys (64 for
+// eight wavefronts), a group has two buffers of it in LDS, as operands; a stage's pieces - 16 keys of K, or 64 channels of 32
+// keys of V - are converted by a wavefront each.  Codes of the stage after the next are requested before a stage's products,
+// converted after the next one's.  One barrier a stage.
+// Bound: neither pipe: in 128 rows of 40 heads over 8320 keys (43 us) products take 22% of the time, other vector instructions 38%
+// and LDS 26%, one much behind the other.  Four wavefronts on a SIMD, so 128 registers (three: 52 us).  Taken back: 32 rows a
+// wavefront, which reads LDS half as often (45 to 62 us), four groups for 64 rows (18.5 us a call over 2112 keys of 32 heads,
+// two 17.5, one 18.4), two for 128.
+template <int D, int NR, int KG>
+__global__ __launch_bounds__(NR * KG * 64, 4) void k_q4_attention_rows(const Q4Attn a, int splits, int blocks)
 {
     constexpr int CT = D / 16, KS = D / 32, TS = NR == 8 ? 2 : 1;             // tiles a stage
     constexpr int kKPieces = 2 * TS, kVPieces = D / 64 * TS, kPieces = kKPieces + kVPieces;
     constexpr int kTileFrags = 2 * KS + CT, kBuf = TS * kTileFrags * 1024;
     __shared__ uint64_t s_mask[2 * GHD_MAX_M];
-    __shared__ uint8_t s_bad[2][TS][KS][4];
+    __shared__ uint8_t s_bad[KG][2][TS][KS][4];
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NR;
     const Q4Item it(a, splits, blocks);
     const int ntiles = (it.total + kQ4Tile - 1) / kQ4Tile, nstages = (ntiles + TS - 1) / TS;
     const int s0 = (int)((int64_t)nstages * it.split / splits), s1 = (int)((int64_t)nstages * (it.split + 1) / splits);
@@ -395,8 +401,9 @@ __global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a
         raw[2] = *(const word4*)(at + off_scale);
     };
     const Q4Bits bits;
+    auto reaches = [&](int stage) { return (stage + 1) * TS * kQ4Tile > a.kv_len; };      // into the drafted rows
     auto convert = [&](int stage, int buf) {
-        char* to = lds + buf * kBuf + of_tile * kTileFrags * 1024 + lane * 16;
+        char* to = lds + (kg * 2 + buf) * kBuf + of_tile * kTileFrags * 1024 + lane * 16;
         if (of_k) {
             uint32_t m = raw[1][0];
 #pragma unroll
@@ -410,9 +417,9 @@ __global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a
             }
         } else if (vp < kVPieces) {
             half8 lo = __builtin_bit_cast(half8, raw[1]), sc = __builtin_bit_cast(half8, raw[2]);
-            if ((stage + 1) * TS * kQ4Tile > a.kv_len) {
+            if (reaches(stage)) {
                 const uint32_t bad = q4_clean(lo, sc, (stage * TS + of_tile) * kQ4Tile + 8 * g, it.total);
-                if (col < 2) s_bad[buf][of_tile][2 * part + col][g] = (uint8_t)bad;
+                if (col < 2) s_bad[kg][buf][of_tile][2 * part + col][g] = (uint8_t)bad;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -425,24 +432,24 @@ __global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a
             }
         }
     };
-    load(s0);
+    load(s0 + kg);
     const int row0 = it.block * NR * 16 + wave * 16, row = row0 + col;
     half8 q[KS];
     q4_queries<D>(a, it, row, g, q);
     if (s1 * TS * kQ4Tile > a.kv_len) q4_masks(a, s_mask);
-    convert(s0, 0);
-    load(s0 + 1);
+    convert(s0 + kg, 0);
+    load(s0 + kg + KG);
     __syncthreads();
     const float c = fabsf(a.scale) * 1.4426950408889634f;
     const uint64_t* mask = s_mask + 2 * (row < it.R ? row / it.rep : 0);
     Q4State<D> st;
     auto work = [&](auto MASKED, int stage) {
         constexpr bool masked = decltype(MASKED)::value;
-        const int buf = (stage - s0) & 1;
-        if (row0 < it.R) {
+        const int buf = (stage - s0) / KG & 1;
+        if (row0 < it.R && stage < s1) {
 #pragma unroll
             for (int tile = 0; tile < TS; ++tile) {
-                const char* base = lds + buf * kBuf + tile * kTileFrags * 1024 + lane * 16;
+                const char* base = lds + (kg * 2 + buf) * kBuf + tile * kTileFrags * 1024 + lane * 16;
                 floatx4 s[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -457,23 +464,48 @@ __global__ __launch_bounds__(NR * 64, 4) void k_q4_attention_rows(const Q4Attn a
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
                     st.o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const half8*)(base + (2 * KS + ct) * 1024), p, st.o[ct], 0, 0, 0);
-                if (masked)
+                if (masked && reaches(stage))
 #pragma unroll
                     for (int i = 0; i < KS; ++i) {
-                        const uint32_t bad = s_bad[buf][tile][i][g];
+                        const uint32_t bad = s_bad[kg][buf][tile][i][g];
                         if (__ballot(bad != 0)) st.poison(i, bad, see);
                     }
             }
         }
-        if (stage + 1 < s1) {
-            convert(stage + 1, buf ^ 1);
-            load(stage + 2);
+        if (stage + KG < s1) {
+            convert(stage + KG, buf ^ 1);
+            load(stage + 2 * KG);
         }
         __syncthreads();
     };
-    int stage = s0;
-    for (; stage < min(s1, a.kv_len / (TS * kQ4Tile)); ++stage) work(std::false_type(), stage);     // all rows see all keys
-    for (; stage < s1; ++stage) work(std::true_type(), stage);
+    // (first of a turn of the groups; up to s_plain all rows see all keys of all the groups' stages)
+    const int s_plain = min(s1, a.kv_len / (TS * kQ4Tile)) - KG + 1;
+    int first = s0;
+    for (; first < s_plain; first += KG) work(std::false_type(), first + kg);
+    for (; first < s1; first += KG) work(std::true_type(), first + kg);
+    if constexpr (KG > 1) {
+        // the groups' states meet in LDS (behind the loop's last barrier nothing there is read any more)
+        constexpr int kShare = CT * 1024 + 256;
+        char* mine = lds + ((kg - 1) * NR + wave) * kShare;
+        if (kg > 0) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) ((floatx4*)mine)[ct * 64 + lane] = st.o[ct];
+            if (g == 0) ((floatx2*)(mine + CT * 1024))[col] = (floatx2){st.m, st.l[0]};
+        }
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int k = 1; k < KG; ++k) {
+            const char* other = lds + ((k - 1) * NR + wave) * kShare;
+            const floatx2 ml = ((const floatx2*)(other + CT * 1024))[col];
+            const float m = fmaxf(st.m, ml[0]), off = m == -INFINITY ? 0.f : m;
+            const float f0 = __builtin_amdgcn_exp2f(st.m - off), f1 = __builtin_amdgcn_exp2f(ml[0] - off);
+            st.m = m;
+            st.l[0] = st.l[0] * f0 + ml[1] * f1;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) st.o[ct] = st.o[ct] * f0 + ((const floatx4*)other)[ct * 64 + lane] * f1;
+        }
+    }
     if (splits > 1) {
         const size_t unit = (size_t)blockIdx.x * NR + wave;
         if (g == 0) ((floatx2*)a.ml_part)[unit * 16 + col] = (floatx2){st.m, st.l[0]};
@@ -549,7 +581,7 @@ struct Q4AttnCut {
     int rows, blocks, splits;    // wavefronts of 16 rows in a workgroup, blocks of rows, parts of the keys
 };
 // Parts of the keys cost a launch that joins them (3 us) and what they write: as many as make 256 workgroups, one a compute unit
-// (64 rows of 32 heads over 2112 keys: 4, 8, 16 parts 23.0, 18.3, 20.4 us), and where each then has long to go twice as many or,
+// (64 rows of 32 heads over 2112 keys: 2, 4, 8 parts 24.8, 19.7, 17.5 us), and where each then has long to go twice as many or,
 // of the wavefronts that wait for the cache most, three times (128 rows of 40 heads over 8320 keys: 6 parts 48.4, 12 45.5;
 // 1 token of 40 heads over 32000: 6 48.9, 12 44.7, 19 43.7).  No parts where a workgroup is through sooner than a second launch
 // (8 tokens of 8 heads over 308 keys: 1 part 7.4, 2 9.4).
@@ -578,13 +610,13 @@ size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
     return align_up(units * 16 * d * 4, 256) + align_up(units * 128, 256);
 }
 
-template <int D, int NR>
+template <int D, int NR, int KG>
 static ghd_status q4_rows_of(const Q4Attn& a, const Q4AttnCut& c, hipStream_t st)
 {
-    const size_t lds = (size_t)2 * (NR == 8 ? 2 : 1) * (D / 8) * 1024;
-    const ghd_status s = launch_resident_checked((const void*)k_q4_attention_rows<D, NR>, NR * 64, lds, nullptr);
+    const size_t lds = (size_t)KG * 2 * (NR == 8 ? 2 : 1) * (D / 8) * 1024;
+    const ghd_status s = launch_resident_checked((const void*)k_q4_attention_rows<D, NR, KG>, NR * KG * 64, lds, nullptr);
     if (s) return s;
-    hipLaunchKernelGGL((k_q4_attention_rows<D, NR>), dim3(a.nkv * c.blocks * c.splits), dim3(NR * 64), lds, st, a, c.splits, c.blocks);
+    hipLaunchKernelGGL((k_q4_attention_rows<D, NR, KG>), dim3(a.nkv * c.blocks * c.splits), dim3(NR * KG * 64), lds, st, a, c.splits, c.blocks);
     return check_launch();
 }
 
@@ -596,9 +628,9 @@ static ghd_status q4_attention_of(const Q4Attn& a, const Q4AttnCut& c, hipStream
         hipLaunchKernelGGL(k_q4_attention_keys<D>, dim3(a.nkv * c.splits), dim3(kQ4KeyWaves * 64), 0, st, a, c.splits);
         s = check_launch();
     } else if (c.rows == 4) {
-        s = q4_rows_of<D, 4>(a, c, st);
+        s = q4_rows_of<D, 4, 2>(a, c, st);
     } else {
-        s = q4_rows_of<D, 8>(a, c, st);
+        s = q4_rows_of<D, 8, 1>(a, c, st);
     }
     if (s || c.splits == 1) return s;
     hipLaunchKernelGGL(k_q4_join<D>, dim3(a.nkv * c.blocks * c.rows * (D / 16)), dim3(256), 0, st, a, c.splits, c.blocks, c.rows);
