@@ -87,7 +87,8 @@ ghd_status ghd_linear_q4(void* y, const void* x, const void* Wq, int M, int N, i
 {
     if (!y || !x || !Wq) return GHD_ERR_NULL;
     if (M < 1 || M > GHD_MAX_M || !weight_shape_ok(N, K, group) || flags > GHD_OUT_F16) return GHD_ERR_SHAPE;
-    if (ldx < K || ldy < N || ldx > (1 << 23) || (M - 1) * ldx + K >= (1 << 30)) return GHD_ERR_SHAPE;   // 32-bit offsets in x
+    // x is read at 32-bit byte offsets: 128 rows so far apart end below 2^31
+    if (ldx < K || ldy < N || ldx > (1 << 23)) return GHD_ERR_SHAPE;
     if (!aligned_to(x, 16) || !aligned_to(Wq, 16) || !aligned_to(y, 16) || ldx % 8 != 0) return GHD_ERR_ALIGN;
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!aligned_to(ws, 16)) return GHD_ERR_ALIGN;

@@ -74,6 +74,40 @@ def test_linear(M, N, K, group, zeros):
         assert (got[M] == 7).all() and (got[:, N:] == 7).all()       # nothing outside y is written
 
 
+# Sizes at which every variant of the kernels is taken, by row tiles, tiles of W, scale groups, with k whole and in parts;
+# neither N nor K fills its last tile.
+VARIANTS = [(1, 47, 21688, 32), (2, 19, 28008, 64), (1, 5503, 24, 32), (1, 223, 60808, 32), (3, 7531, 16, 64),
+            (1, 445, 28496, 64), (3, 6378, 16, 128), (1, 476, 31144, 128), (2, 14522, 16, 32), (1, 1294, 14368, 32),
+            (1, 8419, 56, 64), (3, 1411, 15544, 64), (9, 11101, 16, 128), (2, 1398, 14184, 128), (4, 2347, 30472, 32),
+            (4, 2347, 30472, 64), (13, 17765, 16, 128), (1, 1082, 63184, 128), (28, 20, 5368, 32), (19, 19, 9800, 64),
+            (18, 18, 16, 128), (18, 18, 4976, 128), (21, 5793, 16, 32), (19, 1034, 6832, 32), (20, 6680, 16, 64),
+            (20, 687, 8184, 64), (18, 5185, 16, 128), (19, 1074, 6752, 128), (23, 11038, 16, 32), (18, 378, 52944, 32),
+            (17, 8742, 16, 64), (17, 1070, 15048, 64), (25, 12926, 16, 128), (18, 580, 26616, 128), (75, 27, 3472, 32),
+            (91, 31, 16, 64), (73, 25, 3696, 64), (69, 23, 3824, 128), (38, 4781, 16, 32), (68, 2082, 24, 64),
+            (76, 595, 4456, 64), (65, 2233, 24, 128), (85, 134, 17520, 128), (42, 10189, 16, 32), (65, 143, 49520, 32),
+            (69, 6884, 16, 64), (65, 145, 53416, 64), (68, 5359, 16, 128), (66, 575, 14992, 128), (53, 21, 24, 32),
+            (63, 29, 5208, 32), (100, 20, 4896, 128), (99, 2491, 16, 32), (112, 69, 34480, 32), (97, 2500, 16, 64),
+            (122, 274, 8360, 64), (117, 2537, 16, 128), (51, 270, 17104, 128), (18, 19388, 24, 32), (17, 2796, 28520, 32),
+            (32, 31161, 16, 64), (27, 2360, 22152, 64), (21, 49815, 16, 128), (29, 1083, 41968, 128), (68, 15353, 32, 32),
+            (90, 1361, 12984, 32), (37, 19417, 24, 64), (74, 546, 24856, 64), (83, 1190, 16360, 128), (59, 12742, 16, 32),
+            (113, 523, 9416, 32), (114, 569, 9816, 64), (50, 11109, 16, 128), (56, 571, 17496, 128), (110, 536, 37744, 32),
+            (114, 12349, 32, 64), (54, 557, 44448, 64), (112, 13023, 24, 128), (54, 679, 60992, 128), (60, 22021, 1160, 64),
+            (128, 22021, 1160, 32), (40, 22021, 1160, 128), (30, 22021, 1160, 64), (64, 5011, 1160, 32)]
+
+
+@pytest.mark.parametrize("M,N,K,group", VARIANTS)
+def test_linear_variants(M, N, K, group):
+    """Over a workspace that holds anything (0xFF: NaN)."""
+    print("q4 linear variant", M, N, K, group, flush=True)
+    rng = _rng("variant", M, N, K, group)
+    codes, scales, z = _weights(rng, N, K, group, True)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    ws = B.workspace(B.ghd_linear_q4_workspace_bytes(M, N, K)).fill_(0xFF)
+    got = B.ghd_linear_q4(_dev(x), B.ghd_pack_weight_q4(_dev(codes), _dev(scales), _dev(z), group), N, group, ws=ws)
+    want, tol = P.linear(x, P.unpack_weight(codes, scales, z, K, group), False)
+    _close(got.cpu().numpy(), want, tol)
+
+
 def test_linear_same_bits_every_time_and_for_any_rows_beside():
     """Sums are made in a fixed order: runs agree to the bit."""
     rng = _rng("bits")
@@ -177,6 +211,23 @@ def test_queries_turned_in_place_in_a_fused_row():
     got = B.ghd_kv_append_q4(b, 0, k, v, 5, q=q, rope_base=BASE, q_out=q)
     assert got.data_ptr() == q.data_ptr() and torch.equal(got, want)
     assert torch.equal(a.k, b.k) and torch.equal(a.v, b.v)
+
+
+@pytest.mark.parametrize("pad,first", [(2, 2), (8, 0), (6, 4), (8, 8)])
+def test_rows_at_any_even_offset(pad, first):
+    """Rows that begin at 4, 8 and 16 bytes hold what aligned ones do."""
+    rng = _rng("offset", pad, first)
+    M, nkv, d, kv_len = 13, 2, 64, 21
+    a, b = B.KvQ4(1, nkv, d, 64), B.KvQ4(1, nkv, d, 64)
+    rows = [_rows(rng, M, nkv, d) for _ in range(3)]
+    views = []
+    for x in rows:
+        room = torch.zeros((M, nkv * d + pad + first), dtype=torch.float16, device="cuda")
+        views.append(room[:, first:first + nkv * d].view(M, nkv, d))
+        views[-1].copy_(_dev(x))
+    want = B.ghd_kv_append_q4(a, 0, _dev(rows[0]), _dev(rows[1]), kv_len, q=_dev(rows[2]), rope_base=BASE)
+    got = B.ghd_kv_append_q4(b, 0, views[0], views[1], kv_len, q=views[2], rope_base=BASE)
+    assert torch.equal(got, want) and torch.equal(a.k, b.k) and torch.equal(a.v, b.v)
 
 
 def test_edge_values_of_a_group():
@@ -322,6 +373,20 @@ def test_nan_in_a_drafted_row_reaches_those_who_see_it(where, value, M, kv_len):
         hit[..., :32] = hit[..., 64:] = False            # the group of channel 33
     assert np.isnan(outs[1][hit]).all()
     assert np.array_equal(outs[1][~hit], outs[0][~hit])
+
+
+@pytest.mark.parametrize("M,kv_len", [(3, 2000), (20, 2000), (90, 2000)])
+def test_attention_over_any_workspace(M, kv_len):
+    rng = _rng("garbage", M)
+    nh, nkv, d = 8, 2, 64
+    cache = _filled(1, nkv, d, 2112)
+    B.ghd_kv_append_q4(cache, 0, _dev(_rows(rng, kv_len + M, nkv, d)), _dev(_rows(rng, kv_len + M, nkv, d)), 0)
+    q, parent = _dev(rng.standard_normal((M, nh, d)).astype(np.float16)), _dev(_random_parent(rng, M, "random"))
+    outs = []
+    for byte in (0, 0xFF):
+        ws = B.workspace(B.ghd_attention_q4_workspace_bytes(M, kv_len, nh, nkv, d)).fill_(byte)
+        outs.append(B.ghd_tree_attention_q4(q, cache, 0, parent, kv_len, ws=ws))
+    assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
 
 
 def test_attention_same_bits_every_time_and_on_another_stream():

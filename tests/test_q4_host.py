@@ -124,3 +124,13 @@ def test_attention_refuses_bad_arguments(lib, name):
         _refuses(call, B.GHD_ERR_ALIGN, **kw)
     _refuses(call, B.GHD_ERR_WORKSPACE, ws=None)
     _refuses(call, B.GHD_ERR_WORKSPACE, n=0)
+
+
+def test_linear_refuses_rows_too_far_apart(lib):
+    """x is read at 32-bit byte offsets: rows at most 2^23 apart, 2^30 numbers in all."""
+    def linear(M, K, ldx):
+        return lib.ghd_linear_q4(FAKE, FAKE, FAKE, M, 64, K, 32, ldx, 64, 0, FAKE, 0, None)
+
+    assert linear(1, 64, (1 << 23) + 8) == B.GHD_ERR_SHAPE
+    assert linear(128, 64, 1 << 23) == B.GHD_ERR_WORKSPACE          # (127 * 2^23 < 2^30: only the workspace is too small)
+    assert linear(128, 65536, 1 << 23) == B.GHD_ERR_WORKSPACE
