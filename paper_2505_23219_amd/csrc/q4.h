@@ -112,6 +112,8 @@ struct Q4Attn {
     float *o_part, *ml_part;
     int M, kv_len, nh, nkv, tiles;   // tiles: of the whole cache, a head
     float scale;
+    int rep;                         // query heads of a key head, and 1 / rep (the launch fills these in)
+    float inv_rep;
 };
 size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d);
 ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, hipStream_t st);
