@@ -10,7 +10,7 @@
 // the end.  Up to 16 query rows what counts is that the cache streams: a ring of two tiles a wavefront.  Above, blocks of two to
 // four tiles of rows share a key's conversion, which takes longer than its products with one.  (Before, a wavefront had 16 rows,
 // and operands converted by turns came through LDS with a barrier for every 32 keys: 64 rows of 32 heads over 2112 keys 16.0 us a
-// call, now 15.4; 128 of 40 over 8320 42.7 and 42.1, over 2176 26 and 22; 13 of 4 by 7 heads over a few hundred 10.4 and 7.9.)
+// call, now 15.4; 128 of 40 over 8320 42.7 and 42.1, over 2176 26 and 22; 37 of 20 heads of 64 channels, on 4 key heads, over 814 10.4 and 7.9.)
 #include "q4.h"
 #include "attention_impl.h"
 
@@ -237,11 +237,48 @@ struct Q4Meet {
     }
 };
 
+// 1 / x, in a scalar register
+__device__ __forceinline__ float q4_inverse(int x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, __builtin_amdgcn_rcpf((float)x))));
+}
+
 // How a launch is divided: a head's rows in blocks, its keys in parts of `per` or one more tiles (the first `rem`).
 struct Q4Parts {
     int splits, blocks, per, rem;
-    float inv_splits, inv_blocks;
 };
+// What the first loads need comes in the twelve words that the hardware puts into scalar registers before a kernel starts; the
+// argument block, host memory, is 0.6 us away.
+// rows: kv_len (below 2^24) << 8 | M; heads: nkv - 1 | rep - 1 << 8 | splits (up to 768) << 16; tiles: up to 2^19 | rem << 20 |
+// whether `relation` is masks << 31
+#define Q4_FIRST const char *k, const char *v, const half_t *q, const void *relation, uint32_t rows, uint32_t heads, uint32_t tiles, int per
+__device__ __forceinline__ void q4_rows_and_heads(Q4Attn& a, uint32_t rows, uint32_t heads)
+{
+    a.M = rows & 255;
+    a.kv_len = rows >> 8;
+    a.nkv = (heads & 255) + 1;
+    a.rep = (heads >> 8 & 255) + 1;
+    a.nh = a.nkv * a.rep;
+    a.inv_rep = q4_inverse(a.rep);
+}
+__device__ __forceinline__ void q4_first(Q4Attn& a, Q4Parts& parts, Q4_FIRST)
+{
+    q4_rows_and_heads(a, rows, heads);
+    a.k = k;
+    a.v = v;
+    a.q = q;
+    a.tiles = tiles & 0xfffff;
+    a.mask = tiles >> 31 ? (const uint64_t*)relation : nullptr;
+    a.parent = tiles >> 31 ? nullptr : (const int32_t*)relation;
+    parts.splits = heads >> 16;
+    parts.per = per;
+    parts.rem = tiles >> 20 & 1023;
+}
+static uint32_t q4_rows_word(const Q4Attn& a) { return (uint32_t)a.kv_len << 8 | a.M; }
+static uint32_t q4_heads_word(const Q4Attn& a, const Q4Parts& c) { return (a.nkv - 1) | (a.rep - 1) << 8 | (uint32_t)c.splits << 16; }
+static uint32_t q4_tiles_word(const Q4Attn& a, const Q4Parts& c) { return a.tiles | c.rem << 20 | (a.mask ? 1u << 31 : 0u); }
+static const void* q4_relation(const Q4Attn& a) { return a.mask ? (const void*)a.mask : a.parent; }
+
 struct Q4Item {
     int head, block, split, R, total, t0, t1;
     __device__ __forceinline__ Q4Item(const Q4Attn& a, const Q4Parts& c, int head, int block, int split)
@@ -262,9 +299,9 @@ template <int D>
 __device__ __forceinline__ half8 q4_query(const Q4Attn& a, const Q4Item& it, int row, int g, int s)
 {
     const int node = q4_node(a, row);
-    const half_t* p = a.q + ((size_t)node * a.nh + it.head * a.rep + row - node * a.rep) * D + g * (D / 4);
+    const uint32_t at = (node * a.nh + it.head * a.rep + row - node * a.rep) * D + g * (D / 4);     // (below 2^22)
     half8 q = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (row < it.R) q = *(const half8*)(p + 8 * s);
+    if (row < it.R) q = *(const half8*)(a.q + at + 8 * s);
     return a.scale < 0.f ? -q : q;
 }
 
@@ -278,7 +315,7 @@ __device__ __forceinline__ void q4_out(const Q4Attn& a, int head, int row, int c
     half4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = none ? (half_t)0.f : (half_t)(o[e] * r);
-    *(half4*)(a.out + ((size_t)node * a.nh + head * a.rep + row - node * a.rep) * D + ct * 16 + 4 * g) = y;
+    *(half4*)(a.out + (uint32_t)((node * a.nh + head * a.rep + row - node * a.rep) * D + ct * 16 + 4 * g)) = y;
 }
 
 // ---- up to 16 rows -----------------------------------------------------------------------
@@ -408,8 +445,9 @@ __device__ __forceinline__ void q4_tile(const Q4Attn& a, const Q4Item& it, const
 }
 
 template <int D>
-__global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const Q4Attn a, const Q4Parts parts)
+__global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(Q4_FIRST, Q4Attn a, Q4Parts parts)
 {
+    q4_first(a, parts, k, v, q, relation, rows, heads, tiles, per);
     constexpr int CT = D / 16;
     __shared__ uint64_t s_mask[2 * GHD_MAX_M];
     __shared__ floatx4 s_o[kQ4KeyWaves][CT][64];
@@ -427,9 +465,9 @@ __global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const
         tile[i].load_k(keys, at(t0 + wave + i * kQ4KeyWaves), lane & 15, lane >> 4);
         tile[i].load_v(values, at(t0 + wave + i * kQ4KeyWaves), lane & 15, lane >> 4);
     }
-    half8 q[D / 32];
+    half8 x[D / 32];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) q[s] = q4_query<D>(a, it, lane & 15, lane >> 4, s);
+    for (int s = 0; s < D / 32; ++s) x[s] = q4_query<D>(a, it, lane & 15, lane >> 4, s);
     masks.store(a, wave, lane, s_mask);
     if (reaches) __syncthreads();
     const Q4Bits bits;
@@ -438,7 +476,7 @@ __global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const
     uint32_t nan = 0;                  // a bit for every group of channels of a row: it has seen one there
     int t = t0 + wave;
     // (two tiles in turn: a copy of the one on its way would have to wait for it)
-    auto query = [&](int, int k) { return q[k]; };
+    auto query = [&](int, int k) { return x[k]; };
     for (; t < t1; t += 2 * kQ4KeyWaves) {
         q4_tile<D, 1>(a, it, bits, st, query, tile[0], c, t, 0, lane, s_mask, keys, values, at(t + 2 * kQ4KeyWaves), nan);
         if (t + kQ4KeyWaves >= t1) break;
@@ -475,8 +513,9 @@ __global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(const
 constexpr int kQ4RowWaves = 8;
 
 template <int D, int RT>
-__global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(const Q4Attn a, const Q4Parts parts)
+__global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(Q4_FIRST, Q4Attn a, Q4Parts parts)
 {
+    q4_first(a, parts, k, v, q, relation, rows, heads, tiles, per);
     constexpr int CT = D / 16, KS = D / 32, W = kQ4RowWaves, kFrags = RT * CT, kRound = kFrags < 16 ? kFrags : 16;
     __shared__ uint64_t s_mask[2 * GHD_MAX_M];
     __shared__ Q4Row s_ml[W][RT * 16];
@@ -485,7 +524,7 @@ __global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(const
     // 8 xcds by blocks, by parts in eights: the blocks of a part of a head's keys share an L2
     const int item = blockIdx.y * 8 + (blockIdx.x & 7);
     if (item >= a.nkv * parts.splits) return;
-    const int head = __builtin_amdgcn_readfirstlane(q4_over(item, parts.inv_splits));
+    const int head = __builtin_amdgcn_readfirstlane(q4_over(item, q4_inverse(parts.splits)));
     const Q4Item it(a, parts, head, blockIdx.x >> 3, item - head * parts.splits);
     const int t0 = it.t0, t1 = it.t1;
     const Q4Masks masks(a, t1 * kQ4Tile > a.kv_len, wave, lane);
@@ -495,12 +534,17 @@ __global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(const
     tile.load_k(keys, tile_at(t0 + wave), lane & 15, lane >> 4);
     tile.load_v(values, tile_at(t0 + wave), lane & 15, lane >> 4);
     const int row0 = it.block * RT * 16;
+    constexpr int kMine = (RT * KS + W - 1) / W;                   // operands of q that a wavefront brings
+    half8 x[kMine];
 #pragma unroll
-    for (int f = 0; f < (RT * KS + W - 1) / W; ++f) {
-        const int frag = f * W + wave, row = row0 + frag / KS * 16 + (lane & 15);
-        if (frag < RT * KS) *(half8*)(lds + frag * 1024 + lane * 16) = q4_query<D>(a, it, row, lane >> 4, frag % KS);
+    for (int f = 0; f < kMine; ++f) {
+        const int frag = min(f * W + wave, RT * KS - 1);
+        x[f] = q4_query<D>(a, it, row0 + frag / KS * 16 + (lane & 15), lane >> 4, frag % KS);
     }
     masks.store(a, wave, lane, s_mask);
+#pragma unroll
+    for (int f = 0; f < kMine; ++f)
+        if (f * W + wave < RT * KS) *(half8*)(lds + (f * W + wave) * 1024 + lane * 16) = x[f];
     __syncthreads();
     const Q4Bits bits;
     const float c = q4_power(a.scale);
@@ -523,7 +567,7 @@ __global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(const
 #pragma unroll
         for (int f = f0; f < std::min(f0 + kRound, kFrags); ++f) part[(wave * kRound + f - f0) * 64] = st[f / CT].o[f % CT];
         __syncthreads();
-#pragma unroll 1
+#pragma unroll 2
         for (int e = wave; e < kRound && f0 + e < kFrags; e += W) {
             const int f = f0 + e, r = f / CT, ct = f % CT, row = row0 + r * 16 + col;
             const Q4Meet<W> all(s_ml, r * 16 + col);
@@ -544,14 +588,17 @@ __global__ __launch_bounds__(kQ4RowWaves * 64, 2) void k_q4_attention_rows(const
 // ---- parts of a head's keys to its rows ----------------------------------------------------
 // Four wavefronts take the parts of one fragment - 16 channels by 16 rows - in turn, eight requests at a time.
 template <int D>
-__global__ __launch_bounds__(256) void k_q4_join(const Q4Attn a, const Q4Parts parts, int row_tiles)
+__global__ __launch_bounds__(256) void k_q4_join(const float* o_part, const float* ml_part, half_t* out, uint32_t rows, uint32_t heads,
+                                                 int row_tiles, int blocks, Q4Attn a)
 {
+    q4_rows_and_heads(a, rows, heads);
+    a.out = out;
     constexpr int CT = D / 16, kAt = 8;
     __shared__ floatx4 s_o[4][64];
     __shared__ floatx2 s_ml[4][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const int ct = blockIdx.x, rt = blockIdx.y, hb = blockIdx.z, splits = parts.splits;
-    const int head = q4_over(hb, parts.inv_blocks), block = hb - head * parts.blocks, row = (block * row_tiles + rt) * 16 + col;
+    const int ct = blockIdx.x, rt = blockIdx.y, hb = blockIdx.z, splits = heads >> 16;
+    const int head = q4_over(hb, q4_inverse(blocks)), block = hb - head * blocks, row = (block * row_tiles + rt) * 16 + col;
     if ((block * row_tiles + rt) * 16 >= a.M * a.rep) return;
     float m = -INFINITY, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
@@ -562,8 +609,8 @@ __global__ __launch_bounds__(256) void k_q4_join(const Q4Attn a, const Q4Parts p
 #pragma unroll
         for (int j = 0; j < kAt; ++j) {
             const size_t unit = ((size_t)hb * splits + min(p0 + 4 * j, splits - 1)) * row_tiles + rt;
-            ml[j] = ((const floatx2*)a.ml_part)[unit * 16 + col];
-            v[j] = ((const floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane];
+            ml[j] = ((const floatx2*)ml_part)[unit * 16 + col];
+            v[j] = ((const floatx4*)o_part)[(unit * CT + ct) * 64 + lane];
         }
 #pragma unroll
         for (int j = 0; j < kAt; ++j)
@@ -657,7 +704,8 @@ static ghd_status q4_rows_of(const Q4Attn& a, const Q4Parts& c, hipStream_t st)
     const size_t lds = (size_t)kQ4RowWaves * std::min(RT * (D / 16), 16) * 1024;
     const ghd_status s = launch_resident_checked((const void*)k_q4_attention_rows<D, RT>, kQ4RowWaves * 64, lds, nullptr);
     if (s) return s;
-    hipLaunchKernelGGL((k_q4_attention_rows<D, RT>), dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(kQ4RowWaves * 64), lds, st, a, c);
+    hipLaunchKernelGGL((k_q4_attention_rows<D, RT>), dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(kQ4RowWaves * 64), lds, st, a.k,
+                       a.v, a.q, q4_relation(a), q4_rows_word(a), q4_heads_word(a, c), q4_tiles_word(a, c), c.per, a, c);
     return check_launch();
 }
 
@@ -665,16 +713,18 @@ template <int D>
 static ghd_status q4_attention_of(const Q4Attn& a, const Q4AttnCut& c, hipStream_t st)
 {
     const int ntiles = ceil_div(a.kv_len + a.M, kQ4Tile);
-    const Q4Parts p = {c.splits, c.blocks, ntiles / c.splits, ntiles % c.splits, 1.f / (float)c.splits, 1.f / (float)c.blocks};
+    const Q4Parts p = {c.splits, c.blocks, ntiles / c.splits, ntiles % c.splits};
     ghd_status s;
     if (c.rows == 1) {
-        hipLaunchKernelGGL(k_q4_attention_keys<D>, dim3(c.splits, a.nkv), dim3(kQ4KeyWaves * 64), 0, st, a, p);
+        hipLaunchKernelGGL(k_q4_attention_keys<D>, dim3(c.splits, a.nkv), dim3(kQ4KeyWaves * 64), 0, st, a.k, a.v, a.q, q4_relation(a),
+                           q4_rows_word(a), q4_heads_word(a, p), q4_tiles_word(a, p), p.per, a, p);
         s = check_launch();
     } else {
         s = c.rows == 2 ? q4_rows_of<D, 2>(a, p, st) : c.rows == 3 ? q4_rows_of<D, 3>(a, p, st) : q4_rows_of<D, 4>(a, p, st);
     }
     if (s || c.splits == 1) return s;
-    hipLaunchKernelGGL(k_q4_join<D>, dim3(D / 16, c.rows, a.nkv * c.blocks), dim3(256), 0, st, a, p, c.rows);
+    hipLaunchKernelGGL(k_q4_join<D>, dim3(D / 16, c.rows, a.nkv * c.blocks), dim3(256), 0, st, a.o_part, a.ml_part, a.out,
+                       q4_rows_word(a), q4_heads_word(a, p), c.rows, c.blocks, a);
     return check_launch();
 }
 
