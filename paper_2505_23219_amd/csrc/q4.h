@@ -41,6 +41,16 @@ static inline size_t q4_weight_bytes(int N, int K, int group)
 }
 
 #ifdef __HIPCC__
+// 1 / x, in a scalar register
+__device__ __forceinline__ float q4_inverse(int x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, __builtin_amdgcn_rcpf((float)x))));
+}
+
+// x / n of an x below 2^15 and an n up to 2^10, by 1 / n: half a unit above x the quotient is at least 1 / 2048 from a whole number,
+// and what is rounded in it is less than x / n 2^-22
+__device__ __forceinline__ int q4_over(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
+
 // ---- codes to numbers --------------------------------------------------------------------
 // Masks and 1024.0 are kept in registers: as literals they make an AND and an OR of 8 bytes each out of one instruction.
 struct Q4Bits {

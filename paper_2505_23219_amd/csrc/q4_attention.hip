@@ -237,12 +237,6 @@ struct Q4Meet {
     }
 };
 
-// 1 / x, in a scalar register
-__device__ __forceinline__ float q4_inverse(int x)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, __builtin_amdgcn_rcpf((float)x))));
-}
-
 // How a launch is divided: a head's rows in blocks, its keys in parts of `per` or one more tiles (the first `rem`).
 struct Q4Parts {
     int splits, blocks, per, rem;
@@ -289,9 +283,7 @@ struct Q4Item {
     __device__ __forceinline__ int unit(const Q4Parts& c) const { return (head * c.blocks + block) * c.splits + split; }
 };
 
-// x / n of an x below 2^15 and an n up to 2^10, by 1 / n: half a unit above x the quotient is at least 1 / 2048 from a whole number,
-// and what is rounded in it is less than x / n 2^-22
-__device__ __forceinline__ int q4_over(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
+// the node of a row
 __device__ __forceinline__ int q4_node(const Q4Attn& a, int row) { return q4_over(row, a.inv_rep); }
 
 // operand s of a row; zeros where there is no row

@@ -36,24 +36,52 @@ __device__ __forceinline__ void q4_store(const Q4Linear& a, int n, int m0, float
     }
 }
 
+// What the first loads need comes in the twelve words that the hardware puts into scalar registers before a kernel starts; the
+// argument block, host memory, is 0.6 us away.  cut: M | (groups of rows - 1) << 8 | log2 of the parts of k << 9.
 struct Q4Launch {
-    int ntiles, nunits, splits, items, row_groups;
+    int ntiles, nunits, log_splits, splits, log_groups, row_groups;
 };
+#define Q4_LINEAR_FIRST const char *W, const half_t *x_rows, float *parts, void *out, int ldx, uint32_t cut, int K, int ntiles
+__device__ __forceinline__ Q4Launch q4_linear_first(Q4Linear& a, Q4_LINEAR_FIRST)
+{
+    a.W = W;
+    a.x = x_rows;
+    a.part = parts;
+    a.y = out;
+    a.ldx = ldx;
+    a.M = cut & 255;
+    a.K = K;
+    Q4Launch c;
+    c.ntiles = ntiles;
+    c.nunits = (K + kQ4Unit - 1) / kQ4Unit;
+    c.log_splits = cut >> 9;
+    c.splits = 1 << c.log_splits;
+    c.log_groups = cut >> 8 & 1;
+    c.row_groups = 1 << c.log_groups;
+    return c;
+}
+// Where a workgroup begins in its range of n units: x modulo n, of x below 2^15 or anything.
+__device__ __forceinline__ int q4_turn(int x, int n)
+{
+    const int at = x & 0x7fff;
+    return __builtin_amdgcn_readfirstlane(at - q4_over(at, q4_inverse(n)) * n);
+}
 
 template <int MT, int R, int G>
-__global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(const Q4Linear a, const Q4Launch c)
+__global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST, Q4Linear a)
 {
+    const Q4Launch c = q4_linear_first(a, W, x_rows, parts, out, ldx, cut, K, ntiles);
     constexpr int kUnitBytes = 1024 + 64 * G, kHalf = MT * 2048;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     // workgroup (q row_groups + rows) 8 + xcd: item 8 q + xcd, one of the groups of rows
-    const int q8 = blockIdx.x >> 3, rows = q8 % c.row_groups, item = q8 / c.row_groups * 8 + (blockIdx.x & 7);
-    if (item >= c.items) return;
+    const int q8 = blockIdx.x >> 3, rows = q8 & (c.row_groups - 1), item = (q8 >> c.log_groups) * 8 + (blockIdx.x & 7);
+    if (item >> c.log_splits >= (c.ntiles + R - 1) / R) return;
     const int mrow0 = rows * MT * 16, M = min(a.M - mrow0, MT * 16);
-    const int split = item % c.splits, tile0 = item / c.splits * R;
-    const int u0 = c.nunits * split / c.splits, n = c.nunits * (split + 1) / c.splits - u0;
-    const int turn = q8 / c.row_groups % n, mine = (n - wave + kQ4LinWaves - 1) / kQ4LinWaves;     // this wavefront's units
+    const int split = item & (c.splits - 1), tile0 = (item >> c.log_splits) * R;
+    const int u0 = c.nunits * split >> c.log_splits, n = (c.nunits * (split + 1) >> c.log_splits) - u0;
+    const int turn = q4_turn(q8 >> c.log_groups, n), mine = (n - wave + kQ4LinWaves - 1) / kQ4LinWaves;     // this wavefront's units
     // x through a buffer resource: what lies behind its last row is not read
     const __amdgpu_buffer_rsrc_t xbuf = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)mrow0 * a.ldx), 0,
                                                                           (int)(((M - 1) * a.ldx + a.K) * 2), 0x00027000);
@@ -177,22 +205,23 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(const Q4Linear a
 constexpr int kQ4Groups = 4, kQ4Shares = 4, kQ4RowThreads = kQ4Groups * kQ4Shares * 64;
 
 template <int MT, int RW, int G>
-__global__ __launch_bounds__(kQ4RowThreads) void k_q4_linear_shared(const Q4Linear a, const Q4Launch c)
+__global__ __launch_bounds__(kQ4RowThreads) void k_q4_linear_shared(Q4_LINEAR_FIRST, Q4Linear a)
 {
+    const Q4Launch c = q4_linear_first(a, W, x_rows, parts, out, ldx, cut, K, ntiles);
     constexpr int kUnitBytes = 1024 + 64 * G, kBuf = MT * 4096, KH = kQ4Shares;
     // k-steps summed up before the scale is applied; row tiles whose sums are under way (what the registers hold)
     constexpr int kSteps = G == 2 && MT * RW == 8 ? 1 : 4 / G, kAt = kSteps == 1 && MT > 3 ? 2 : MT;
     // workgroup (q row_groups + rows) 8 + xcd: item 8 q + xcd, one of the groups of rows
-    const int q8 = blockIdx.x >> 3, rows = q8 % c.row_groups, item = q8 / c.row_groups * 8 + (blockIdx.x & 7);
-    if (item >= c.items) return;
+    const int q8 = blockIdx.x >> 3, rows = q8 & (c.row_groups - 1), item = (q8 >> c.log_groups) * 8 + (blockIdx.x & 7);
+    if (item >> c.log_splits >= (c.ntiles + kQ4Groups * RW - 1) / (kQ4Groups * RW)) return;
     const int mrow0 = rows * MT * 16, M = min(a.M - mrow0, MT * 16);
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int share = wave / kQ4Groups, grp = wave % kQ4Groups;
-    const int split = item % c.splits, tile0 = (item / c.splits * kQ4Groups + grp) * RW;
-    const int u0 = c.nunits * split / c.splits, n = c.nunits * (split + 1) / c.splits - u0;
-    const int turn = q8 / c.row_groups % n;
+    const int split = item & (c.splits - 1), tile0 = ((item >> c.log_splits) * kQ4Groups + grp) * RW;
+    const int u0 = c.nunits * split >> c.log_splits, n = (c.nunits * (split + 1) >> c.log_splits) - u0;
+    const int turn = q4_turn(q8 >> c.log_groups, n);
     // the turn of four with the unit that K does not fill
     const int short_turn = a.K % kQ4Unit != 0 && u0 + n == c.nunits ? (turn == n - 1 ? 0 : n - 1 - turn) / KH : -1;
     // x through a buffer resource: what lies behind its last row is not read.  A wavefront requests 8 rows (the first or last
@@ -346,13 +375,19 @@ __global__ __launch_bounds__(kQ4RowThreads) void k_q4_linear_shared(const Q4Line
         }
 }
 
-// Sums of the parts of k, in their order.  A wavefront takes one fragment.
-__global__ __launch_bounds__(256) void k_q4_linear_sum(const Q4Linear a, int frags, int mts, int splits)
+// Sums of the parts of k, in their order.  A wavefront takes one fragment.  cut: M | parts << 8 | (fp16 results) << 16.
+__global__ __launch_bounds__(256) void k_q4_linear_sum(const floatx4* part, void* out, int N, int ntiles, int64_t ldy, uint32_t cut)
 {
-    const int lane = threadIdx.x & 63, f = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (f >= frags) return;
-    const floatx4* p = (const floatx4*)a.part + (size_t)f * 64 + lane;
-    const size_t step = (size_t)frags * 64;
+    const int lane = threadIdx.x & 63, tile = blockIdx.x * 4 + (threadIdx.x >> 6), mt = blockIdx.y, mts = gridDim.y, splits = cut >> 8 & 255;
+    if (tile >= ntiles) return;
+    Q4Linear a = {};
+    a.y = out;
+    a.M = cut & 255;
+    a.N = N;
+    a.ldy = ldy;
+    a.out16 = cut >> 16;
+    const floatx4* p = part + ((size_t)tile * mts + mt) * 64 + lane;
+    const size_t step = (size_t)ntiles * mts * 64;
     floatx4 y = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < splits; s0 += 8) {          // eight requests at a time
         floatx4 v[8];
@@ -362,7 +397,7 @@ __global__ __launch_bounds__(256) void k_q4_linear_sum(const Q4Linear a, int fra
         for (int s = 0; s < 8; ++s)
             if (s0 + s < splits) y += v[s];
     }
-    q4_store(a, f / mts * 16 + (lane & 15), f % mts * 16 + 4 * (lane >> 4), y);
+    q4_store(a, tile * 16 + (lane & 15), mt * 16 + 4 * (lane >> 4), y);
 }
 
 struct Q4Cut {
@@ -414,18 +449,19 @@ size_t q4_linear_bytes(int M, int N, int K)
     return c.splits == 1 ? 256 : align_up((size_t)c.splits * ceil_div(N, 16) * q4_row_groups(M, c.mt) * c.mt * 1024, 256);
 }
 
-static ghd_status q4_linear_start(const Q4Linear& a, const Q4Cut& c, void (*kernel)(Q4Linear, Q4Launch), int threads, int tiles, size_t lds,
-                                  hipStream_t st)
+static ghd_status q4_linear_start(const Q4Linear& a, const Q4Cut& c,
+                                  void (*kernel)(const char*, const half_t*, float*, void*, int, uint32_t, int, int, Q4Linear), int threads,
+                                  int tiles, size_t lds, hipStream_t st)
 {
     const int groups = q4_row_groups(a.M, c.mt), ntiles = ceil_div(a.N, 16);
-    const Q4Launch l = {ntiles, ceil_div(a.K, kQ4Unit), c.splits, ceil_div(ntiles, tiles) * c.splits, groups};
     const ghd_status s = launch_resident_checked((const void*)kernel, threads, lds, nullptr);
     if (s) return s;
-    hipLaunchKernelGGL(kernel, dim3(ceil_div(l.items, 8) * 8 * groups), dim3(threads), lds, st, a, l);
-    if (c.splits > 1) {
-        const int frags = ntiles * groups * c.mt;
-        hipLaunchKernelGGL(k_q4_linear_sum, dim3(ceil_div(frags, 4)), dim3(256), 0, st, a, frags, groups * c.mt, c.splits);
-    }
+    const uint32_t cut = a.M | (groups - 1) << 8 | __builtin_ctz(c.splits) << 9;
+    hipLaunchKernelGGL(kernel, dim3(ceil_div(ceil_div(ntiles, tiles) * c.splits, 8) * 8 * groups), dim3(threads), lds, st, a.W, a.x, a.part, a.y,
+                       (int)a.ldx, cut, a.K, ntiles, a);
+    if (c.splits > 1)
+        hipLaunchKernelGGL(k_q4_linear_sum, dim3(ceil_div(ntiles, 4), groups * c.mt), dim3(256), 0, st, (const floatx4*)a.part, a.y, a.N, ntiles,
+                           a.ldy, a.M | c.splits << 8 | (a.out16 ? 1u << 16 : 0u));
     return check_launch();
 }
 
