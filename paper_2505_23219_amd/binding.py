@@ -616,16 +616,17 @@ def ghd_attention_q4_workspace_bytes(M: int, kv_len: int, nh: int, nkv: int, d: 
 
 def _attention_q4(fn, name, q, cache, layer, relation, kv_len, scale, ws, out):
     M, nh, d = q.shape
-    assert d == cache.d
+    assert q.is_cuda and q.dtype is torch.float16 and q.is_contiguous() and d == cache.d, (q.device, q.dtype, q.shape)
     if out is None:
         out = torch.empty_like(q)
-    if scale is None:
-        scale = 1.0 / (d ** 0.5)
+    else:
+        assert out.is_cuda and out.dtype is torch.float16 and out.is_contiguous() and out.shape == q.shape, (out.dtype, out.shape)
     if ws is None:
-        ws = workspace(lib().ghd_attention_q4_workspace_bytes(M, kv_len, nh, cache.nkv, d), q.device)
-    assert out.shape == q.shape
-    _check(fn(_ptr(_dev(out, torch.float16)), _ptr(_dev(q, torch.float16)), cache.layers[layer], relation, M, kv_len, nh,
-              cache.nkv, d, cache.capacity, scale, _ptr(ws), ws.numel(), _stream()), name)
+        ws = workspace(_lib.ghd_attention_q4_workspace_bytes(M, kv_len, nh, cache.nkv, d), q.device)
+    st = fn(out.data_ptr(), q.data_ptr(), cache.layers[layer], relation.data_ptr(), M, kv_len, nh, cache.nkv, d, cache.capacity,
+            d ** -0.5 if scale is None else scale, ws.data_ptr(), ws.numel(), _stream())
+    if st:
+        _check(st, name)
     return out
 
 
@@ -634,8 +635,8 @@ def ghd_tree_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, parent: torc
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q fp16 [M, nh, d] over the rows [0, kv_len + M) of a layer; returns fp16 [M, nh, d]."""
     assert parent.numel() == q.shape[0]
-    return _attention_q4(lib().ghd_tree_attention_q4, "ghd_tree_attention_q4", q, cache, layer,
-                         _ptr(_dev(parent, torch.int32)), kv_len, scale, ws, out)
+    return _attention_q4(lib().ghd_tree_attention_q4, "ghd_tree_attention_q4", q, cache, layer, _dev(parent, torch.int32), kv_len,
+                         scale, ws, out)
 
 
 def ghd_masked_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, mask: torch.Tensor, kv_len: int,
@@ -643,8 +644,8 @@ def ghd_masked_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, mask: torc
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """As ghd_tree_attention_q4 with the relation as int64 [M, 2] bit masks (ghd_masked_attention)."""
     assert mask.shape == (q.shape[0], 2)
-    return _attention_q4(lib().ghd_masked_attention_q4, "ghd_masked_attention_q4", q, cache, layer,
-                         _ptr(_dev(mask, torch.int64)), kv_len, scale, ws, out)
+    return _attention_q4(lib().ghd_masked_attention_q4, "ghd_masked_attention_q4", q, cache, layer, _dev(mask, torch.int64), kv_len,
+                         scale, ws, out)
 
 
 def ghd_commit_path_q4(cache: KvQ4, res: torch.Tensor, M: int, kv_len: int) -> None:

@@ -126,7 +126,7 @@ struct Q4Attn {
     float inv_rep;
 };
 size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d);
-ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, hipStream_t st);
+ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, size_t ws_bytes, hipStream_t st);     // GHD_ERR_WORKSPACE: too small
 
 struct Q4Linear {
     void* y;
@@ -138,7 +138,7 @@ struct Q4Linear {
     bool out16;
 };
 size_t q4_linear_bytes(int M, int N, int K);
-ghd_status launch_q4_linear(const Q4Linear& a, void* ws, hipStream_t st);
+ghd_status launch_q4_linear(Q4Linear a, void* ws, size_t ws_bytes, hipStream_t st);              // the same
 ghd_status launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int N, int K, int group,
                           hipStream_t st);
 

@@ -42,7 +42,6 @@ static ghd_status attention_q4(void* out, const void* q, const ghd_kv* kv, const
     if (!aligned_to(out, 16) || !aligned_to(q, 16) || !aligned_to(mask, 8) || !aligned_to(parent, 4)) return GHD_ERR_ALIGN;
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!aligned_to(ws, 16)) return GHD_ERR_ALIGN;
-    if (ws_bytes < q4_attention_bytes(M, kv_len, nh, nkv, d)) return GHD_ERR_WORKSPACE;
     Q4Attn a = {};
     a.out = (half_t*)out;
     a.q = (const half_t*)q;
@@ -56,7 +55,7 @@ static ghd_status attention_q4(void* out, const void* q, const ghd_kv* kv, const
     a.nkv = nkv;
     a.tiles = cap / kQ4Tile;
     a.scale = scale;
-    return launch_q4_attention(a, d, ws, (hipStream_t)stream);
+    return launch_q4_attention(a, d, ws, ws_bytes, (hipStream_t)stream);
 }
 
 }  // namespace ghd
@@ -92,7 +91,6 @@ ghd_status ghd_linear_q4(void* y, const void* x, const void* Wq, int M, int N, i
     if (!aligned_to(x, 16) || !aligned_to(Wq, 16) || !aligned_to(y, 16) || ldx % 8 != 0) return GHD_ERR_ALIGN;
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!aligned_to(ws, 16)) return GHD_ERR_ALIGN;
-    if (ws_bytes < q4_linear_bytes(M, N, K)) return GHD_ERR_WORKSPACE;
     Q4Linear a = {};
     a.y = y;
     a.x = (const half_t*)x;
@@ -104,7 +102,7 @@ ghd_status ghd_linear_q4(void* y, const void* x, const void* Wq, int M, int N, i
     a.ldx = ldx;
     a.ldy = ldy;
     a.out16 = flags == GHD_OUT_F16;
-    return launch_q4_linear(a, ws, (hipStream_t)stream);
+    return launch_q4_linear(a, ws, ws_bytes, (hipStream_t)stream);
 }
 
 size_t ghd_kv_q4_bytes(int nkv, int capacity, int d)

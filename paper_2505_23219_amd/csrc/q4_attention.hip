@@ -667,7 +667,7 @@ static Q4AttnCut q4_attn_cut(int M, int kv_len, int nh, int nkv, int d)
         const int blocks = ceil_div(rt, most), rows = ceil_div(rt, blocks), items = nkv * blocks;
         if (rows != most) continue;
         const float turn = d == 128 ? 1.2f + 0.4f * rows : 0.72f + 0.24f * rows, rest = d == 128 ? 3.6f + 1.7f * rows : 3.8f + 0.85f * rows;
-        for (int splits = 1; splits == 1 || (splits * items <= 256 && splits <= ntiles); ++splits) {
+        for (int splits = 1; splits == 1 || (splits * items <= 256 && splits <= ntiles); splits += 1 + splits / 8) {
             const int turns = ceil_div(ceil_div(ntiles, splits), kQ4RowWaves), rounds = ceil_div(items * splits, 256);
             float us = rounds * (rest + turns * turn);
             if (splits > 1) us += 3.5f + 0.35e-6f * 64.f * d * splits * items * rows;
@@ -682,12 +682,16 @@ static Q4AttnCut q4_attn_cut(int M, int kv_len, int nh, int nkv, int d)
 
 static size_t q4_attn_units(const Q4AttnCut& c, int nkv) { return (size_t)nkv * c.blocks * c.splits * c.rows; }
 
-size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
+static size_t q4_attn_bytes(const Q4AttnCut& c, int nkv, int d)
 {
-    const Q4AttnCut c = q4_attn_cut(M, kv_len, nh, nkv, d);
     if (c.splits == 1) return 256;
     const size_t units = q4_attn_units(c, nkv);
     return align_up(units * 16 * d * 4, 256) + align_up(units * 128, 256);
+}
+
+size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
+{
+    return q4_attn_bytes(q4_attn_cut(M, kv_len, nh, nkv, d), nkv, d);
 }
 
 template <int D, int RT>
@@ -720,9 +724,10 @@ static ghd_status q4_attention_of(const Q4Attn& a, const Q4AttnCut& c, hipStream
     return check_launch();
 }
 
-ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, hipStream_t st)
+ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, size_t ws_bytes, hipStream_t st)
 {
     const Q4AttnCut c = q4_attn_cut(a.M, a.kv_len, a.nh, a.nkv, d);
+    if (ws_bytes < q4_attn_bytes(c, a.nkv, d)) return GHD_ERR_WORKSPACE;
     a.rep = a.nh / a.nkv;
     a.inv_rep = 1.f / (float)a.rep;
     a.o_part = (float*)ws;

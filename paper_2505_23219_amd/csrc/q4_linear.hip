@@ -443,11 +443,12 @@ static Q4Cut q4_cut(int M, int N, int K)
     return best;
 }
 
-size_t q4_linear_bytes(int M, int N, int K)
+static size_t q4_cut_bytes(const Q4Cut& c, int M, int N)
 {
-    const Q4Cut c = q4_cut(M, N, K);
     return c.splits == 1 ? 256 : align_up((size_t)c.splits * ceil_div(N, 16) * q4_row_groups(M, c.mt) * c.mt * 1024, 256);
 }
+
+size_t q4_linear_bytes(int M, int N, int K) { return q4_cut_bytes(q4_cut(M, N, K), M, N); }
 
 static ghd_status q4_linear_start(const Q4Linear& a, const Q4Cut& c,
                                   void (*kernel)(const char*, const half_t*, float*, void*, int, uint32_t, int, int, Q4Linear), int threads,
@@ -507,8 +508,10 @@ static ghd_status q4_linear_tiles(const Q4Linear& a, const Q4Cut& c, hipStream_t
     return q4_linear_group<MT, 2>(a, c, st);
 }
 
-static ghd_status q4_linear_cut(Q4Linear a, const Q4Cut& c, void* ws, hipStream_t st)
+ghd_status launch_q4_linear(Q4Linear a, void* ws, size_t ws_bytes, hipStream_t st)
 {
+    const Q4Cut c = q4_cut(a.M, a.N, a.K);
+    if (ws_bytes < q4_cut_bytes(c, a.M, a.N)) return GHD_ERR_WORKSPACE;
     a.part = (float*)ws;
     switch (c.mt) {
     case 1: return q4_linear_tiles<1>(a, c, st);
@@ -516,11 +519,6 @@ static ghd_status q4_linear_cut(Q4Linear a, const Q4Cut& c, void* ws, hipStream_
     case 3: return q4_linear_tiles<3>(a, c, st);
     default: return q4_linear_tiles<4>(a, c, st);
     }
-}
-
-ghd_status launch_q4_linear(const Q4Linear& a, void* ws, hipStream_t st)
-{
-    return q4_linear_cut(a, q4_cut(a.M, a.N, a.K), ws, st);
 }
 
 // ---- packing -----------------------------------------------------------------------------
