@@ -97,7 +97,8 @@ __device__ __forceinline__ uint32_t keys_of_channel(uint32_t w, int lane)
 // those half a row further, which turn with them: two 16-byte requests, and a word of K codes, each.  The workgroup's
 // four wavefronts have one octet, whose cosines and sines, worked out in 64 bits, they share through LDS (worked out by every
 // wavefront for itself the smallest call took 9 us, 4096 rows of 32 + 8 heads 47).
-// Bound: for a tree's rows latency - parents, cosines, rows, one behind the other; for a prompt the bytes.
+// Bound: for a tree's rows latency - parents, cosines, rows, one behind the other (64 rows of 32 heads and 32 key heads 7 us); for a
+// prompt the bytes (4096 rows of 32 and 8 heads 23 us for 89 MB, 3.9 TB/s; a copy reaches 4.75).
 template <int D>
 __global__ __launch_bounds__(256) void k_q4_append(const Q4Append a, int chunks, int per_chunk)
 {
@@ -233,7 +234,7 @@ struct Q4Layers {
 
 // One wavefront a (layer, head, K or V).  The path's rows are taken eight at a time, all read before the first is written;
 // rows come from behind where they go (path[j] >= j), so a later eight's are still as they were.
-// Bound: latency, two trips to memory one behind the other.
+// Bound: latency, two trips to memory one behind the other: 4 rows of 32 heads in 32 layers 4.8 us.
 template <int D>
 __global__ __launch_bounds__(256) void k_q4_commit(const Q4Layers a, int L, int nkv, int tiles, int kv_len, int M,
                                                    const int32_t* res)
@@ -333,7 +334,8 @@ ghd_status launch_q4_commit(void* const* k, void* const* v, int L, int nkv, int 
 }
 
 // ---- reading back ------------------------------------------------------------------------
-// A wavefront reads one octet of a (layer, head), K and V, and writes rows of fp16.  Bound: the bytes written.
+// A wavefront reads one octet of a (layer, head), K and V, and writes rows of fp16.  Bound: the bytes written (64 rows of 32
+// heads in 32 layers, 34 MB, 10.5 us), for fewer a launch (3.2 us).
 template <int D>
 __global__ __launch_bounds__(256) void k_q4_read(const Q4Layers a, int nkv, int tiles, int octets, int row0, int rows,
                                                  half_t* ko, half_t* vo, int64_t units)
