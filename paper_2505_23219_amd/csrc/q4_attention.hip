@@ -10,7 +10,7 @@
 // the end.  Up to 16 query rows what counts is that the cache streams: a ring of two tiles a wavefront.  Above, blocks of two to
 // four tiles of rows share a key's conversion, which takes longer than its products with one.  (Before, a wavefront had 16 rows,
 // and operands converted by turns came through LDS with a barrier for every 32 keys: 64 rows of 32 heads over 2112 keys 16.0 us a
-// call, now 15.4; 128 of 40 over 8320 42.7 and 42.1, over 2176 26 and 22; 37 of 20 heads of 64 channels, on 4 key heads, over 814 10.4 and 7.9.)
+// call, this way 14.4; 128 of 40 over 8320 42.7 and 40.8; 37 of 20 heads of 64 channels, on 4 key heads, over 814 10.4 and 7.7.)
 #include "q4.h"
 #include "attention_impl.h"
 
@@ -311,6 +311,8 @@ __device__ __forceinline__ void q4_out(const Q4Attn& a, int head, int row, int c
 }
 
 // ---- up to 16 rows -----------------------------------------------------------------------
+// Bound: the bytes (1 row of 32 heads, on 8 key heads, over 65537 keys 20.2 us, 4.2 TB/s of a copy's 4.75, the second launch among
+// them); over few keys the way from queries and masks to the states' meeting (6 us).
 constexpr int kQ4KeyWaves = 4;
 
 // a tile of 32 keys, as a wavefront has it on its way
@@ -496,11 +498,14 @@ __global__ __launch_bounds__(kQ4KeyWaves * 64, 3) void k_q4_attention_keys(Q4_FI
 }
 
 // ---- more rows ---------------------------------------------------------------------------
-// Blocks of RT tiles of 16 rows, queries as operands in LDS.  Bound, over many keys, by vector instructions: with four tiles of rows
-// 240 for the conversion of a tile of keys and 62 for the softmax of each (the exponentials, at a quarter of the rate, are half of
-// those), 85% of the time that it takes; products are 1090 of 2640 cycles beside them.  Over few keys by what comes one after
-// another: 2.5 us to the first products, 1.3 us of them the queries, and 2 to 4 us until the states have met.  A workgroup of four
-// wavefronts instead of eight, two of them on a compute unit: 64 rows of 32 heads over 2112 keys 19.6 us instead of 15.2.
+// Blocks of RT tiles of 16 rows, queries as operands in LDS.
+// Bound, over many keys, by the issue of vector instructions: 32 keys by four tiles of rows take 2640 cycles of a wavefront when two
+// share a SIMD, of them 240 instructions for the conversion and 62 for the softmax of each tile (exponentials, at a quarter of
+// the rate, are half of those) at 4 cycles, and 68 products, which keep the issue for 10 cycles each (measured: 17 cycles for
+// a product alone, 32 for 8 packed instructions, 42 for both).  128 rows of 40 heads over 8320 keys: 41 us, 0.53 PFLOP/s.
+// Over few keys by what comes one after another, in cycles of 64 rows of 32 heads: 5000 until queries are there, 1600 for the
+// ancestors' masks meanwhile, 3500 for the first keys (whose instructions are fetched, too), 4700 until the states have met.
+// Four wavefronts a workgroup and two of those on a compute unit: 64 rows of 32 heads over 2112 keys 19.6 us instead of 15.2.
 // Queries in registers: 32 rows over 224 keys 9.9 instead of 8.6 us (all wavefronts read all of them).
 constexpr int kQ4RowWaves = 8;
 
@@ -655,8 +660,8 @@ static int q4_key_splits(int ntiles, int nkv)
 // Above, what is estimated to be fastest of blocks of 2, 3 and 4 tiles of rows and of parts that fill the compute units once: a turn
 // of the wavefronts takes 2.0, 2.4 or 2.8 us, so the larger a block the better where keys are many, and getting to the first and
 // from the last 7, 9 or 10.4 (with 64 channels .6 of the one, 5.5, 6.5 and 7.2 of the other), so the smaller the better where
-// they are few.  64 rows of 32 heads, traced: over 512 keys blocks of 2 9.8, of 4 12.8; over 8256 22.0 and 22.2; 128 rows of 40
-// heads over 8320 64 and 41.
+// they are few.  64 rows of 32 heads, the kernel alone: over 512 keys blocks of 2 9.8, of 4 12.8; over 8256 22.0 and 22.2; 128
+// rows of 40 heads over 8320 64 and 41.
 static Q4AttnCut q4_attn_cut(int M, int kv_len, int nh, int nkv, int d)
 {
     const int rt = ceil_div(M * (nh / nkv), 16), ntiles = ceil_div(kv_len + M, kQ4Tile);

@@ -13,6 +13,7 @@
 // reads 36 bytes/ns instead of 121.  LDS takes a request lane after lane; so that operands are read without bank conflicts the
 // 16-byte pieces of row r of the 8 lie in the order piece ^ r.  Above 64 rows there are two groups of rows in workgroups of
 // their own, on the same XCD, whose L2 has the weights for the second.
+// Bound: at one row the bytes ([22016, 4096] 11.4 us, 4.1 TB/s); for small matrices the launch (3 to 4 us).
 // Every workgroup begins somewhere else in its range (`turn`): rows of x are often a power of two apart, a unit's 256 bytes of
 // all of them then lie in one channel of the L2, and all workgroups would ask that one at a time.
 #include "q4.h"
@@ -201,7 +202,10 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST,
 // Four groups of wavefronts have RW tiles each; four shares of every group take the units of the workgroup's k range in turn, x
 // and weights of the next four requested while four are worked on, one barrier every four; the shares' sums meet in LDS.  (Two
 // shares of twice the registers, operands read ahead: [22016, 4096] at 64 rows 24.4 us, 21.8 with four; a finer ring, half
-// a unit a barrier: 25.8.)
+// a unit a barrier: 25.8; two shares with three turns under way instead of one: 23.2 and 22.3.)
+// Bound: [32000, 5120] at 128 rows, 58 us with all weights from HBM, would take 27 with neither weights nor x to fetch, 33 with x
+// alone, 50 with weights alone: their way into a compute unit, at 2 TB/s of the card's 4.75, with more of them under way no faster.
+// [4096, 11008] at 64 rows: 10 us, 4 of them before the first and behind the last product, and a launch that adds up.
 constexpr int kQ4Groups = 4, kQ4Shares = 4, kQ4RowThreads = kQ4Groups * kQ4Shares * 64;
 
 template <int MT, int RW, int G>
