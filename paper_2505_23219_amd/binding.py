@@ -576,6 +576,10 @@ class KvQ4:
         self.kv = (KV * L)(*[KV(self.k[i].data_ptr(), self.v[i].data_ptr()) for i in range(L)])
         self.layers = [C.byref(kv) for kv in self.kv]
 
+    @property
+    def device(self) -> torch.device:
+        return self.k.device
+
 
 def _row_step(t: torch.Tensor, M: int, heads: int, d: int) -> int:
     """How far the rows of a [M, heads, d] tensor whose heads lie side by side are apart."""
@@ -596,9 +600,11 @@ def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, 
     nh, ld_q, ld_qo, q_ptr, qo_ptr, tree = 0, 0, 0, None, None, None
     if q is not None:
         nh = q.shape[1]
+        ld_q = _row_step(q, M, nh, d)
         if q_out is None:
-            q_out = torch.empty((M, nh, d), dtype=torch.float16, device=q.device)
-        ld_q, ld_qo = _row_step(q, M, nh, d), _row_step(q_out, M, nh, d)
+            q_out, ld_qo = torch.empty((M, nh, d), dtype=torch.float16, device=cache.device), nh * d
+        else:
+            ld_qo = _row_step(q_out, M, nh, d)
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     if parent is not None:
         assert parent.numel() == M
@@ -650,8 +656,10 @@ def ghd_masked_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, mask: torc
 
 def ghd_commit_path_q4(cache: KvQ4, res: torch.Tensor, M: int, kv_len: int) -> None:
     """ghd_commit_path for all layers of a 4-bit cache."""
-    _check(lib().ghd_commit_path_q4(cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, _ptr(_dev(res, torch.int32)),
-                                    M, kv_len, _stream()), "ghd_commit_path_q4")
+    st = (_lib or lib()).ghd_commit_path_q4(cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, _dev(res, torch.int32).data_ptr(),
+                                            M, kv_len, _stream())
+    if st:
+        _check(st, "ghd_commit_path_q4")
 
 
 def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] = None,
@@ -659,10 +667,15 @@ def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] 
     """What rows row0 .. row0 + rows - 1 of all layers stand for: fp16 [L, rows, nkv, d], keys and values."""
     shape = (cache.L, rows, cache.nkv, cache.d)
     if k is None:
-        k = torch.empty(shape, dtype=torch.float16, device=cache.k.device)
+        k = torch.empty(shape, dtype=torch.float16, device=cache.device)
+    else:
+        assert _dev(k, torch.float16).shape == shape, k.shape
     if v is None:
-        v = torch.empty(shape, dtype=torch.float16, device=cache.k.device)
-    assert k.shape == shape and v.shape == shape
-    _check(lib().ghd_kv_read_q4(_ptr(_dev(k, torch.float16)), _ptr(_dev(v, torch.float16)), cache.kv, cache.L, cache.nkv,
-                                cache.d, cache.capacity, row0, rows, _stream()), "ghd_kv_read_q4")
+        v = torch.empty(shape, dtype=torch.float16, device=cache.device)
+    else:
+        assert _dev(v, torch.float16).shape == shape, v.shape
+    st = (_lib or lib()).ghd_kv_read_q4(k.data_ptr(), v.data_ptr(), cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, row0, rows,
+                                        _stream())
+    if st:
+        _check(st, "ghd_kv_read_q4")
     return k, v
