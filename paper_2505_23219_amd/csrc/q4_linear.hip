@@ -202,7 +202,8 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST,
 // Four groups of wavefronts have RW tiles each; four shares of every group take the units of the workgroup's k range in turn, x
 // and weights of the next four requested while four are worked on, one barrier every four; the shares' sums meet in LDS.  (Two
 // shares of twice the registers, operands read ahead: [22016, 4096] at 64 rows 24.4 us, 21.8 with four; a finer ring, half
-// a unit a barrier: 25.8; two shares with three turns under way instead of one: 23.2 and 22.3.)
+// a unit a barrier: 25.8; two shares with three turns under way instead of one: 23.2 and 22.3; weights requested a whole turn ahead
+// instead of half of one 21.7 and 22.5, but with groups of 32 and 64 more registers than there are.)
 // Bound: [32000, 5120] at 128 rows, 58 us with all weights from HBM, would take 27 with neither weights nor x to fetch, 33 with x
 // alone, 50 with weights alone: their way into a compute unit, at 2 TB/s of the card's 4.75, with more of them under way no faster.
 // [4096, 11008] at 64 rows: 10 us, 4 of them before the first and behind the last product, and a launch that adds up.
