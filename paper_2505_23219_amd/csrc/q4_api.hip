@@ -208,4 +208,8 @@ ghd_status ghd_kv_read_q4(void* k_out, void* v_out, const ghd_kv* kv_host, int L
     return launch_q4_read(k, v, L, nkv, d, capacity, row0, rows, (half_t*)k_out, (half_t*)v_out, (hipStream_t)stream);
 }
 
+/* Test support (not part of the documented ABI): the host's rules and the kernels' arithmetic. */
+/* out2 = {bytes from the beginning of x to the end of the last that a call reads, numbers of x that it reads}. */
+void ghd_debug_q4_x(int M, int N, int K, int ldx, int64_t* out2) { q4_x_on_host(M, N, K, ldx, out2); }
+
 }  // extern "C"

@@ -68,6 +68,14 @@ __device__ __forceinline__ int q4_turn(int x, int n)
     return __builtin_amdgcn_readfirstlane(at - q4_over(at, q4_inverse(n)) * n);
 }
 
+// x comes through a buffer resource of as many bytes as lie between its first and behind its last number, and a request for what lies
+// behind is dropped.  Of the two offsets that a request has the check counts the lane's and may leave out the scalar one, so all
+// of where a request goes is in the lane's: one addition for each (16 rows of [22016, 4096] 12.1 and 12.2 us).  A lane takes 16 bytes of 8 rows by 64 columns, which begin
+// `first` bytes behind the first row's.
+__host__ __device__ __forceinline__ int q4_x_bytes(int M, int K, int ldx) { return ((M - 1) * ldx + K) * 2; }
+__host__ __device__ __forceinline__ int q4_x_lane(int lane, int ldx) { return (lane >> 3) * ldx * 2 + ((lane & 7) ^ (lane >> 3)) * 16; }
+__host__ __device__ __forceinline__ int q4_x_first(int row, int col, int ldx) { return row * (ldx * 2) + col * 2; }
+
 template <int MT, int R, int G>
 __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST, Q4Linear a)
 {
@@ -83,10 +91,9 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST,
     const int split = item & (c.splits - 1), tile0 = (item >> c.log_splits) * R;
     const int u0 = c.nunits * split >> c.log_splits, n = (c.nunits * (split + 1) >> c.log_splits) - u0;
     const int turn = q4_turn(q8 >> c.log_groups, n), mine = (n - wave + kQ4LinWaves - 1) / kQ4LinWaves;     // this wavefront's units
-    // x through a buffer resource: what lies behind its last row is not read
-    const __amdgpu_buffer_rsrc_t xbuf = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)mrow0 * a.ldx), 0,
-                                                                          (int)(((M - 1) * a.ldx + a.K) * 2), 0x00027000);
-    const int row8 = 8 * (int)a.ldx * 2, xlane = (lane >> 3) * (int)a.ldx * 2 + ((lane & 7) ^ (lane >> 3)) * 16;
+    const __amdgpu_buffer_rsrc_t xbuf =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)mrow0 * a.ldx), 0, q4_x_bytes(M, a.K, (int)a.ldx), 0x00027000);
+    const int xlane = q4_x_lane(lane, (int)a.ldx);
     const int tile_bytes = c.nunits * kUnitBytes;
     GLOBAL const char* wbase = gp(a.W + (size_t)tile0 * tile_bytes);
     const int last = min(R, c.ntiles - tile0) - 1;                 // (tiles that are not there: the last one again)
@@ -99,8 +106,8 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST,
         const uint32_t to = lds0 + (wave * 2 + (j & 1)) * kHalf;
 #pragma unroll
         for (int m = 0; m < 2 * MT; ++m)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (LdsPtr)(uintptr_t)(to + m * 1024), 16, xlane,
-                                                     m * row8 + u * (kQ4Unit * 2) + (j & 1) * 128, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (LdsPtr)(uintptr_t)(to + m * 1024), 16,
+                                                     xlane + q4_x_first(8 * m, u * kQ4Unit + (j & 1) * 64, (int)a.ldx), 0, 0, 0);
         pin_order();
     };
     struct {
@@ -229,11 +236,10 @@ __global__ __launch_bounds__(kQ4RowThreads) void k_q4_linear_shared(Q4_LINEAR_FI
     const int turn = q4_turn(q8 >> c.log_groups, n);
     // the turn of four with the unit that K does not fill
     const int short_turn = a.K % kQ4Unit != 0 && u0 + n == c.nunits ? (turn == n - 1 ? 0 : n - 1 - turn) / KH : -1;
-    // x through a buffer resource: what lies behind its last row is not read.  A wavefront requests 8 rows (the first or last
-    // of 16: grp / 2) by 64 columns (grp % 2) of every row tile of its share's unit.
+    // A wavefront requests 8 rows (the first or last of 16: grp / 2) by 64 columns (grp % 2) of every row tile of its share's unit.
     const __amdgpu_buffer_rsrc_t xbuf =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)mrow0 * a.ldx), 0, (int)(((M - 1) * a.ldx + a.K) * 2), 0x00027000);
-    const int xlane = (grp / 2 * 8 + (lane >> 3)) * (int)a.ldx * 2 + grp % 2 * 128 + ((lane & 7) ^ (lane >> 3)) * 16, xtile = 16 * (int)a.ldx * 2;
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)mrow0 * a.ldx), 0, q4_x_bytes(M, a.K, (int)a.ldx), 0x00027000);
+    const int xlane = q4_x_lane(lane, (int)a.ldx) + q4_x_first(grp / 2 * 8, grp % 2 * 64, (int)a.ldx);
     GLOBAL const char* wtile[RW];
 #pragma unroll
     for (int t = 0; t < RW; ++t) wtile[t] = gp(a.W + (size_t)min(tile0 + t, c.ntiles - 1) * c.nunits * kUnitBytes);
@@ -251,7 +257,7 @@ __global__ __launch_bounds__(kQ4RowThreads) void k_q4_linear_shared(Q4_LINEAR_FI
 #pragma unroll
         for (int m = from; m < to; ++m)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (LdsPtr)(uintptr_t)(lds0 + ((i & 1) * KH + share) * kBuf + (m * 4 + grp) * 1024),
-                                                     16, xlane, m * xtile + u * (kQ4Unit * 2), 0, 0);
+                                                     16, xlane + q4_x_first(m * 16, u * kQ4Unit, (int)a.ldx), 0, 0, 0);
         pin_order();
     };
     auto request_w = [&](int i, int slot) {
@@ -523,6 +529,26 @@ ghd_status launch_q4_linear(Q4Linear a, void* ws, size_t ws_bytes, hipStream_t s
     case 2: return q4_linear_tiles<2>(a, c, st);
     case 3: return q4_linear_tiles<3>(a, c, st);
     default: return q4_linear_tiles<4>(a, c, st);
+    }
+}
+
+// Which bytes behind x the requests of a call that the hardware lets through end at most, and how many numbers of x they bring.
+void q4_x_on_host(int M, int N, int K, int ldx, int64_t* out2)
+{
+    const Q4Cut c = q4_cut(M, N, K);
+    out2[0] = out2[1] = 0;
+    for (int mrow0 = 0; mrow0 < M; mrow0 += c.mt * 16) {
+        const int rows = std::min(M - mrow0, c.mt * 16), bytes = q4_x_bytes(rows, K, ldx);
+        for (int u = 0; u < ceil_div(K, kQ4Unit); ++u)
+            for (int half = 0; half < 2; ++half)
+                for (int row = 0; row < c.mt * 16; row += 8)
+                    for (int lane = 0; lane < 64; ++lane) {
+                        const int at = q4_x_lane(lane, ldx) + q4_x_first(row, u * kQ4Unit + half * 64, ldx);
+                        if (at >= bytes) continue;
+                        out2[0] = std::max<int64_t>(out2[0], (int64_t)mrow0 * ldx * 2 + at + 16);
+                        const int col = u * kQ4Unit + half * 64 + ((lane & 7) ^ (lane >> 3)) * 8;
+                        if (row + (lane >> 3) < rows && col < K) out2[1] += 8;
+                    }
     }
 }
 
