@@ -435,7 +435,8 @@ ghd_status ghd_pack_weight_q4(void *dst, const void *codes, const void *scales, 
 /* y = x W^T as ghd_linear_skinny, with Wq from ghd_pack_weight_q4: x fp16 [M, ldx],
  * y float or fp16 (flags) [M, ldy].  Products and sums in 32 bits, scales applied to
  * sums of x times whole numbers: nothing is rounded to fewer bits before y.  ldx % 8 == 0,
- * ldx <= 2^23; x, y and Wq 16-byte aligned.  y must not meet x or Wq in memory. */
+ * ldx <= 2^23; x, y and Wq 16-byte aligned.  y must not meet x or Wq in memory.
+ * The workspace's size does not fall with M: one for the widest tree does for all. */
 ghd_status ghd_linear_q4(void *y, const void *x, const void *Wq, int M, int N, int K, int group,
                          int64_t ldx, int64_t ldy, uint32_t flags, void *ws, size_t ws_bytes,
                          void *stream);
@@ -459,7 +460,9 @@ ghd_status ghd_kv_append_q4(const ghd_kv *kv, const void *k, const void *v, cons
 
 /* ghd_tree_attention and ghd_masked_attention over a 4-bit cache whose rows
  * [0, kv_len + M) are there: q, out fp16 [M, nh, d].  An infinity or NaN in a row
- * reaches the tokens that see the row and no others. */
+ * reaches the tokens that see the row and no others.  The workspace's size falls
+ * neither with M nor with kv_len: one for the widest tree over the longest context
+ * does for every step of a loop. */
 ghd_status ghd_tree_attention_q4(void *out, const void *q, const ghd_kv *kv,
                                  const int32_t *parent_dev, int M, int kv_len, int nh, int nkv, int d,
                                  int capacity, float scale, void *ws, size_t ws_bytes, void *stream);

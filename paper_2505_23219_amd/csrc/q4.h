@@ -126,6 +126,7 @@ struct Q4Attn {
     float inv_rep;
 };
 size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d);
+void q4_attention_on_host(int M, int kv_len, int nh, int nkv, int d, int64_t* out4);
 ghd_status launch_q4_attention(Q4Attn a, int d, void* ws, size_t ws_bytes, hipStream_t st);     // GHD_ERR_WORKSPACE: too small
 
 struct Q4Linear {

@@ -212,4 +212,10 @@ ghd_status ghd_kv_read_q4(void* k_out, void* v_out, const ghd_kv* kv_host, int L
 /* out2 = {bytes from the beginning of x to the end of the last that a call reads, numbers of x that it reads}. */
 void ghd_debug_q4_x(int M, int N, int K, int ldx, int64_t* out2) { q4_x_on_host(M, N, K, ldx, out2); }
 
+/* out4 = {tiles of 16 rows in a block, blocks of a key head, parts of its keys, bytes of workspace} of an attention call. */
+void ghd_debug_q4_attention(int M, int kv_len, int nh, int nkv, int d, int64_t* out4)
+{
+    q4_attention_on_host(M, kv_len, nh, nkv, d, out4);
+}
+
 }  // extern "C"

@@ -687,16 +687,30 @@ static Q4AttnCut q4_attn_cut(int M, int kv_len, int nh, int nkv, int d)
 
 static size_t q4_attn_units(const Q4AttnCut& c, int nkv) { return (size_t)nkv * c.blocks * c.splits * c.rows; }
 
-static size_t q4_attn_bytes(const Q4AttnCut& c, int nkv, int d)
-{
-    if (c.splits == 1) return 256;
-    const size_t units = q4_attn_units(c, nkv);
-    return align_up(units * 16 * d * 4, 256) + align_up(units * 128, 256);
-}
+static size_t q4_units_bytes(size_t units, int d) { return align_up(units * 16 * d * 4, 256) + align_up(units * 128, 256); }
 
+static size_t q4_attn_bytes(const Q4AttnCut& c, int nkv, int d) { return c.splits == 1 ? 256 : q4_units_bytes(q4_attn_units(c, nkv), d); }
+
+// The most that a call of up to M tokens over up to kv_len rows takes, whatever its cut: what a caller makes once for its widest tree
+// and longest context does for every step on the way there.
 size_t q4_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
 {
-    return q4_attn_bytes(q4_attn_cut(M, kv_len, nh, nkv, d), nkv, d);
+    const int rep = nh / nkv, ntiles = ceil_div(kv_len + M, kQ4Tile), rt = ceil_div(M * rep, 16);
+    size_t units = 0;
+    if (rep <= 16 && q4_key_splits(ntiles, nkv) > 1) units = (size_t)nkv * q4_key_splits(ntiles, nkv);
+    // blocks of 2 to 4 tiles: at most 256 workgroups where there are parts, a part has a tile, and blocks end up to a tile behind the rows
+    if (rt > 1 && ntiles > 1 && nkv <= 128)
+        units = std::max(units, (size_t)std::min<int64_t>(256 * 4, (int64_t)nkv * (rt + (rt + 1) / 2 - 1) * ntiles));
+    return units ? q4_units_bytes(units, d) : 256;
+}
+
+void q4_attention_on_host(int M, int kv_len, int nh, int nkv, int d, int64_t* out4)
+{
+    const Q4AttnCut c = q4_attn_cut(M, kv_len, nh, nkv, d);
+    out4[0] = c.rows;
+    out4[1] = c.blocks;
+    out4[2] = c.splits;
+    out4[3] = q4_attn_bytes(c, nkv, d);
 }
 
 template <int D, int RT>

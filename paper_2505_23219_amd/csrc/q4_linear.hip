@@ -459,7 +459,13 @@ static size_t q4_cut_bytes(const Q4Cut& c, int M, int N)
     return c.splits == 1 ? 256 : align_up((size_t)c.splits * ceil_div(N, 16) * q4_row_groups(M, c.mt) * c.mt * 1024, 256);
 }
 
-size_t q4_linear_bytes(int M, int N, int K) { return q4_cut_bytes(q4_cut(M, N, K), M, N); }
+// The most that a call of up to M rows takes, whatever its cut.
+size_t q4_linear_bytes(int M, int N, int K)
+{
+    size_t most = 0;
+    for (int m = std::min(M, 16); m <= M; m = m < M ? std::min(m + 16, M) : m + 1) most = std::max(most, q4_cut_bytes(q4_cut(m, N, K), m, N));
+    return most;
+}
 
 static ghd_status q4_linear_start(const Q4Linear& a, const Q4Cut& c,
                                   void (*kernel)(const char*, const half_t*, float*, void*, int, uint32_t, int, int, Q4Linear), int threads,
