@@ -435,8 +435,9 @@ ghd_status ghd_pack_weight_q4(void *dst, const void *codes, const void *scales, 
 /* y = x W^T as ghd_linear_skinny, with Wq from ghd_pack_weight_q4: x fp16 [M, ldx],
  * y float or fp16 (flags) [M, ldy].  Products and sums in 32 bits, scales applied to
  * sums of x times whole numbers: nothing is rounded to fewer bits before y.  ldx % 8 == 0,
- * ldx <= 2^23; x, y and Wq 16-byte aligned.  y must not meet x or Wq in memory.
- * The workspace's size does not fall with M: one for the widest tree does for all. */
+ * ldx <= 2^23; x, y and Wq 16-byte aligned.
+ * A y that meets x or Wq in memory is refused (GHD_ERR_SHAPE); its rows may lie between
+ * those of x.  The workspace's size does not fall with M: one for the widest tree does for all. */
 ghd_status ghd_linear_q4(void *y, const void *x, const void *Wq, int M, int N, int K, int group,
                          int64_t ldx, int64_t ldy, uint32_t flags, void *ws, size_t ws_bytes,
                          void *stream);

@@ -139,6 +139,7 @@ struct Q4Linear {
     bool out16;
 };
 size_t q4_linear_bytes(int M, int N, int K);
+bool q4_linear_meets(const Q4Linear& a);
 void q4_x_on_host(int M, int N, int K, int ldx, int64_t* out2);
 ghd_status launch_q4_linear(Q4Linear a, void* ws, size_t ws_bytes, hipStream_t st);              // the same
 ghd_status launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int N, int K, int group,

@@ -28,6 +28,22 @@ static bool weight_shape_ok(int N, int K, int group)
     return group == 32 || group == 64 || group == 128;
 }
 
+static Q4Linear linear_args(void* y, const void* x, const void* Wq, int M, int N, int K, int group, int64_t ldx, int64_t ldy, uint32_t flags)
+{
+    Q4Linear a = {};
+    a.y = y;
+    a.x = (const half_t*)x;
+    a.W = (const char*)Wq;
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.group = group;
+    a.ldx = ldx;
+    a.ldy = ldy;
+    a.out16 = flags == GHD_OUT_F16;
+    return a;
+}
+
 static ghd_status attention_q4(void* out, const void* q, const ghd_kv* kv, const int32_t* parent, const uint64_t* mask, int M,
                                int kv_len, int nh, int nkv, int d, int cap, float scale, void* ws, size_t ws_bytes,
                                void* stream)
@@ -91,17 +107,7 @@ ghd_status ghd_linear_q4(void* y, const void* x, const void* Wq, int M, int N, i
     if (!aligned_to(x, 16) || !aligned_to(Wq, 16) || !aligned_to(y, 16) || ldx % 8 != 0) return GHD_ERR_ALIGN;
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!aligned_to(ws, 16)) return GHD_ERR_ALIGN;
-    Q4Linear a = {};
-    a.y = y;
-    a.x = (const half_t*)x;
-    a.W = (const char*)Wq;
-    a.M = M;
-    a.N = N;
-    a.K = K;
-    a.group = group;
-    a.ldx = ldx;
-    a.ldy = ldy;
-    a.out16 = flags == GHD_OUT_F16;
+    const Q4Linear a = linear_args(y, x, Wq, M, N, K, group, ldx, ldy, flags);
     return launch_q4_linear(a, ws, ws_bytes, (hipStream_t)stream);
 }
 
@@ -216,6 +222,12 @@ void ghd_debug_q4_x(int M, int N, int K, int ldx, int64_t* out2) { q4_x_on_host(
 void ghd_debug_q4_attention(int M, int kv_len, int nh, int nkv, int d, int64_t* out4)
 {
     q4_attention_on_host(M, kv_len, nh, nkv, d, out4);
+}
+
+/* Would y of a linear call meet x or Wq? */
+int ghd_debug_q4_linear_meets(void* y, const void* x, const void* Wq, int M, int N, int K, int group, int64_t ldx, int64_t ldy, uint32_t flags)
+{
+    return q4_linear_meets(linear_args(y, x, Wq, M, N, K, group, ldx, ldy, flags));
 }
 
 }  // extern "C"

@@ -525,10 +525,35 @@ static ghd_status q4_linear_tiles(const Q4Linear& a, const Q4Cut& c, hipStream_t
     return q4_linear_group<MT, 2>(a, c, st);
 }
 
+// Do rows of a and of b share a byte?  (Rows of one may lie between those of the other: halves of one wide buffer.)
+struct Q4Rows {
+    uintptr_t at;
+    int64_t step, bytes;
+    int n;
+};
+static bool q4_meet(Q4Rows a, Q4Rows b)
+{
+    while (a.n > 0 && b.n > 0) {
+        if (a.at + a.bytes <= b.at) a.at += a.step, --a.n;
+        else if (b.at + b.bytes <= a.at) b.at += b.step, --b.n;
+        else return true;
+    }
+    return false;
+}
+
+// Workgroups that are done write y while others still read x and W.
+bool q4_linear_meets(const Q4Linear& a)
+{
+    const int size = a.out16 ? 2 : 4;
+    const Q4Rows y = {(uintptr_t)a.y, a.ldy * size, (int64_t)a.N * size, a.M};
+    return q4_meet(y, {(uintptr_t)a.x, a.ldx * 2, a.K * 2, a.M}) || q4_meet(y, {(uintptr_t)a.W, 0, (int64_t)q4_weight_bytes(a.N, a.K, a.group), 1});
+}
+
 ghd_status launch_q4_linear(Q4Linear a, void* ws, size_t ws_bytes, hipStream_t st)
 {
     const Q4Cut c = q4_cut(a.M, a.N, a.K);
     if (ws_bytes < q4_cut_bytes(c, a.M, a.N)) return GHD_ERR_WORKSPACE;
+    if (q4_linear_meets(a)) return GHD_ERR_SHAPE;
     a.part = (float*)ws;
     switch (c.mt) {
     case 1: return q4_linear_tiles<1>(a, c, st);
