@@ -555,9 +555,9 @@ def ghd_linear_q4(x: torch.Tensor, Wq: torch.Tensor, N: int, group: int, out_dty
     assert x.is_cuda and x.dtype is torch.float16 and one == 1, (x.device, x.dtype, x.stride())
     assert y.is_cuda and y.shape == (M, N) and also == 1 and (half or y.dtype is torch.float32), (y.shape, y.dtype)
     assert Wq.is_cuda and Wq.dtype is torch.uint8 and Wq.is_contiguous()
-    st = L.ghd_linear_q4(y.data_ptr(), x.data_ptr(), Wq.data_ptr(), M, N, K, group, ldx if M > 1 else max(ldx, K),
-                         ldy if M > 1 else max(ldy, N), GHD_OUT_F16 if half else GHD_OUT_F32, ws.data_ptr(), ws.numel(),
-                         _stream())
+    # (one row has no next one: its stride may be anything)
+    st = L.ghd_linear_q4(y.data_ptr(), x.data_ptr(), Wq.data_ptr(), M, N, K, group, ldx if M > 1 else K, ldy if M > 1 else N,
+                         GHD_OUT_F16 if half else GHD_OUT_F32, ws.data_ptr(), ws.numel(), _stream())
     if st:
         _check(st, "ghd_linear_q4")
     return y
