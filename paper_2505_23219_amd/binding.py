@@ -519,6 +519,25 @@ def ghd_spec_step(spec: SpecState, parent: torch.Tensor, rank: torch.Tensor, kv_
 
 
 # ---- weights and cache in 4 bits ------------------------------------------------
+# (Checks that stay under python -O: behind them a pointer goes to the GPU.)
+def _misfit(name: str, t: torch.Tensor, want: str) -> ValueError:
+    return ValueError("%s must be %s, not %s %s with strides %s on %s"
+                      % (name, want, str(t.dtype).replace("torch.", ""), tuple(t.shape), t.stride(), t.device))
+
+
+def _whole(name: str, t: torch.Tensor, dtype) -> int:
+    """Where a contiguous tensor of dtype on the GPU lies."""
+    if not (t.is_cuda and t.dtype is dtype and t.is_contiguous()):
+        raise _misfit(name, t, "a contiguous %s tensor on the GPU" % str(dtype).replace("torch.", ""))
+    return t.data_ptr()
+
+
+def _scratch(ws: torch.Tensor) -> int:
+    if not (ws.is_cuda and ws.is_contiguous()):
+        raise _misfit("ws", ws, "a contiguous tensor on the GPU")
+    return ws.data_ptr()
+
+
 def ghd_pack_weight_q4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], group: int
                        ) -> torch.Tensor:
     """codes uint8 [N, K / 2] (even column in the low four bits), scales fp16 [N, ceil(K / group)],
@@ -528,8 +547,8 @@ def ghd_pack_weight_q4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optiona
     if tuple(scales.shape) != shape or (zeros is not None and tuple(zeros.shape) != shape):
         raise ValueError("scales and zeros must be %s" % (shape,))
     out = torch.empty(lib().ghd_weight_q4_bytes(N, K, group), dtype=torch.uint8, device=codes.device)
-    _check(lib().ghd_pack_weight_q4(_ptr(out), _ptr(_dev(codes, torch.uint8)), _ptr(_dev(scales, torch.float16)),
-                                    None if zeros is None else _ptr(_dev(zeros, torch.uint8)), N, K, group,
+    _check(lib().ghd_pack_weight_q4(_ptr(out), _whole("codes", codes, torch.uint8), _whole("scales", scales, torch.float16),
+                                    None if zeros is None else _whole("zeros", zeros, torch.uint8), N, K, group,
                                     _stream()), "ghd_pack_weight_q4")
     return out
 
@@ -552,12 +571,13 @@ def ghd_linear_q4(x: torch.Tensor, Wq: torch.Tensor, N: int, group: int, out_dty
     ldx, one = x.stride()
     ldy, also = y.stride()
     half = y.dtype is torch.float16
-    assert x.is_cuda and x.dtype is torch.float16 and one == 1, (x.device, x.dtype, x.stride())
-    assert y.is_cuda and y.shape == (M, N) and also == 1 and (half or y.dtype is torch.float32), (y.shape, y.dtype)
-    assert Wq.is_cuda and Wq.dtype is torch.uint8 and Wq.is_contiguous()
+    if not (x.is_cuda and x.dtype is torch.float16 and one == 1):
+        raise _misfit("x", x, "float16 on the GPU, the numbers of a row side by side")
+    if not (y.is_cuda and y.shape == (M, N) and also == 1 and (half or y.dtype is torch.float32)):
+        raise _misfit("y", y, "float16 or float32 (%d, %d) on the GPU, the numbers of a row side by side" % (M, N))
     # (one row has no next one: its stride may be anything)
-    st = L.ghd_linear_q4(y.data_ptr(), x.data_ptr(), Wq.data_ptr(), M, N, K, group, ldx if M > 1 else K, ldy if M > 1 else N,
-                         GHD_OUT_F16 if half else GHD_OUT_F32, ws.data_ptr(), ws.numel(), _stream())
+    st = L.ghd_linear_q4(y.data_ptr(), x.data_ptr(), _whole("Wq", Wq, torch.uint8), M, N, K, group, ldx if M > 1 else K,
+                         ldy if M > 1 else N, GHD_OUT_F16 if half else GHD_OUT_F32, _scratch(ws), ws.nbytes, _stream())
     if st:
         _check(st, "ghd_linear_q4")
     return y
@@ -571,6 +591,8 @@ class KvQ4:
         if n == 0:
             raise ValueError("no 4-bit cache of %d heads of %d channels by %d rows" % (nkv, d, capacity))
         self.L, self.nkv, self.d, self.capacity = L, nkv, d, capacity
+        if torch.device(device).type != "cuda":
+            raise ValueError("a 4-bit cache lies on the GPU, not on %s" % device)
         self.k = torch.zeros((L, n), dtype=torch.uint8, device=device)
         self.v = torch.zeros((L, n), dtype=torch.uint8, device=device)
         self.kv = (KV * L)(*[KV(self.k[i].data_ptr(), self.v[i].data_ptr()) for i in range(L)])
@@ -581,12 +603,20 @@ class KvQ4:
         return self.k.device
 
 
-def _row_step(t: torch.Tensor, M: int, heads: int, d: int) -> int:
+def _row_step(name: str, t: torch.Tensor, M: int, heads: int, d: int) -> int:
     """How far the rows of a [M, heads, d] tensor whose heads lie side by side are apart."""
+    if not (t.is_cuda and t.dtype is torch.float16 and t.shape == (M, heads, d)):
+        raise _misfit(name, t, "float16 (%d, %d, %d) on the GPU" % (M, heads, d))
     step, head, one = t.stride()
-    assert t.is_cuda and t.dtype is torch.float16 and t.shape == (M, heads, d), (t.device, t.dtype, t.shape)
-    assert one == 1 and (heads == 1 or head == d), t.stride()
+    if one != 1 or (heads != 1 and head != d):
+        raise _misfit(name, t, "rows whose heads lie side by side")
     return step if M > 1 else heads * d
+
+
+def _parents(parent: torch.Tensor, M: int) -> int:
+    if parent.numel() != M:
+        raise _misfit("parent", parent, "one for each of %d tokens" % M)
+    return _whole("parent", parent, torch.int32)
 
 
 def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, kv_len: int,
@@ -596,19 +626,18 @@ def ghd_kv_append_q4(cache: KvQ4, layer: int, k: torch.Tensor, v: torch.Tensor, 
     turned where rope_base > 0: at kv_len + depth of parent, or at kv_len + i.  q fp16 [M, nh, d] is
     turned likewise and returned."""
     M, nkv, d = k.shape[0], cache.nkv, cache.d
-    ld_k, ld_v = _row_step(k, M, nkv, d), _row_step(v, M, nkv, d)
+    ld_k, ld_v = _row_step("k", k, M, nkv, d), _row_step("v", v, M, nkv, d)
     nh, ld_q, ld_qo, q_ptr, qo_ptr, tree = 0, 0, 0, None, None, None
     if q is not None:
         nh = q.shape[1]
-        ld_q = _row_step(q, M, nh, d)
+        ld_q = _row_step("q", q, M, nh, d)
         if q_out is None:
             q_out, ld_qo = torch.empty((M, nh, d), dtype=torch.float16, device=cache.device), nh * d
         else:
-            ld_qo = _row_step(q_out, M, nh, d)
+            ld_qo = _row_step("q_out", q_out, M, nh, d)
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     if parent is not None:
-        assert parent.numel() == M
-        tree = _dev(parent, torch.int32).data_ptr()
+        tree = _parents(parent, M)
     st = (_lib or lib()).ghd_kv_append_q4(cache.layers[layer], k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, tree, M, kv_len, nh,
                                           nkv, d, cache.capacity, ld_k, ld_v, ld_q, ld_qo, rope_base, _stream())
     if st:
@@ -622,15 +651,17 @@ def ghd_attention_q4_workspace_bytes(M: int, kv_len: int, nh: int, nkv: int, d: 
 
 def _attention_q4(fn, name, q, cache, layer, relation, kv_len, scale, ws, out):
     M, nh, d = q.shape
-    assert q.is_cuda and q.dtype is torch.float16 and q.is_contiguous() and d == cache.d, (q.device, q.dtype, q.shape)
+    if d != cache.d:
+        raise _misfit("q", q, "of heads of %d channels" % cache.d)
+    q_ptr = _whole("q", q, torch.float16)
     if out is None:
         out = torch.empty_like(q)
-    else:
-        assert out.is_cuda and out.dtype is torch.float16 and out.is_contiguous() and out.shape == q.shape, (out.dtype, out.shape)
+    elif out.shape != q.shape:
+        raise _misfit("out", out, "of q's shape %s" % (tuple(q.shape),))
     if ws is None:
         ws = workspace(_lib.ghd_attention_q4_workspace_bytes(M, kv_len, nh, cache.nkv, d), q.device)
-    st = fn(out.data_ptr(), q.data_ptr(), cache.layers[layer], relation.data_ptr(), M, kv_len, nh, cache.nkv, d, cache.capacity,
-            d ** -0.5 if scale is None else scale, ws.data_ptr(), ws.numel(), _stream())
+    st = fn(_whole("out", out, torch.float16), q_ptr, cache.layers[layer], relation, M, kv_len, nh, cache.nkv, d, cache.capacity,
+            d ** -0.5 if scale is None else scale, _scratch(ws), ws.nbytes, _stream())
     if st:
         _check(st, name)
     return out
@@ -640,8 +671,7 @@ def ghd_tree_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, parent: torc
                           scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q fp16 [M, nh, d] over the rows [0, kv_len + M) of a layer; returns fp16 [M, nh, d]."""
-    assert parent.numel() == q.shape[0]
-    return _attention_q4(lib().ghd_tree_attention_q4, "ghd_tree_attention_q4", q, cache, layer, _dev(parent, torch.int32), kv_len,
+    return _attention_q4(lib().ghd_tree_attention_q4, "ghd_tree_attention_q4", q, cache, layer, _parents(parent, q.shape[0]), kv_len,
                          scale, ws, out)
 
 
@@ -649,14 +679,15 @@ def ghd_masked_attention_q4(q: torch.Tensor, cache: KvQ4, layer: int, mask: torc
                             scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """As ghd_tree_attention_q4 with the relation as int64 [M, 2] bit masks (ghd_masked_attention)."""
-    assert mask.shape == (q.shape[0], 2)
-    return _attention_q4(lib().ghd_masked_attention_q4, "ghd_masked_attention_q4", q, cache, layer, _dev(mask, torch.int64), kv_len,
-                         scale, ws, out)
+    if mask.shape != (q.shape[0], 2):
+        raise _misfit("mask", mask, "(%d, 2)" % q.shape[0])
+    return _attention_q4(lib().ghd_masked_attention_q4, "ghd_masked_attention_q4", q, cache, layer, _whole("mask", mask, torch.int64),
+                         kv_len, scale, ws, out)
 
 
 def ghd_commit_path_q4(cache: KvQ4, res: torch.Tensor, M: int, kv_len: int) -> None:
     """ghd_commit_path for all layers of a 4-bit cache."""
-    st = (_lib or lib()).ghd_commit_path_q4(cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, _dev(res, torch.int32).data_ptr(),
+    st = (_lib or lib()).ghd_commit_path_q4(cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, _whole("res", res, torch.int32),
                                             M, kv_len, _stream())
     if st:
         _check(st, "ghd_commit_path_q4")
@@ -668,14 +699,14 @@ def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] 
     shape = (cache.L, rows, cache.nkv, cache.d)
     if k is None:
         k = torch.empty(shape, dtype=torch.float16, device=cache.device)
-    else:
-        assert _dev(k, torch.float16).shape == shape, k.shape
+    elif k.shape != shape:
+        raise _misfit("k", k, str(shape))
     if v is None:
         v = torch.empty(shape, dtype=torch.float16, device=cache.device)
-    else:
-        assert _dev(v, torch.float16).shape == shape, v.shape
-    st = (_lib or lib()).ghd_kv_read_q4(k.data_ptr(), v.data_ptr(), cache.kv, cache.L, cache.nkv, cache.d, cache.capacity, row0, rows,
-                                        _stream())
+    elif v.shape != shape:
+        raise _misfit("v", v, str(shape))
+    st = (_lib or lib()).ghd_kv_read_q4(_whole("k", k, torch.float16), _whole("v", v, torch.float16), cache.kv, cache.L, cache.nkv,
+                                        cache.d, cache.capacity, row0, rows, _stream())
     if st:
         _check(st, "ghd_kv_read_q4")
     return k, v
