@@ -112,6 +112,7 @@ ghd_status launch_q4_commit(void* const* k, void* const* v, int L, int nkv, int 
 ghd_status launch_q4_read(void* const* k, void* const* v, int L, int nkv, int d, int cap, int row0, int rows, half_t* ko,
                           half_t* vo, hipStream_t st);
 constexpr int kQ4MaxLayers = 48;
+constexpr int kQ4MostGroups = 1 << 23;           // workgroups of 256 in a launch, which has below 2^32 threads along an axis
 
 struct Q4Attn {
     half_t* out;

@@ -586,10 +586,10 @@ void q4_x_on_host(int M, int N, int K, int ldx, int64_t* out2)
 // ---- packing -----------------------------------------------------------------------------
 // One thread a word of codes; the first 16 of a unit's 256 also write a row's scales and zero points.
 __global__ __launch_bounds__(256) void k_q4_pack(char* dst, const uint8_t* codes, const half_t* scales, const uint8_t* zeros,
-                                                 int N, int K, int group, int nunits)
+                                                 int N, int K, int group, int nunits, int tile0)
 {
-    const int tile = blockIdx.x / nunits, unit = blockIdx.x % nunits, per = kQ4Unit / group, groups = (K + group - 1) / group;
-    char* at = dst + (size_t)blockIdx.x * q4_unit_bytes(group);
+    const int tile = tile0 + blockIdx.x / nunits, unit = blockIdx.x % nunits, per = kQ4Unit / group, groups = (K + group - 1) / group;
+    char* at = dst + ((size_t)tile * nunits + unit) * q4_unit_bytes(group);
     const int lane = threadIdx.x >> 2, s = threadIdx.x & 3, n = tile * 16 + (lane & 15);
     const int k = unit * kQ4Unit + 32 * s + 8 * (lane >> 4);
     uint32_t word = 0;
@@ -614,10 +614,14 @@ __global__ __launch_bounds__(256) void k_q4_pack(char* dst, const uint8_t* codes
 ghd_status launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int N, int K, int group,
                           hipStream_t st)
 {
-    const int nunits = ceil_div(K, kQ4Unit);
-    hipLaunchKernelGGL(k_q4_pack, dim3(ceil_div(N, 16) * nunits), dim3(256), 0, st, (char*)dst, (const uint8_t*)codes,
-                       (const half_t*)scales, (const uint8_t*)zeros, N, K, group, nunits);
-    return check_launch();
+    const int nunits = ceil_div(K, kQ4Unit), ntiles = ceil_div(N, 16), most = kQ4MostGroups / nunits;
+    for (int tile0 = 0; tile0 < ntiles; tile0 += most) {
+        hipLaunchKernelGGL(k_q4_pack, dim3(std::min(most, ntiles - tile0) * nunits), dim3(256), 0, st, (char*)dst, (const uint8_t*)codes,
+                           (const half_t*)scales, (const uint8_t*)zeros, N, K, group, nunits, tile0);
+        const ghd_status s = check_launch();
+        if (s) return s;
+    }
+    return GHD_OK;
 }
 
 }  // namespace ghd
