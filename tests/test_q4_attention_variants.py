@@ -15,7 +15,7 @@ from paper_2505_23219_amd import binding as B
 import q4_plain as P
 
 # M, nh, nkv, kv_len
-CASES = [(1, 1, 1, 0), (1, 1, 1, 300), (3, 4, 1, 150), (1, 8, 2, 700), (1, 2, 2, 16384), (5, 6, 3, 16391), (1, 6, 6, 12000),
+CASES = [(1, 1, 1, 0), (1, 1, 1, 300), (3, 4, 1, 150), (1, 8, 2, 700), (2, 3, 1, 1000), (1, 2, 2, 16384), (5, 6, 3, 16391), (1, 6, 6, 12000),
          (1, 40, 40, 16384),
          (8, 5, 1, 0), (17, 1, 1, 300), (33, 1, 1, 300), (17, 32, 32, 700), (65, 12, 12, 700), (17, 1, 1, 1000), (33, 2, 2, 16384),
          (37, 20, 4, 777), (37, 40, 40, 1500), (17, 32, 32, 4096),
