@@ -67,3 +67,36 @@ def test_reading_back_more_than_one_launch():
     for t, w in zip(out, want):
         for layer in (0, 23, 46, 47):
             assert torch.equal(t[layer], w), layer
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_heads_beyond_4_gib(d):
+    """The last head's rows begin above 2^32 bytes."""
+    nkv, nh, cap, M, kv = 640 // d, 1280 // d, 1 << 24, 6, 50
+    _enough(20)
+    n = B.lib().ghd_kv_q4_bytes(nkv, cap, d)
+    assert n // nkv * (nkv - 1) > 1 << 32
+    rng = np.random.default_rng(d)
+    cache = B.KvQ4.__new__(B.KvQ4)
+    cache.L, cache.nkv, cache.d, cache.capacity = 1, nkv, d, cap
+    cache.k, cache.v = (torch.empty((1, n), dtype=torch.uint8, device="cuda") for _ in range(2))
+    cache.kv = (B.KV * 1)(B.KV(cache.k.data_ptr(), cache.v.data_ptr()))
+    cache.layers = [C.byref(cache.kv[0])]
+    k, v = (rng.standard_normal((kv + M, nkv, d)).astype(np.float16) for _ in range(2))
+    q = rng.standard_normal((M, nh, d)).astype(np.float16)
+    parent = np.arange(-1, M - 1, dtype=np.int32)
+    kt, vt, qt, pt = (torch.from_numpy(t).cuda() for t in (k, v, q, parent))
+    B.ghd_kv_append_q4(cache, 0, kt, vt, 0)
+    got = B.ghd_tree_attention_q4(qt, cache, 0, pt, kv).cpu().numpy().astype(np.float64)
+    want, tol = P.attention(q, P.held(k), P.held(v), P.sees_of_parent(parent), kv, 1 / math.sqrt(d))
+    assert (np.abs(got - want) <= tol).all()
+    # rows far behind in every head
+    at = cap - 40
+    B.ghd_kv_append_q4(cache, 0, kt[:40], vt[:40], at)
+    B.ghd_commit_path_q4(cache, torch.tensor([3, 0, 0, 11, 39], dtype=torch.int32, device="cuda"), 40, at)
+    order = [0, 11, 39] + list(range(3, 40))
+    for got, x in zip(B.ghd_kv_read_q4(cache, at, 40), (k, v)):
+        assert np.array_equal(got[0].cpu().numpy(), P.held(x[:40])[order])
+    # the first rows are as they were
+    for got, x in zip(B.ghd_kv_read_q4(cache, 0, kv + M), (k, v)):
+        assert np.array_equal(got[0].cpu().numpy(), P.held(x))
