@@ -144,8 +144,8 @@ __device__ __forceinline__ uint32_t q4_clean(half8& lo, half8& s, int key0, int 
     return bad;
 }
 
-// scores to powers of two; above 0, so that minus infinity, the score of a key that is not seen, stays that
-__device__ __forceinline__ float q4_power(float scale) { return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f); }
+// scores to powers of two; above 0, so that minus infinity, the score of a key that is not seen, stays that (a NaN stays one, too)
+__device__ __forceinline__ float q4_power(float scale) { return __builtin_elementwise_maximum(fabsf(scale) * 1.4426950408889634f, 1e-37f); }
 
 // A row tile's state over the keys so far.
 template <int D>
