@@ -409,7 +409,7 @@ size_t ghd_spec_workspace_bytes(const ghd_spec_model *m, int M, int kv_len);
  * ghd_linear_skinny, ghd_tree_attention / ghd_masked_attention and ghd_commit_path
  * in a step whose weights and cache are held that way.
  *
- * Weights: codes 0..15 with a scale (fp16) and a zero point (a whole number) for
+ * Weights: codes 0..15 with a scale (fp16) and a zero point (0..255) for
  * every `group` columns of a row, group in {32, 64, 128}; the last group of a
  * row may be short:  W[n, k] = (code[n, k] - zero[n, k / group]) * scale[n, k / group].
  *
@@ -437,7 +437,8 @@ ghd_status ghd_pack_weight_q4(void *dst, const void *codes, const void *scales, 
  * sums of x times whole numbers: nothing is rounded to fewer bits before y.  ldx % 8 == 0,
  * ldx <= 2^23; x, y and Wq 16-byte aligned.
  * A y that meets x or Wq in memory is refused (GHD_ERR_SHAPE); its rows may lie between
- * those of x.  The workspace's size does not fall with M: one for the widest tree does for all. */
+ * those of x.  The workspace's size does not fall with M: one for the widest tree does
+ * for all; other N and K have sizes of their own. */
 ghd_status ghd_linear_q4(void *y, const void *x, const void *Wq, int M, int N, int K, int group,
                          int64_t ldx, int64_t ldy, uint32_t flags, void *ws, size_t ws_bytes,
                          void *stream);
@@ -460,10 +461,11 @@ ghd_status ghd_kv_append_q4(const ghd_kv *kv, const void *k, const void *v, cons
                             int64_t ld_q_out, float rope_base, void *stream);
 
 /* ghd_tree_attention and ghd_masked_attention over a 4-bit cache whose rows
- * [0, kv_len + M) are there: q, out fp16 [M, nh, d].  An infinity or NaN in a row
- * reaches the tokens that see the row and no others.  The workspace's size falls
- * neither with M nor with kv_len: one for the widest tree over the longest context
- * does for every step of a loop. */
+ * [0, kv_len + M) are there: q, out fp16 [M, nh, d].  Scores, maxima and sums are 32
+ * bits; probabilities are rounded to fp16 before they are summed and meet V.  An
+ * infinity or NaN in a row reaches the tokens that see the row and no others.  The
+ * workspace's size falls neither with M nor with kv_len: one for the widest tree
+ * over the longest context does for every step of a loop. */
 ghd_status ghd_tree_attention_q4(void *out, const void *q, const ghd_kv *kv,
                                  const int32_t *parent_dev, int M, int kv_len, int nh, int nkv, int d,
                                  int capacity, float scale, void *ws, size_t ws_bytes, void *stream);

@@ -13,7 +13,8 @@
 // reads 36 bytes/ns instead of 121.  LDS takes a request lane after lane; so that operands are read without bank conflicts the
 // 16-byte pieces of row r of the 8 lie in the order piece ^ r.  Above 64 rows there are two groups of rows in workgroups of
 // their own, on the same XCD, whose L2 has the weights for the second.
-// Bound: at one row the bytes ([22016, 4096] 11.4 us, 4.1 TB/s); for small matrices the launch (3 to 4 us).
+// Bound: at one row the bytes ([22016, 4096] 11.3 us with weights in the 256 MB cache, 13.0 from HBM, 3.6 TB/s); for small matrices
+// the launch (3 to 4 us).
 // Every workgroup begins somewhere else in its range (`turn`): rows of x are often a power of two apart, a unit's 256 bytes of
 // all of them then lie in one channel of the L2, and all workgroups would ask that one at a time.
 #include "q4.h"
@@ -68,10 +69,10 @@ __device__ __forceinline__ int q4_turn(int x, int n)
     return __builtin_amdgcn_readfirstlane(at - q4_over(at, q4_inverse(n)) * n);
 }
 
-// x comes through a buffer resource of as many bytes as lie between its first and behind its last number, and a request for what lies
-// behind is dropped.  Of the two offsets that a request has the check counts the lane's and may leave out the scalar one, so all
-// of where a request goes is in the lane's: one addition for each (16 rows of [22016, 4096] 12.1 and 12.2 us).  A lane takes 16 bytes of 8 rows by 64 columns, which begin
-// `first` bytes behind the first row's.
+// x comes through a buffer resource that ends with the last number of its last row, and a request for what lies behind is dropped.
+// Of the two offsets that a request has the check counts the lane's and may leave out the scalar one, so all of where a request
+// goes is in the lane's: an addition for each (16 rows of [22016, 4096] 12.2 us, with scalar offsets 12.1).  A wavefront's lanes
+// take 16 bytes each of 8 rows by 64 columns.
 __host__ __device__ __forceinline__ int q4_x_bytes(int M, int K, int ldx) { return ((M - 1) * ldx + K) * 2; }
 __host__ __device__ __forceinline__ int q4_x_lane(int lane, int ldx) { return (lane >> 3) * ldx * 2 + ((lane & 7) ^ (lane >> 3)) * 16; }
 __host__ __device__ __forceinline__ int q4_x_first(int row, int col, int ldx) { return row * (ldx * 2) + col * 2; }
@@ -211,9 +212,10 @@ __global__ __launch_bounds__(kQ4LinWaves * 64) void k_q4_linear(Q4_LINEAR_FIRST,
 // shares of twice the registers, operands read ahead: [22016, 4096] at 64 rows 24.4 us, 21.8 with four; a finer ring, half
 // a unit a barrier: 25.8; two shares with three turns under way instead of one: 23.2 and 22.3; weights requested a whole turn ahead
 // instead of half of one 21.7 and 22.5, but with groups of 32 and 64 more registers than there are.)
-// Bound: [32000, 5120] at 128 rows, 58 us with all weights from HBM, would take 27 with neither weights nor x to fetch, 33 with x
-// alone, 50 with weights alone: their way into a compute unit, at 2 TB/s of the card's 4.75, with more of them under way no faster.
-// [4096, 11008] at 64 rows: 10 us, 4 of them before the first and behind the last product, and a launch that adds up.
+// Bound: [32000, 5120] at 128 rows takes 54 to 56 us, from HBM as from the 256 MB cache (which three such matrices pass).  Of an earlier
+// 58 it would have taken 27 with neither weights nor x to fetch, 33 with x alone, 50 with weights alone: their way into a compute
+// unit, at 2 TB/s of the card's 4.75, with more of them under way no faster.  [4096, 11008] at 64 rows, 13.8 us (16.2 from HBM): a
+// launch of 10, 4 of them before the first and behind the last product, and one that adds up.
 constexpr int kQ4Groups = 4, kQ4Shares = 4, kQ4RowThreads = kQ4Groups * kQ4Shares * 64;
 
 template <int MT, int RW, int G>
@@ -541,7 +543,7 @@ static bool q4_meet(Q4Rows a, Q4Rows b)
     return false;
 }
 
-// Workgroups that are done write y while others still read x and W.
+// Workgroups that are done write y while others still read x and W, so y must lie beside both.
 bool q4_linear_meets(const Q4Linear& a)
 {
     const int size = a.out16 ? 2 : 4;
