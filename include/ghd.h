@@ -484,6 +484,82 @@ ghd_status ghd_commit_path_q4(const ghd_kv *kv_host, int L, int nkv, int d, int 
 ghd_status ghd_kv_read_q4(void *k_out, void *v_out, const ghd_kv *kv_host, int L, int nkv, int d,
                           int capacity, int row0, int rows, void *stream);
 
+/* ---- long contexts: attention over blocks of the cache that each token selects --------
+ * With a long context the step's bytes are the committed cache (section 2.2.2).  These calls let every
+ * drafted token read a part of it: bounds are kept of the keys of every block of 64
+ * committed rows, a token's queries are scored against them, and the attention reads the
+ * blocks that a token has selected, the committed rows behind the last whole block, and the drafted
+ * rows that the token sees.  The cache is the one of ghd_tree_attention, with nkv key heads:
+ * nh % nkv == 0, query head h reads key head h / (nh / nkv).  nh <= 256, d in {64, 128},
+ * kv_len <= 2^21.  Blocks are counted from row 0; kv_len / 64 are whole.
+ *
+ * Bounds of one layer (ghd_block_bounds_bytes, 16-byte aligned), of every block and channel: HI = ceil(max
+ * K / s), LO = floor(min K / s), whole numbers within -127 .. 127, s = 2^(floor(log2 a) - 6) with a the
+ * largest |K| of the block.  Only these calls look inside; blocks that were never given may hold anything. */
+
+/* capacity: rows of the cache, up to 2^24; 0 for sizes that are not taken. */
+size_t ghd_block_bounds_bytes(int nkv, int capacity, int d);
+
+/* Bounds of blocks [block0, block0 + blocks), whose rows have to be there.  To be called for blocks that
+ * have become whole, once; again where rows of a block change. */
+ghd_status ghd_block_bounds(void *bounds, const void *k_cache, int block0, int blocks, int nkv, int d,
+                            int capacity, int64_t k_stride_head, int64_t k_stride_tok, void *stream);
+
+/* What the bounds of blocks [block0, block0 + blocks) stand for: hi, lo float [nkv, blocks, d], 16-byte
+ * aligned: HI s and LO s; infinity and minus infinity for a block that holds an infinity or NaN. */
+ghd_status ghd_block_bounds_read(float *hi, float *lo, const void *bounds, int block0, int blocks, int nkv,
+                                 int d, int capacity, void *stream);
+
+/* Which blocks each token reads: the first `sinks`, the last `recent` (sinks + recent <= count) and
+ * of the others the best, min(count, kv_len / 64) in all, the lowest index on ties.
+ *   q        fp16 [M, nh, d]
+ *   sel_dev  uint64 [nkv][ceil(M / 64)][kv_len / 64]: bit i % 64 of word i / 64 says that token i reads
+ *            the block (NULL is fine where there is no whole block)
+ * A block's score for a token and a key head is the largest over the head's query heads of
+ * s' s sum_c (max(Q_c, 0) HI_c + min(Q_c, 0) LO_c), where Q = rint(q / s') is the query held like a
+ * key: up to the rounding of q the highest score that a key of the block can have.  It is exact in 32 bits: equal inputs
+ * have equal selections.  A block that holds an infinity or NaN scores infinity; a query head that
+ * does scores 0. */
+ghd_status ghd_block_select(uint64_t *sel_dev, const void *q, const void *bounds, int M, int kv_len, int nh,
+                            int nkv, int d, int capacity, int count, int sinks, int recent, void *ws,
+                            size_t ws_bytes, void *stream);
+size_t ghd_block_select_workspace_bytes(int M, int kv_len, int nkv);
+
+/* ghd_tree_attention (parent_dev) or ghd_masked_attention (mask_dev; exactly one of the two) over what each
+ * token reads: rows of whole blocks by sel_dev - from ghd_block_select, or any other - , rows from
+ * 64 (kv_len / 64) on, and drafted rows.  q, out fp16 [M, nh, d]; out may be q, and meets nothing else that the call
+ * reads.  A token that sees no key gives zeros.  An infinity or NaN in a row reaches the tokens that
+ * see the row and no others (a call over such rows is many times slower).  Statistics and sums are 32
+ * bits, probabilities are rounded to fp16.  The workspace's size falls neither with M nor with kv_len. */
+ghd_status ghd_sparse_attention(void *out, const void *q, const void *k_cache, const void *v_cache,
+                                const uint64_t *sel_dev, const int32_t *parent_dev, const uint64_t *mask_dev,
+                                int M, int kv_len, int nh, int nkv, int d, int64_t k_stride_head,
+                                int64_t k_stride_tok, int64_t v_stride_head, int64_t v_stride_ch, float scale,
+                                void *ws, size_t ws_bytes, void *stream);
+size_t ghd_sparse_attention_workspace_bytes(int M, int kv_len, int nh, int nkv, int d);
+
+/* ---- sampled acceptance: drafted tokens against the target's probabilities --------------
+ * Takes ghd_accept_greedy's place where the answer is sampled: what is accepted and what follows has the
+ * distribution of sampling token by token from p = softmax(logits[node] / temperature).  From the root on, the
+ * children of the node that was accepted last are tried in index order, x = tokens[c]:
+ *   q_logits NULL (drafts that were not drawn, such as ghd_draft_tokens'):
+ *     accepted if u[c] sum(p) < p(x); otherwise p(x) becomes 0
+ *   q_logits float [q_rows, V], children drawn in their order, without replacement, from q = softmax(q_logits[r] /
+ *   q_temperature), r = q_row_dev[node] (clamped to the rows; NULL: r = node, q_rows >= M):
+ *     accepted if u[c] q(x) < p(x); otherwise p becomes max(p - q, 0), normalised (it stays as it is
+ *     where that is 0 throughout), and q without x, normalised
+ * Where no child is accepted the next token is the first at which the running sum of p exceeds u[0] sum(p).
+ *   u_dev    float [M], in [0, 1): u[c] tries node c, u[0] draws the last token
+ *   res_dev  as ghd_accept_greedy's: length, next token, path; words behind the path are not written
+ * NaN and -infinity among logits have the probability 0; where a row holds infinity its infinities share all of it.  The next
+ * token is -1 where no token has a probability.  Tokens outside of the vocabulary are rejected.
+ * Weights are 24 bits, their arguments and sums 64.  V <= 262144, q_rows <= GHD_MAX_M. */
+ghd_status ghd_accept_sampled(const float *logits, const int32_t *tokens_dev, const int32_t *parent_dev,
+                              const float *u_dev, const float *q_logits, const int32_t *q_row_dev, int q_rows,
+                              int M, int V, float temperature, float q_temperature, int32_t *res_dev, void *ws,
+                              size_t ws_bytes, void *stream);
+size_t ghd_accept_sampled_workspace_bytes(int M, int V);
+
 #ifdef __cplusplus
 }
 #endif

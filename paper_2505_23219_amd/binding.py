@@ -114,6 +114,16 @@ def lib() -> C.CDLL:
             "ghd_attention_q4_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
             "ghd_commit_path_q4": (C.c_int32, [vp, i32, i32, i32, i32, vp, i32, i32, vp]),
             "ghd_kv_read_q4": (C.c_int32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]),
+            "ghd_block_bounds_bytes": (sz, [i32, i32, i32]),
+            "ghd_block_bounds": (C.c_int32, [vp, vp, i32, i32, i32, i32, i32, i64, i64, vp]),
+            "ghd_block_bounds_read": (C.c_int32, [vp, vp, vp, i32, i32, i32, i32, i32, vp]),
+            "ghd_block_select": (C.c_int32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
+            "ghd_block_select_workspace_bytes": (sz, [i32, i32, i32]),
+            "ghd_sparse_attention": (C.c_int32, [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i64, i64, i64, i64,
+                                                 f32, vp, sz, vp]),
+            "ghd_sparse_attention_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+            "ghd_accept_sampled": (C.c_int32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp, sz, vp]),
+            "ghd_accept_sampled_workspace_bytes": (sz, [i32, i32]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -135,7 +145,10 @@ EXPORTS = ["ghd_status_str", "ghd_last_hip_error", "ghd_tree_validate", "ghd_tre
            "ghd_spec_workspace_bytes",
            "ghd_weight_q4_bytes", "ghd_pack_weight_q4", "ghd_linear_q4", "ghd_linear_q4_workspace_bytes",
            "ghd_kv_q4_bytes", "ghd_kv_append_q4", "ghd_tree_attention_q4", "ghd_masked_attention_q4",
-           "ghd_attention_q4_workspace_bytes", "ghd_commit_path_q4", "ghd_kv_read_q4"]
+           "ghd_attention_q4_workspace_bytes", "ghd_commit_path_q4", "ghd_kv_read_q4",
+           "ghd_block_bounds_bytes", "ghd_block_bounds", "ghd_block_bounds_read", "ghd_block_select",
+           "ghd_block_select_workspace_bytes", "ghd_sparse_attention", "ghd_sparse_attention_workspace_bytes",
+           "ghd_accept_sampled", "ghd_accept_sampled_workspace_bytes"]
 
 
 def status_str(status: int) -> str:
@@ -710,3 +723,160 @@ def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] 
     if st:
         _check(st, "ghd_kv_read_q4")
     return k, v
+
+
+# ---- attention over selected blocks of a long cache ------------------------------
+# (Checks that stay under python -O, as for the 4-bit calls; these also hold every tensor to the current device.)
+GHD_BLOCK = 64
+
+
+def _here(name: str, t: torch.Tensor, dtype, shape=None) -> int:
+    """Where a contiguous tensor of dtype (and shape) on the current GPU lies."""
+    if not (t.is_cuda and t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape)):
+        raise _misfit(name, t, "a contiguous %s tensor%s on the GPU"
+                      % (str(dtype).replace("torch.", ""), "" if shape is None else " %s" % (tuple(shape),)))
+    _on_current(name, t)
+    return t.data_ptr()
+
+
+def _on_current(name: str, t: torch.Tensor) -> None:
+    if t.get_device() != torch.cuda.current_device():
+        raise _misfit(name, t, "on the current device, cuda:%d" % torch.cuda.current_device())
+
+
+def _cache_at(name: str, t: torch.Tensor, heads: int, rows: int, cols: int) -> int:
+    """Where a cache [heads, >= rows, >= cols] (any strides, the last axis side by side) lies."""
+    if not (t.is_cuda and t.dtype is torch.float16 and t.dim() == 3 and t.stride(2) == 1 and t.shape[0] == heads
+            and t.shape[1] >= rows and t.shape[2] >= cols):
+        raise _misfit(name, t, "float16 on the GPU, at least (%d, %d, %d), its last axis side by side" % (heads, rows, cols))
+    _on_current(name, t)
+    return t.data_ptr()
+
+
+class BlockBounds:
+    """Bounds of the keys of every whole block of 64 rows of one layer's cache of `capacity` rows."""
+
+    def __init__(self, nkv: int, d: int, capacity: int, device="cuda"):
+        n = lib().ghd_block_bounds_bytes(nkv, capacity, d)
+        if n == 0 and not (0 < capacity < GHD_BLOCK and 1 <= nkv <= 256 and d in (64, 128)):
+            raise ValueError("no bounds of %d heads of %d channels by %d rows" % (nkv, d, capacity))
+        if torch.device(device).type != "cuda":
+            raise ValueError("bounds lie on the GPU, not on %s" % device)
+        self.nkv, self.d, self.capacity = nkv, d, capacity
+        self.data = torch.zeros(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def ghd_block_bounds(bounds: BlockBounds, k_cache: torch.Tensor, block0: int, blocks: int) -> None:
+    """Bounds of blocks block0 .. block0 + blocks - 1 from k_cache fp16 [nkv, rows, d]."""
+    nkv, d = bounds.nkv, bounds.d
+    k = _cache_at("k_cache", k_cache, nkv, (block0 + blocks) * GHD_BLOCK, d)
+    head, tok, _ = k_cache.stride()
+    st = (_lib or lib()).ghd_block_bounds(_here("bounds", bounds.data, torch.uint8), k, block0, blocks, nkv, d, bounds.capacity, head, tok,
+                                          _stream())
+    if st:
+        _check(st, "ghd_block_bounds")
+
+
+def ghd_block_bounds_read(bounds: BlockBounds, block0: int, blocks: int, hi: Optional[torch.Tensor] = None,
+                          lo: Optional[torch.Tensor] = None) -> tuple:
+    """What the bounds stand for: float [nkv, blocks, d], largest and smallest key of each channel."""
+    shape = (bounds.nkv, blocks, bounds.d)
+    data = _here("bounds", bounds.data, torch.uint8)
+    if hi is None:
+        hi = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
+    if lo is None:
+        lo = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
+    st = (_lib or lib()).ghd_block_bounds_read(_here("hi", hi, torch.float32, shape), _here("lo", lo, torch.float32, shape), data, block0,
+                                               blocks, bounds.nkv, bounds.d, bounds.capacity, _stream())
+    if st:
+        _check(st, "ghd_block_bounds_read")
+    return hi, lo
+
+
+def ghd_block_select_workspace_bytes(M: int, kv_len: int, nkv: int) -> int:
+    return lib().ghd_block_select_workspace_bytes(M, kv_len, nkv)
+
+
+def ghd_block_select(q: torch.Tensor, bounds: BlockBounds, kv_len: int, count: int, sinks: int = 1, recent: int = 1,
+                     sel: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q fp16 [M, nh, d] -> int64 [nkv, ceil(M / 64), kv_len // 64]: bit i % 64 of word i / 64 says that
+    token i reads the block; `count` blocks a token, the first `sinks` and the last `recent` among them."""
+    L = _lib or lib()
+    M, nh, d = q.shape
+    nkv = bounds.nkv
+    if d != bounds.d:
+        raise _misfit("q", q, "of heads of %d channels" % bounds.d)
+    q_ptr, shape = _here("q", q, torch.float16), (nkv, -(-M // 64), kv_len // GHD_BLOCK)
+    if sel is None:
+        sel = torch.empty(shape, dtype=torch.int64, device=q.device)
+    if ws is None:
+        ws = workspace(L.ghd_block_select_workspace_bytes(M, kv_len, nkv), q.device)
+    st = L.ghd_block_select(_here("sel", sel, torch.int64, shape), q_ptr, _here("bounds", bounds.data, torch.uint8), M, kv_len, nh, nkv, d,
+                            bounds.capacity, count, sinks, recent, _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    if st:
+        _check(st, "ghd_block_select")
+    return sel
+
+
+def ghd_sparse_attention_workspace_bytes(M: int, kv_len: int, nh: int, nkv: int, d: int) -> int:
+    return lib().ghd_sparse_attention_workspace_bytes(M, kv_len, nh, nkv, d)
+
+
+def ghd_sparse_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, sel: torch.Tensor, kv_len: int,
+                         parent: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                         ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q fp16 [M, nh, d] over the blocks of `sel` (ghd_block_select), the committed rows behind the last whole
+    block, and the drafted rows by `parent` (a tree) or `mask` (int64 [M, 2], as ghd_masked_attention).
+    k_cache fp16 [nkv, rows, d]; v_cache fp16 [nkv, d, rows] (channel-major); returns fp16 [M, nh, d]."""
+    L = _lib or lib()
+    M, nh, d = q.shape
+    nkv, rows = k_cache.shape[0], kv_len + M
+    if (parent is None) == (mask is None):
+        raise ValueError("either parent or mask says which drafted tokens a token sees")
+    q_ptr, k, v = _here("q", q, torch.float16), _cache_at("k_cache", k_cache, nkv, rows, d), _cache_at("v_cache", v_cache, nkv, d, rows)
+    k_head, k_tok, _ = k_cache.stride()
+    v_head, v_ch, _ = v_cache.stride()
+    if out is None:
+        out = torch.empty_like(q)
+    if ws is None:
+        ws = workspace(L.ghd_sparse_attention_workspace_bytes(M, kv_len, nh, nkv, d), q.device)
+    st = L.ghd_sparse_attention(_here("out", out, torch.float16, q.shape), q_ptr, k, v,
+                                _here("sel", sel, torch.int64, (nkv, -(-M // 64), kv_len // GHD_BLOCK)),
+                                None if parent is None else _here("parent", parent, torch.int32, (M,)),
+                                None if mask is None else _here("mask", mask, torch.int64, (M, 2)), M, kv_len, nh, nkv, d, k_head, k_tok,
+                                v_head, v_ch, d ** -0.5 if scale is None else scale, _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    if st:
+        _check(st, "ghd_sparse_attention")
+    return out
+
+
+# ---- sampled acceptance -----------------------------------------------------------
+def ghd_accept_sampled_workspace_bytes(M: int, V: int) -> int:
+    return lib().ghd_accept_sampled_workspace_bytes(M, V)
+
+
+def ghd_accept_sampled(logits: torch.Tensor, tokens: torch.Tensor, parent: torch.Tensor, u: torch.Tensor, temperature: float = 1.0,
+                       q_logits: Optional[torch.Tensor] = None, q_row: Optional[torch.Tensor] = None,
+                       q_temperature: Optional[float] = None, res: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Acceptance against softmax(logits / temperature) by the random numbers u float [M]; q_logits float
+    [rows, V]: what the children of node i were drawn from, row q_row[i] (int32 [M]) or i, at
+    q_temperature (that of the target by default).  Returns res int32 [2 + M] as ghd_accept_greedy."""
+    L = _lib or lib()
+    M, V = logits.shape
+    if res is None:
+        res = torch.zeros(2 + M, dtype=torch.int32, device=logits.device)
+    if ws is None:
+        ws = workspace(L.ghd_accept_sampled_workspace_bytes(M, V), logits.device)
+    q_rows = 0
+    if q_logits is not None:
+        q_rows = q_logits.shape[0]
+    st = L.ghd_accept_sampled(_here("logits", logits, torch.float32, (M, V)), _here("tokens", tokens, torch.int32, (M,)),
+                              _here("parent", parent, torch.int32, (M,)), _here("u", u, torch.float32, (M,)),
+                              None if q_logits is None else _here("q_logits", q_logits, torch.float32, (q_rows, V)),
+                              None if q_row is None else _here("q_row", q_row, torch.int32, (M,)), q_rows, M, V, temperature,
+                              temperature if q_temperature is None else q_temperature, _here("res", res, torch.int32, (2 + M,)),
+                              _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    if st:
+        _check(st, "ghd_accept_sampled")
+    return res

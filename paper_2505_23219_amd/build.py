@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libghd.so")
 PROBE = os.path.join(HERE, "ghd_stream_probe")       # measurement tool (bench.py --stream-probe), its own program
 PROBE_SOURCE = "stream_probe.hip"
 SOURCES = ["api.hip", "fused.hip", "linear.hip", "accept.hip", "draft.hip", "coo.hip",
-           "q4_api.hip", "q4_cache.hip", "q4_attention.hip", "q4_linear.hip"] + \
+           "q4_api.hip", "q4_cache.hip", "q4_attention.hip", "q4_linear.hip",
+           "sparse_api.hip", "blocks.hip", "sparse_attention.hip", "sampled.hip"] + \
     ["linear_mt%d.hip" % n for n in (1, 2, 3, 4, 6, 8)] + ["qkv_attn_mt%d.hip" % n for n in (1, 2, 3, 4, 6, 8)]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # keep the compiler from forming packed-fp32 instructions
@@ -24,7 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics"]
 # The persistent kernels must not use scratch memory: a launch of a kernel that has a private
 # segment costs several microseconds more here, whatever the kernel does with it.
-NO_SCRATCH = ("k_linear", "k_qkv_attn", "k_attention", "k_q4_")
+NO_SCRATCH = ("k_linear", "k_qkv_attn", "k_attention", "k_q4_", "k_block_", "k_sparse_", "k_sample_")
 
 
 def _hipcc() -> str:

@@ -1,0 +1,172 @@
+"""What the calls of the sparse attention and the sampled acceptance take and refuse, without a GPU."""
+import os
+import subprocess
+import sys
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2505_23219_amd import binding as B
+
+FAR = [0x10000000 + 0x10000000 * i for i in range(16)]      # 16-byte aligned, apart, never dereferenced here
+SMALL = dict(M=4, kv_len=640, nh=8, nkv=4, d=64)
+
+
+def _select(**kw):
+    a = dict(SMALL, sel=FAR[0], q=FAR[1], bounds=FAR[2], capacity=700, count=3, sinks=1, recent=1, ws=FAR[3], ws_bytes=1 << 24, **{})
+    a.update(kw)
+    return B.lib().ghd_block_select(a["sel"], a["q"], a["bounds"], a["M"], a["kv_len"], a["nh"], a["nkv"], a["d"], a["capacity"], a["count"],
+                                    a["sinks"], a["recent"], a["ws"], a["ws_bytes"], None)
+
+
+def _attend(**kw):
+    a = dict(SMALL, out=FAR[0], q=FAR[1], k=FAR[2], v=FAR[4], sel=FAR[6], parent=FAR[7], mask=None, kh=700 * 64, kt=64, vh=704 * 64, vc=704,
+             scale=0.125, ws=FAR[8], ws_bytes=1 << 26)
+    a.update(kw)
+    return B.lib().ghd_sparse_attention(a["out"], a["q"], a["k"], a["v"], a["sel"], a["parent"], a["mask"], a["M"], a["kv_len"], a["nh"],
+                                        a["nkv"], a["d"], a["kh"], a["kt"], a["vh"], a["vc"], a["scale"], a["ws"], a["ws_bytes"], None)
+
+
+def _accept(**kw):
+    a = dict(logits=FAR[0], tokens=FAR[1], parent=FAR[2], u=FAR[3], q=None, row=None, rows=0, M=8, V=1000, T=1.0, qT=1.0, res=FAR[4],
+             ws=FAR[5], ws_bytes=1 << 24)
+    a.update(kw)
+    return B.lib().ghd_accept_sampled(a["logits"], a["tokens"], a["parent"], a["u"], a["q"], a["row"], a["rows"], a["M"], a["V"], a["T"],
+                                      a["qT"], a["res"], a["ws"], a["ws_bytes"], None)
+
+
+def _bounds(**kw):
+    a = dict(bounds=FAR[0], k=FAR[1], b0=0, n=4, nkv=4, d=64, cap=640, kh=640 * 64, kt=64)
+    a.update(kw)
+    return B.lib().ghd_block_bounds(a["bounds"], a["k"], a["b0"], a["n"], a["nkv"], a["d"], a["cap"], a["kh"], a["kt"], None)
+
+
+def _read(**kw):
+    a = dict(hi=FAR[0], lo=FAR[1], bounds=FAR[2], b0=0, n=4, nkv=4, d=64, cap=640)
+    a.update(kw)
+    return B.lib().ghd_block_bounds_read(a["hi"], a["lo"], a["bounds"], a["b0"], a["n"], a["nkv"], a["d"], a["cap"], None)
+
+
+NULL, SHAPE, CAPACITY, WORKSPACE, ALIGN = (B.GHD_ERR_NULL, B.GHD_ERR_SHAPE, B.GHD_ERR_CAPACITY, B.GHD_ERR_WORKSPACE, B.GHD_ERR_ALIGN)
+nan, inf = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("call,want,change", [
+    (_bounds, NULL, dict(bounds=None)), (_bounds, NULL, dict(k=None)), (_bounds, SHAPE, dict(d=96)), (_bounds, SHAPE, dict(nkv=0)),
+    (_bounds, SHAPE, dict(nkv=257)), (_bounds, CAPACITY, dict(cap=0)), (_bounds, CAPACITY, dict(cap=(1 << 24) + 1)),
+    (_bounds, CAPACITY, dict(n=11)), (_bounds, CAPACITY, dict(b0=7)), (_bounds, SHAPE, dict(b0=-1)), (_bounds, SHAPE, dict(n=-1)),
+    (_bounds, CAPACITY, dict(b0=2 ** 31 - 1)), (_bounds, SHAPE, dict(kt=63)), (_bounds, SHAPE, dict(kh=-8)), (_bounds, ALIGN, dict(kt=68)),
+    (_bounds, ALIGN, dict(kh=41004)), (_bounds, ALIGN, dict(k=FAR[1] + 8)), (_bounds, SHAPE, dict(bounds=FAR[1] + 1024)),
+    (_bounds, SHAPE, dict(bounds=FAR[1] - 1024)), (_bounds, B.GHD_OK, dict(n=0)),
+    (_read, NULL, dict(hi=None)), (_read, NULL, dict(lo=None)), (_read, NULL, dict(bounds=None)), (_read, CAPACITY, dict(n=11)),
+    (_read, ALIGN, dict(lo=FAR[1] + 4)), (_read, SHAPE, dict(lo=FAR[0] + 64)), (_read, SHAPE, dict(hi=FAR[2] + 64)),
+    (_read, B.GHD_OK, dict(n=0, hi=None, lo=None)),
+    (_select, NULL, dict(sel=None)), (_select, NULL, dict(q=None)), (_select, NULL, dict(bounds=None)), (_select, SHAPE, dict(M=0)),
+    (_select, SHAPE, dict(M=129)), (_select, SHAPE, dict(kv_len=-1)), (_select, SHAPE, dict(kv_len=(1 << 21) + 1)),
+    (_select, SHAPE, dict(nh=9)), (_select, SHAPE, dict(nh=260)), (_select, SHAPE, dict(nkv=0)), (_select, SHAPE, dict(d=32)),
+    (_select, CAPACITY, dict(capacity=639)), (_select, SHAPE, dict(count=1)), (_select, SHAPE, dict(count=-1, sinks=0, recent=0)),
+    (_select, SHAPE, dict(sinks=-1)), (_select, SHAPE, dict(recent=-1)), (_select, SHAPE, dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1)),
+    (_select, WORKSPACE, dict(ws=None)), (_select, WORKSPACE, dict(ws_bytes=100)), (_select, ALIGN, dict(ws=FAR[3] + 8)),
+    (_select, ALIGN, dict(sel=FAR[0] + 4)), (_select, ALIGN, dict(q=FAR[1] + 2)), (_select, SHAPE, dict(sel=FAR[1] + 16)),
+    (_select, SHAPE, dict(sel=FAR[2])), (_select, SHAPE, dict(sel=FAR[3] + 64)), (_select, B.GHD_OK, dict(kv_len=63, sel=None, ws=None)),
+    (_attend, NULL, dict(out=None)), (_attend, NULL, dict(q=None)), (_attend, NULL, dict(k=None)), (_attend, NULL, dict(v=None)),
+    (_attend, NULL, dict(sel=None)), (_attend, NULL, dict(parent=None)), (_attend, SHAPE, dict(mask=FAR[9])), (_attend, SHAPE, dict(M=0)),
+    (_attend, SHAPE, dict(M=129)), (_attend, SHAPE, dict(kv_len=(1 << 21) + 1)), (_attend, SHAPE, dict(kv_len=-64)),
+    (_attend, SHAPE, dict(nkv=3)), (_attend, SHAPE, dict(d=80)), (_attend, SHAPE, dict(scale=nan)), (_attend, SHAPE, dict(scale=inf)),
+    (_attend, SHAPE, dict(kt=56)), (_attend, SHAPE, dict(vh=-8)), (_attend, CAPACITY, dict(vc=640)), (_attend, ALIGN, dict(vc=645)),
+    (_attend, ALIGN, dict(kt=68)), (_attend, ALIGN, dict(out=FAR[0] + 8)), (_attend, ALIGN, dict(parent=FAR[7] + 2)),
+    (_attend, ALIGN, dict(sel=FAR[6] + 4)), (_attend, ALIGN, dict(mask=FAR[9] + 4, parent=None)), (_attend, WORKSPACE, dict(ws=None)),
+    (_attend, WORKSPACE, dict(ws_bytes=0)), (_attend, ALIGN, dict(ws=FAR[8] + 8)), (_attend, SHAPE, dict(out=FAR[1] + 16)),
+    (_attend, SHAPE, dict(out=FAR[2] + 4096)), (_attend, SHAPE, dict(out=FAR[4])), (_attend, SHAPE, dict(out=FAR[6])),
+    (_attend, SHAPE, dict(out=FAR[7])), (_attend, SHAPE, dict(out=FAR[8] + 256)),
+    (_accept, NULL, dict(logits=None)), (_accept, NULL, dict(tokens=None)), (_accept, NULL, dict(parent=None)), (_accept, NULL, dict(u=None)),
+    (_accept, NULL, dict(res=None)), (_accept, NULL, dict(row=FAR[7])), (_accept, SHAPE, dict(M=0)), (_accept, SHAPE, dict(M=129)),
+    (_accept, SHAPE, dict(V=0)), (_accept, SHAPE, dict(V=262145)), (_accept, SHAPE, dict(T=0.0)), (_accept, SHAPE, dict(T=-1.0)),
+    (_accept, SHAPE, dict(T=nan)), (_accept, SHAPE, dict(T=inf)), (_accept, SHAPE, dict(q=FAR[6], rows=7)),
+    (_accept, SHAPE, dict(q=FAR[6], rows=0, row=FAR[7])), (_accept, SHAPE, dict(q=FAR[6], rows=129)),
+    (_accept, SHAPE, dict(q=FAR[6], rows=8, qT=0.0)), (_accept, SHAPE, dict(q=FAR[6], rows=8, qT=nan)), (_accept, ALIGN, dict(logits=FAR[0] + 2)),
+    (_accept, ALIGN, dict(res=FAR[4] + 1)), (_accept, WORKSPACE, dict(ws=None)), (_accept, WORKSPACE, dict(ws_bytes=64)),
+    (_accept, ALIGN, dict(ws=FAR[5] + 8)), (_accept, SHAPE, dict(res=FAR[5] + 64))])
+def test_refused(call, want, change):
+    assert call(**change) == want
+
+
+def test_sizes():
+    L = B.lib()
+    assert L.ghd_block_bounds_bytes(4, 640, 64) == 4 * 10 * (128 + 4) and L.ghd_block_bounds_bytes(4, 63, 64) == 0
+    for bad in ((0, 640, 64), (257, 640, 64), (4, 0, 64), (4, (1 << 24) + 1, 64), (4, 640, 48)):
+        assert L.ghd_block_bounds_bytes(*bad) == 0
+    assert L.ghd_block_select_workspace_bytes(0, 64, 1) == L.ghd_block_select_workspace_bytes(1, -1, 1) == 0
+    assert L.ghd_sparse_attention_workspace_bytes(1, 64, 3, 2, 64) == 0
+    assert L.ghd_accept_sampled_workspace_bytes(129, 10) == L.ghd_accept_sampled_workspace_bytes(1, 0) == 0
+
+
+def test_workspaces_do_not_shrink():
+    """One made for the widest tree over the longest context does for every step on the way there."""
+    L = B.lib()
+    for nh, nkv, d in ((32, 32, 128), (32, 8, 128), (20, 4, 64), (40, 1, 64), (256, 256, 128)):
+        for f in (lambda M, kv: L.ghd_sparse_attention_workspace_bytes(M, kv, nh, nkv, d), lambda M, kv: L.ghd_block_select_workspace_bytes(M, kv, nkv)):
+            most = {}
+            for M in (1, 2, 3, 5, 9, 16, 17, 31, 33, 64, 65, 100, 128):
+                for kv in (0, 1, 64, 700, 4096, 33000, 131072, 1 << 21):
+                    most[M, kv] = max([f(M, kv)] + [most[m, k] for m, k in most if m <= M and k <= kv])
+                    assert f(M, kv) == most[M, kv], (nh, nkv, d, M, kv)
+    sizes = [L.ghd_accept_sampled_workspace_bytes(M, 32000) for M in range(1, 129)]
+    assert sizes == sorted(sizes)
+
+
+def _host_calls():
+    """Python calls with tensors in host memory, of wrong types or shapes."""
+    half, i32, i64, f32 = (lambda *n: torch.zeros(n, dtype=torch.float16)), (lambda *n: torch.zeros(n, dtype=torch.int32)), (
+        lambda *n: torch.zeros(n, dtype=torch.int64)), (lambda *n: torch.zeros(n))
+    bounds = SimpleNamespace(nkv=2, d=64, capacity=128, data=torch.zeros(1024, dtype=torch.uint8))
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    yield lambda: B.BlockBounds(2, 64, 128, "cpu")
+    yield lambda: B.BlockBounds(2, 65, 128)
+    yield lambda: B.ghd_block_bounds(bounds, half(2, 128, 64), 0, 1)
+    yield lambda: B.ghd_block_bounds_read(bounds, 0, 1)
+    yield lambda: B.ghd_block_select(half(3, 2, 64), bounds, 128, 2)
+    yield lambda: B.ghd_block_select(half(3, 2, 128), bounds, 128, 2)
+    yield lambda: B.ghd_sparse_attention(half(3, 2, 64), half(2, 136, 64), half(2, 64, 136), i64(2, 1, 2), 128, parent=i32(3), ws=ws)
+    yield lambda: B.ghd_sparse_attention(half(3, 2, 64), half(2, 136, 64), half(2, 64, 136), i64(2, 1, 2), 128, ws=ws)
+    yield lambda: B.ghd_sparse_attention(half(3, 2, 64), half(2, 136, 64), half(2, 64, 136), i64(2, 1, 2), 128, parent=i32(3), mask=i64(3, 2))
+    yield lambda: B.ghd_accept_sampled(f32(3, 10), i32(3), i32(3), f32(3), ws=ws)
+
+
+def _refused():
+    for i, call in enumerate(_host_calls()):
+        try:
+            call()
+        except ValueError:
+            continue
+        raise SystemExit("call %d was not refused" % i)
+    print("refused", i + 1)
+
+
+def test_host_tensors_are_refused():
+    _refused()
+
+
+def test_they_are_refused_without_assertions_too():
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-O", "-c", "import test_sparse_arguments as t; t._refused()"], capture_output=True, text=True,
+                       env={**os.environ, "PYTHONPATH": os.pathsep.join([here, os.path.dirname(here)])})
+    assert r.returncode == 0 and "refused 10" in r.stdout, r.stdout + r.stderr
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class Elsewhere:
+        is_cuda, dtype, shape, device = True, torch.float16, (2, 2, 64), "cuda:1"
+
+        def is_contiguous(self):
+            return True
+
+        def get_device(self):
+            return 1
+
+        def stride(self):
+            return (128, 64, 1)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device, cuda:0"):
+        B._here("q", Elsewhere(), torch.float16)
