@@ -726,31 +726,33 @@ def ghd_kv_read_q4(cache: KvQ4, row0: int, rows: int, k: Optional[torch.Tensor] 
 
 
 # ---- attention over selected blocks of a long cache ------------------------------
-# (Checks that stay under python -O, as for the 4-bit calls; these also hold every tensor to the current device.)
+# (Checks that stay under python -O, as for the 4-bit calls; these also hold every tensor to the current device.  They cost the
+# host more than the C call: one look at a tensor's device says whether it is on the GPU, and on which.)
 GHD_BLOCK = 64
 
 
-def _here(name: str, t: torch.Tensor, dtype, shape=None) -> int:
-    """Where a contiguous tensor of dtype (and shape) on the current GPU lies."""
-    if not (t.is_cuda and t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape)):
-        raise _misfit(name, t, "a contiguous %s tensor%s on the GPU"
-                      % (str(dtype).replace("torch.", ""), "" if shape is None else " %s" % (tuple(shape),)))
-    _on_current(name, t)
+def _here(name: str, t: torch.Tensor, dtype, shape, dev: int) -> int:
+    """Where a contiguous tensor of dtype (and shape, unless it is None) on GPU `dev` lies."""
+    if dev < 0 or t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise _misfit(name, t, "a contiguous %s tensor%s on the GPU%s" % (
+            str(dtype).replace("torch.", ""), "" if shape is None else " %s" % (tuple(shape),), "" if dev < 0 else " cuda:%d" % dev))
     return t.data_ptr()
 
 
-def _on_current(name: str, t: torch.Tensor) -> None:
-    if t.get_device() != torch.cuda.current_device():
-        raise _misfit(name, t, "on the current device, cuda:%d" % torch.cuda.current_device())
-
-
-def _cache_at(name: str, t: torch.Tensor, heads: int, rows: int, cols: int) -> int:
-    """Where a cache [heads, >= rows, >= cols] (any strides, the last axis side by side) lies."""
-    if not (t.is_cuda and t.dtype is torch.float16 and t.dim() == 3 and t.stride(2) == 1 and t.shape[0] == heads
-            and t.shape[1] >= rows and t.shape[2] >= cols):
+def _cache_at(name: str, t: torch.Tensor, heads: int, rows: int, cols: int, dev: int) -> int:
+    """Where a cache [heads, >= rows, >= cols] (any strides, the last axis side by side) on GPU `dev` lies."""
+    if (dev < 0 or t.get_device() != dev or t.dtype is not torch.float16 or t.dim() != 3 or t.stride(2) != 1 or t.shape[0] != heads
+            or t.shape[1] < rows or t.shape[2] < cols):
         raise _misfit(name, t, "float16 on the GPU, at least (%d, %d, %d), its last axis side by side" % (heads, rows, cols))
-    _on_current(name, t)
     return t.data_ptr()
+
+
+def _stream_of(dev: int) -> int:
+    """The current stream, if `dev` is the current device."""
+    now = torch.cuda.current_device()
+    if now != dev:
+        raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (dev, now))
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
 class BlockBounds:
@@ -768,11 +770,11 @@ class BlockBounds:
 
 def ghd_block_bounds(bounds: BlockBounds, k_cache: torch.Tensor, block0: int, blocks: int) -> None:
     """Bounds of blocks block0 .. block0 + blocks - 1 from k_cache fp16 [nkv, rows, d]."""
-    nkv, d = bounds.nkv, bounds.d
-    k = _cache_at("k_cache", k_cache, nkv, (block0 + blocks) * GHD_BLOCK, d)
+    nkv, d, dev = bounds.nkv, bounds.d, k_cache.get_device()
+    k = _cache_at("k_cache", k_cache, nkv, (block0 + blocks) * GHD_BLOCK, d, dev)
     head, tok, _ = k_cache.stride()
-    st = (_lib or lib()).ghd_block_bounds(_here("bounds", bounds.data, torch.uint8), k, block0, blocks, nkv, d, bounds.capacity, head, tok,
-                                          _stream())
+    st = (_lib or lib()).ghd_block_bounds(_here("bounds", bounds.data, torch.uint8, None, dev), k, block0, blocks, nkv, d, bounds.capacity,
+                                          head, tok, _stream_of(dev))
     if st:
         _check(st, "ghd_block_bounds")
 
@@ -780,14 +782,14 @@ def ghd_block_bounds(bounds: BlockBounds, k_cache: torch.Tensor, block0: int, bl
 def ghd_block_bounds_read(bounds: BlockBounds, block0: int, blocks: int, hi: Optional[torch.Tensor] = None,
                           lo: Optional[torch.Tensor] = None) -> tuple:
     """What the bounds stand for: float [nkv, blocks, d], largest and smallest key of each channel."""
-    shape = (bounds.nkv, blocks, bounds.d)
-    data = _here("bounds", bounds.data, torch.uint8)
+    shape, dev = (bounds.nkv, blocks, bounds.d), bounds.data.get_device()
+    data = _here("bounds", bounds.data, torch.uint8, None, dev)
     if hi is None:
         hi = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
     if lo is None:
         lo = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
-    st = (_lib or lib()).ghd_block_bounds_read(_here("hi", hi, torch.float32, shape), _here("lo", lo, torch.float32, shape), data, block0,
-                                               blocks, bounds.nkv, bounds.d, bounds.capacity, _stream())
+    st = (_lib or lib()).ghd_block_bounds_read(_here("hi", hi, torch.float32, shape, dev), _here("lo", lo, torch.float32, shape, dev), data,
+                                               block0, blocks, bounds.nkv, bounds.d, bounds.capacity, _stream_of(dev))
     if st:
         _check(st, "ghd_block_bounds_read")
     return hi, lo
@@ -803,16 +805,16 @@ def ghd_block_select(q: torch.Tensor, bounds: BlockBounds, kv_len: int, count: i
     token i reads the block; `count` blocks a token, the first `sinks` and the last `recent` among them."""
     L = _lib or lib()
     M, nh, d = q.shape
-    nkv = bounds.nkv
+    nkv, dev = bounds.nkv, q.get_device()
     if d != bounds.d:
         raise _misfit("q", q, "of heads of %d channels" % bounds.d)
-    q_ptr, shape = _here("q", q, torch.float16), (nkv, -(-M // 64), kv_len // GHD_BLOCK)
+    q_ptr, shape = _here("q", q, torch.float16, None, dev), (nkv, -(-M // 64), kv_len // GHD_BLOCK)
     if sel is None:
         sel = torch.empty(shape, dtype=torch.int64, device=q.device)
     if ws is None:
         ws = workspace(L.ghd_block_select_workspace_bytes(M, kv_len, nkv), q.device)
-    st = L.ghd_block_select(_here("sel", sel, torch.int64, shape), q_ptr, _here("bounds", bounds.data, torch.uint8), M, kv_len, nh, nkv, d,
-                            bounds.capacity, count, sinks, recent, _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    st = L.ghd_block_select(_here("sel", sel, torch.int64, shape, dev), q_ptr, _here("bounds", bounds.data, torch.uint8, None, dev), M, kv_len,
+                            nh, nkv, d, bounds.capacity, count, sinks, recent, _here("ws", ws, ws.dtype, None, dev), ws.nbytes, _stream_of(dev))
     if st:
         _check(st, "ghd_block_select")
     return sel
@@ -830,21 +832,23 @@ def ghd_sparse_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     k_cache fp16 [nkv, rows, d]; v_cache fp16 [nkv, d, rows] (channel-major); returns fp16 [M, nh, d]."""
     L = _lib or lib()
     M, nh, d = q.shape
-    nkv, rows = k_cache.shape[0], kv_len + M
+    nkv, rows, dev = k_cache.shape[0], kv_len + M, q.get_device()
     if (parent is None) == (mask is None):
         raise ValueError("either parent or mask says which drafted tokens a token sees")
-    q_ptr, k, v = _here("q", q, torch.float16), _cache_at("k_cache", k_cache, nkv, rows, d), _cache_at("v_cache", v_cache, nkv, d, rows)
+    q_ptr = _here("q", q, torch.float16, None, dev)
+    k, v = _cache_at("k_cache", k_cache, nkv, rows, d, dev), _cache_at("v_cache", v_cache, nkv, d, rows, dev)
     k_head, k_tok, _ = k_cache.stride()
     v_head, v_ch, _ = v_cache.stride()
     if out is None:
         out = torch.empty_like(q)
     if ws is None:
         ws = workspace(L.ghd_sparse_attention_workspace_bytes(M, kv_len, nh, nkv, d), q.device)
-    st = L.ghd_sparse_attention(_here("out", out, torch.float16, q.shape), q_ptr, k, v,
-                                _here("sel", sel, torch.int64, (nkv, -(-M // 64), kv_len // GHD_BLOCK)),
-                                None if parent is None else _here("parent", parent, torch.int32, (M,)),
-                                None if mask is None else _here("mask", mask, torch.int64, (M, 2)), M, kv_len, nh, nkv, d, k_head, k_tok,
-                                v_head, v_ch, d ** -0.5 if scale is None else scale, _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    st = L.ghd_sparse_attention(_here("out", out, torch.float16, q.shape, dev), q_ptr, k, v,
+                                _here("sel", sel, torch.int64, (nkv, -(-M // 64), kv_len // GHD_BLOCK), dev),
+                                None if parent is None else _here("parent", parent, torch.int32, (M,), dev),
+                                None if mask is None else _here("mask", mask, torch.int64, (M, 2), dev), M, kv_len, nh, nkv, d, k_head, k_tok,
+                                v_head, v_ch, d ** -0.5 if scale is None else scale, _here("ws", ws, ws.dtype, None, dev), ws.nbytes,
+                                _stream_of(dev))
     if st:
         _check(st, "ghd_sparse_attention")
     return out
@@ -868,15 +872,13 @@ def ghd_accept_sampled(logits: torch.Tensor, tokens: torch.Tensor, parent: torch
         res = torch.zeros(2 + M, dtype=torch.int32, device=logits.device)
     if ws is None:
         ws = workspace(L.ghd_accept_sampled_workspace_bytes(M, V), logits.device)
-    q_rows = 0
-    if q_logits is not None:
-        q_rows = q_logits.shape[0]
-    st = L.ghd_accept_sampled(_here("logits", logits, torch.float32, (M, V)), _here("tokens", tokens, torch.int32, (M,)),
-                              _here("parent", parent, torch.int32, (M,)), _here("u", u, torch.float32, (M,)),
-                              None if q_logits is None else _here("q_logits", q_logits, torch.float32, (q_rows, V)),
-                              None if q_row is None else _here("q_row", q_row, torch.int32, (M,)), q_rows, M, V, temperature,
-                              temperature if q_temperature is None else q_temperature, _here("res", res, torch.int32, (2 + M,)),
-                              _here("ws", ws, ws.dtype), ws.nbytes, _stream())
+    dev, q_rows = logits.get_device(), 0 if q_logits is None else q_logits.shape[0]
+    st = L.ghd_accept_sampled(_here("logits", logits, torch.float32, None, dev), _here("tokens", tokens, torch.int32, (M,), dev),
+                              _here("parent", parent, torch.int32, (M,), dev), _here("u", u, torch.float32, (M,), dev),
+                              None if q_logits is None else _here("q_logits", q_logits, torch.float32, (q_rows, V), dev),
+                              None if q_row is None else _here("q_row", q_row, torch.int32, (M,), dev), q_rows, M, V, temperature,
+                              temperature if q_temperature is None else q_temperature, _here("res", res, torch.int32, (2 + M,), dev),
+                              _here("ws", ws, ws.dtype, None, dev), ws.nbytes, _stream_of(dev))
     if st:
         _check(st, "ghd_accept_sampled")
     return res

@@ -104,75 +104,91 @@ __device__ __forceinline__ uint32_t max_over_four(uint32_t x)
     return max(x, (uint32_t)__shfl_xor((int)x, 32));
 }
 
-// 16 channels' codes: those above zero (which meet HI) and those below (which meet LO)
-__device__ __forceinline__ void query_codes(const half8 (&x)[2], float inv, int4_& above, int4_& below)
+// 16 channels' codes, those above zero (which meet HI) and those below (which meet LO), by pairs in fp16: a number times the two
+// factors of 1 / unit is exact (or so far below a half that it does not matter), and 1536 more is rounded to a whole number,
+// ties to even, whose low byte is the code.
+__device__ __forceinline__ void query_codes(const half8 (&x)[2], half2_ first, half2_ second, int4_& above, int4_& below)
 {
+    const half2_ zero = {0, 0}, most = {127, 127}, round = {1536, 1536};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        uint32_t p = 0, n = 0;
+        uint32_t up[2], down[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = code_of(rintf((float)x[w / 2][w % 2 * 4 + e] * inv));
-            p |= (uint32_t)max(c, 0) << 8 * e;
-            n |= (uint32_t)(min(c, 0) & 255) << 8 * e;
+        for (int e = 0; e < 2; ++e) {
+            const int at = w % 2 * 4 + 2 * e;
+            const half2_ v = (half2_){x[w / 2][at], x[w / 2][at + 1]} * first * second;
+            up[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_max(v, zero), most) + round);
+            down[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_min(v, zero), -most) + round);
         }
-        above[w] = (int32_t)p;
-        below[w] = (int32_t)n;
+        above[w] = (int32_t)__builtin_amdgcn_perm(up[1], up[0], 0x06040200u);
+        below[w] = (int32_t)__builtin_amdgcn_perm(down[1], down[0], 0x06040200u);
     }
 }
 
-constexpr int kScoreTiles = 4;                   // of 16 blocks: a wavefront's
-
-// Blocks are the rows of the product, 16 tokens of one query head its columns.  A wavefront keeps the codes of 64 blocks in registers
-// and goes through the query heads.  Bound: over long contexts the bytes of the codes.
-template <int D>
+// Blocks are the rows of the product, 16 tokens of one query head its columns.  A wavefront keeps the codes of TILES tiles of 16 blocks in
+// registers and goes through the query heads.
+template <int D, int TILES>
 __global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
 {
     constexpr int KS = 2 * D / 64;               // k-steps: the first half of them HI, the second LO
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int b0 = (blockIdx.x * 4 + wave) * kScoreTiles * 16, head = blockIdx.y, m = blockIdx.z * 16 + col;
+    const int b0 = (blockIdx.x * 4 + wave) * TILES * 16, head = blockIdx.y, m = blockIdx.z * 16 + col;
     if (b0 >= a.n) return;
-    const size_t row0 = (size_t)head * a.bounds.blocks;
-    int4_ code[kScoreTiles][KS];
+    half8 x[KS / 2][2];
+    const half_t* q = a.q + ((size_t)min(m, a.M - 1) * a.nkv + head) * a.rep * D + g * 16;
+    auto ask_for = [&]() {
 #pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t)
+        for (int s = 0; s < KS / 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[s][e] = *(const half8*)(q + s * 64 + e * 8);
+    };
+    ask_for();
+    const size_t row0 = (size_t)head * a.bounds.blocks;
+    int4_ code[TILES][KS];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int s = 0; s < KS; ++s)
             code[t][s] = *(const int4_*)(a.bounds.codes + (row0 + min(b0 + t * 16 + col, a.n - 1)) * 2 * D + s * 64 + g * 16);
-    floatx4 unit[kScoreTiles], best[kScoreTiles];
+    floatx4 unit[TILES], best[TILES];
 #pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t) {
+    for (int t = 0; t < TILES; ++t) {
         best[t] = (floatx4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int r = 0; r < 4; ++r) unit[t][r] = a.bounds.units[row0 + min(b0 + t * 16 + 4 * g + r, a.n - 1)];
     }
-    if (blockIdx.z == 0 && b0 + lane < a.n)      // the picks set bits
+    if (a.zero && blockIdx.z == 0 && lane < TILES * 16 && b0 + lane < a.n)       // the picks set bits
         for (int w = 0; w < (a.M + 63) / 64; ++w) a.sel[((size_t)head * ((a.M + 63) / 64) + w) * a.n + b0 + lane] = 0;
-    const half_t* q = a.q + ((size_t)min(m, a.M - 1) * a.nkv + head) * a.rep * D + g * 16;
-    for (int h = 0; h < a.rep; ++h, q += D) {
-        half8 x[KS / 2][2];
-        uint32_t top = 0;
+    for (int h = 0; h < a.rep; ++h) {
+        typedef uint16_t ushort2_ __attribute__((ext_vector_type(2)));
+        ushort2_ size = {0, 0};
 #pragma unroll
         for (int s = 0; s < KS / 2; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                x[s][e] = *(const half8*)(q + s * 64 + e * 8);
                 const uint4_ w = __builtin_bit_cast(uint4_, x[s][e]) & 0x7fff7fffu;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0xffffu, w[i] >> 16));
+                for (int i = 0; i < 4; ++i) size = __builtin_elementwise_max(size, __builtin_bit_cast(ushort2_, (uint32_t)w[i]));
             }
-        top = max_over_four(top);
+        const uint32_t top = max_over_four(max((uint32_t)size[0], (uint32_t)size[1]));
         // (a head that holds an infinity or NaN, or only zeros, scores 0 everywhere)
         const bool some = top > 0 && top < 0x7c00u;
-        const float step = some ? unit_below(__builtin_bit_cast(half_t, (uint16_t)top)) : 0.f, inv = some ? one_over_power(step) : 0.f;
+        const float step = some ? unit_below(__builtin_bit_cast(half_t, (uint16_t)top)) : 0.f;
+        // 1 / step is 2^-9 to 2^30: two factors, each an fp16 number
+        const int up = some ? 127 - (int)(__float_as_uint(step) >> 23) : 0, half = up >> 1;
+        const half_t f1 = __builtin_bit_cast(half_t, (uint16_t)((half + 15) << 10)), f2 = __builtin_bit_cast(half_t, (uint16_t)((up - half + 15) << 10));
         int4_ ask[KS];
 #pragma unroll
         for (int s = 0; s < KS / 2; ++s) {
-            query_codes(x[s], inv, ask[s], ask[KS / 2 + s]);
+            query_codes(x[s], (half2_){f1, f1}, (half2_){f2, f2}, ask[s], ask[KS / 2 + s]);
             if (!some) ask[s] = ask[KS / 2 + s] = (int4_){0, 0, 0, 0};
         }
+        if (h + 1 < a.rep) {
+            q += D;
+            ask_for();
+        }
 #pragma unroll
-        for (int t = 0; t < kScoreTiles; ++t) {
+        for (int t = 0; t < TILES; ++t) {
             int4_ sum = {0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < KS; ++s) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(code[t][s], ask[s], sum, 0, 0, 0);
@@ -184,7 +200,7 @@ __global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
     const int n4 = (a.n + 3) & ~3;
     uint32_t* to = a.keys + ((size_t)head * a.M + m) * n4;
 #pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t) {
+    for (int t = 0; t < TILES; ++t) {
         const int b = b0 + t * 16 + 4 * g;
         if (b >= n4) continue;
         uint4_ key;
@@ -195,32 +211,88 @@ __global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
 }
 
 // ---- picks -------------------------------------------------------------------------------
-// A workgroup has a token and a key head: the lowest key of the `keep` best is found 8 bits at a time, then what is above it is
-// taken and of those equal to it the first.
-__global__ __launch_bounds__(256) void k_block_pick(SelectArgs a)
+// A team of wavefronts has a token and a key head: one wavefront, of eight in a workgroup, or all of a workgroup's.  The range of the keys is
+// cut in 256 steps and the step counted out in which the `keep` best end (scores lie close together: by their leading bits nearly
+// all would fall in a few); what is above is taken, and what is in it ranked, or, if it is much, cut again.  Of more
+// equal keys than are ranked the first are taken in order.
+template <int TEAM>
+struct PickShared {
+    static constexpr int kWaves = TEAM / 64, kRanked = TEAM < 256 ? TEAM : 256;
+    uint32_t hist[256], low[kWaves], high[kWaves], step, need, in, n, key[kRanked];
+    int at[kRanked];
+};
+template <int TEAM>
+__device__ __forceinline__ void team_sync()
 {
-    __shared__ uint32_t s_hist[256], s_bin, s_need, s_same;
-    const int tid = threadIdx.x, m = blockIdx.x, head = blockIdx.y;
-    const uint32_t* keys = a.keys + ((size_t)head * a.M + m) * ((a.n + 3) & ~3);
-    uint64_t* sel = a.sel + ((size_t)head * ((a.M + 63) / 64) + m / 64) * a.n;
-    const uint64_t bit = 1ull << (m % 64);
-    auto take = [&](int b) { atomicOr((unsigned long long*)(sel + b), (unsigned long long)bit); };
-    for (int b = tid; b < a.lo + (a.n - a.hi); b += 256) take(b < a.lo ? b : a.hi + b - a.lo);
-    if (a.keep <= 0) return;
-    uint32_t prefix = 0, known = 0, need = a.keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        s_hist[tid] = 0;
+    if constexpr (TEAM == 64) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
         __syncthreads();
-        for (int b = a.lo + tid; b < a.hi; b += 256) {
-            const uint32_t key = keys[b];
-            if ((key & known) == prefix) atomicAdd(&s_hist[key >> shift & 255], 1u);
+    }
+}
+
+// KEPT: keys that a thread keeps in registers, all of them; 0: they are read again each time.  take(b): block b is taken.
+template <int TEAM, int KEPT, class Take>
+__device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM>& s, const uint32_t* keys, int tid, const Take& take)
+{
+    typedef PickShared<TEAM> S;
+    const int lane = tid & 63, wave = tid >> 6;
+    uint32_t kept[KEPT ? KEPT : 1];
+    if constexpr (KEPT > 0) {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) kept[i] = a.lo + i * TEAM + tid < a.hi ? keys[a.lo + i * TEAM + tid] : 0;
+    }
+    // (0 is no score)
+    auto each = [&](auto f) {
+        if constexpr (KEPT > 0) {
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i)
+                if (kept[i] != 0) f(kept[i], a.lo + i * TEAM + tid);
+        } else {
+            for (int b = a.lo + tid; b < a.hi; b += TEAM) f(keys[b], b);
         }
-        __syncthreads();
-        if (tid < 64) {                          // bins from the highest on: lane l has 255 - 4 l .. 252 - 4 l
+    };
+    for (int b = tid; b < a.lo + (a.n - a.hi); b += TEAM) take(b < a.lo ? b : a.hi + b - a.lo);
+    if (a.keep <= 0) return;
+    uint32_t low = ~0u, high = 0;
+    each([&](uint32_t key, int) {
+        low = min(low, key);
+        high = max(high, key);
+    });
+    for (int off = 32; off > 0; off >>= 1) {
+        low = min(low, (uint32_t)__shfl_xor((int)low, off));
+        high = max(high, (uint32_t)__shfl_xor((int)high, off));
+    }
+    for (int i = tid; i < 256; i += TEAM) s.hist[i] = 0;
+    if (tid == 0) s.n = 0;
+    if constexpr (TEAM > 64) {
+        if (lane == 0) {
+            s.low[wave] = low;
+            s.high[wave] = high;
+        }
+    }
+    team_sync<TEAM>();
+    if constexpr (TEAM > 64) {
+#pragma unroll
+        for (int w = 0; w < S::kWaves; ++w) {
+            low = min(low, s.low[w]);
+            high = max(high, s.high[w]);
+        }
+    }
+    uint32_t need = a.keep, in;                  // of the keys from low to high, of which there are `in`
+    int shift = max(0, 24 - (int)__builtin_clz((high - low) | 1));
+    for (;;) {
+        each([&](uint32_t key, int) {
+            if (key >= low && key <= high) atomicAdd(&s.hist[(key - low) >> shift], 1u);
+        });
+        team_sync<TEAM>();
+        if (tid < 64) {                          // steps from the highest on: lane l has 255 - 4 l .. 252 - 4 l
             uint32_t c[4], sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += c[e] = s_hist[255 - 4 * tid - e];
+            for (int e = 0; e < 4; ++e) sum += c[e] = s.hist[255 - 4 * tid - e];
             uint32_t before = sum;
+#pragma unroll
             for (int off = 1; off < 64; off *= 2) {
                 const uint32_t o = (uint32_t)__shfl_up((int)before, off);
                 if (tid >= off) before += o;
@@ -229,41 +301,108 @@ __global__ __launch_bounds__(256) void k_block_pick(SelectArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (before < need && before + c[e] >= need) {
-                    s_bin = 255 - 4 * tid - e;
-                    s_need = need - before;
-                    s_same = c[e];
+                    s.step = 255 - 4 * tid - e;
+                    s.need = need - before;
+                    s.in = c[e];
                 }
                 before += c[e];
             }
         }
-        __syncthreads();
-        prefix |= s_bin << shift;
-        known |= 255u << shift;
-        need = s_need;
+        team_sync<TEAM>();
+        const uint32_t from = low + (s.step << shift), to = from + ((1u << shift) - 1);
+        each([&](uint32_t key, int b) {
+            if (key > to && key <= high) take(b);
+        });
+        low = from;
+        high = to;
+        need = s.need;
+        in = s.in;
+        if (in == need || in <= S::kRanked || shift == 0) break;
+        shift = max(0, shift - 8);
+        for (int i = tid; i < 256; i += TEAM) s.hist[i] = 0;   // (read last before it was synchronised)
+        team_sync<TEAM>();
     }
-    const uint32_t same = s_same;
-    for (int b = a.lo + tid; b < a.hi; b += 256) {
-        const uint32_t key = keys[b];
-        if (key > prefix || (same == need && key == prefix)) take(b);
+    if (in == need) {
+        each([&](uint32_t key, int b) {
+            if (key >= low && key <= high) take(b);
+        });
+        return;
     }
-    if (same == need) return;
-    // more of them than are needed: the first, in order
-    uint32_t* s_count = s_hist;                  // (read last before a barrier)
-    for (int b0 = a.lo; b0 < a.hi && need > 0; b0 += 256) {
+    if (in <= S::kRanked) {
+        each([&](uint32_t key, int b) {
+            if (key < low || key > high) return;
+            const uint32_t to = atomicAdd(&s.n, 1u);
+            s.key[to] = key;
+            s.at[to] = b;
+        });
+        team_sync<TEAM>();
+        if (tid >= (int)in) return;
+        const uint32_t key = s.key[tid];
+        const int at = s.at[tid];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < in; ++j) rank += s.key[j] > key || (s.key[j] == key && s.at[j] < at);
+        if (rank < need) take(at);
+        return;
+    }
+    // equal keys, more than are needed: the first, in order
+    for (int b0 = a.lo; b0 < a.hi && need > 0; b0 += TEAM) {
         const int b = b0 + tid;
-        const bool is = b < a.hi && keys[b] == prefix;
+        const bool is = b < a.hi && keys[b] == low;
         const uint64_t with = __ballot(is);
-        if ((tid & 63) == 0) s_count[tid >> 6] = __popcll(with);
-        __syncthreads();
-        uint32_t before = __popcll(with & ((1ull << (tid & 63)) - 1)), all = 0;
-        for (int w = 0; w < 4; ++w) {
-            if (w < tid >> 6) before += s_count[w];
-            all += s_count[w];
+        uint32_t before = __popcll(with & ((1ull << lane) - 1)), all = __popcll(with);
+        if constexpr (TEAM > 64) {
+            if (lane == 0) s.low[wave] = all;
+            __syncthreads();
+            all = 0;
+            for (int w = 0; w < S::kWaves; ++w) {
+                if (w < wave) before += s.low[w];
+                all += s.low[w];
+            }
+            __syncthreads();
         }
         if (is && before < need) take(b);
         need -= min(need, all);
-        __syncthreads();
     }
+}
+
+// A workgroup has eight tokens, a byte of the words, and the blocks' bytes in LDS; the last tokens' workgroup writes what is left of
+// the words, too.  64 tokens of 32 heads over 512 blocks: 8.2 us, a workgroup a token and its bits set by atomic operations 15.8.
+constexpr int kPickBytes = 2048;                 // blocks
+template <int KEPT>
+__global__ __launch_bounds__(512) void k_block_pick_eight(SelectArgs a)
+{
+    __shared__ PickShared<64> s[8];
+    __shared__ uint32_t s_bits[kPickBytes / 4];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m0 = blockIdx.x * 8, m = m0 + wave, head = blockIdx.y;
+    for (int i = tid; i < (a.n + 3) / 4; i += 512) s_bits[i] = 0;
+    __syncthreads();
+    if (m < a.M)
+        pick_blocks<64, KEPT>(a, s[wave], a.keys + ((size_t)head * a.M + m) * ((a.n + 3) & ~3), tid & 63,
+                              [&](int b) { atomicOr(&s_bits[b >> 2], 1u << (8 * (b & 3) + wave)); });
+    __syncthreads();
+    uint8_t* to = (uint8_t*)(a.sel + ((size_t)head * ((a.M + 63) / 64) + m0 / 64) * a.n) + m0 % 64 / 8;
+    const int left = m0 + 8 >= a.M ? 8 - m0 % 64 / 8 : 1;          // bytes of a word that are this workgroup's
+    for (int b = tid; b < a.n; b += 512) {
+        const uint8_t x = (uint8_t)(s_bits[b >> 2] >> 8 * (b & 3));
+        if (left == 8) {
+            a.sel[((size_t)head * ((a.M + 63) / 64) + m0 / 64) * a.n + b] = x;
+        } else {
+            to[(size_t)8 * b] = x;
+            for (int i = 1; i < left; ++i) to[(size_t)8 * b + i] = 0;
+        }
+    }
+}
+
+// A workgroup has a token; the words are zeros before (k_block_scores).
+template <int KEPT>
+__global__ __launch_bounds__(1024) void k_block_pick(SelectArgs a)
+{
+    __shared__ PickShared<1024> s;
+    const int m = blockIdx.x, head = blockIdx.y;
+    uint64_t* sel = a.sel + ((size_t)head * ((a.M + 63) / 64) + m / 64) * a.n;
+    const uint64_t bit = 1ull << (m % 64);
+    pick_blocks<1024, KEPT>(a, s, a.keys + ((size_t)head * a.M + m) * ((a.n + 3) & ~3), threadIdx.x,
+                            [&](int b) { atomicOr((unsigned long long*)(sel + b), (unsigned long long)bit); });
 }
 
 ghd_status launch_block_bounds(Bounds to, const half_t* k, int first, int n, int nkv, int d, int64_t k_head, int64_t k_tok, hipStream_t st)
@@ -284,15 +423,34 @@ ghd_status launch_block_bounds_read(float* hi, float* lo, Bounds from, int first
     return check_launch();
 }
 
-ghd_status launch_block_select(const SelectArgs& a, int d, hipStream_t st)
+ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
 {
     if (a.n == 0) return GHD_OK;
-    const dim3 grid(ceil_div(a.n, 4 * kScoreTiles * 16), a.nkv, ceil_div(a.M, 16));
-    if (d == 128) hipLaunchKernelGGL(k_block_scores<128>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_block_scores<64>, grid, dim3(256), 0, st, a);
+    // a wavefront has 64 blocks, or 16 where there would be fewer than four wavefronts for each compute unit
+    const int tiles = ceil_div(a.M, 16), per = (int64_t)ceil_div(a.n, 64) * a.nkv * tiles >= 1024 ? 4 : 1;
+    const dim3 grid(ceil_div(a.n, 64 * per), a.nkv, tiles);
+    const bool eight = a.n <= kPickBytes && (a.M > 4 || a.n <= 512);
+    a.zero = !eight;
+    if (d == 128) {
+        if (per == 4) hipLaunchKernelGGL((k_block_scores<128, 4>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_block_scores<128, 1>), grid, dim3(256), 0, st, a);
+    } else {
+        if (per == 4) hipLaunchKernelGGL((k_block_scores<64, 4>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_block_scores<64, 1>), grid, dim3(256), 0, st, a);
+    }
     const ghd_status s = check_launch();
     if (s) return s;
-    hipLaunchKernelGGL(k_block_pick, dim3(a.M, a.nkv), dim3(256), 0, st, a);
+    const int range = a.hi - a.lo;
+    if (eight) {
+        const dim3 teams(ceil_div(a.M, 8), a.nkv);
+        if (range <= 64 * 8) hipLaunchKernelGGL(k_block_pick_eight<8>, teams, dim3(512), 0, st, a);
+        else if (range <= 64 * 16) hipLaunchKernelGGL(k_block_pick_eight<16>, teams, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL(k_block_pick_eight<32>, teams, dim3(512), 0, st, a);
+    } else if (range <= 1024 * 4) {
+        hipLaunchKernelGGL(k_block_pick<4>, dim3(a.M, a.nkv), dim3(1024), 0, st, a);
+    } else {
+        hipLaunchKernelGGL(k_block_pick<0>, dim3(a.M, a.nkv), dim3(1024), 0, st, a);
+    }
     return check_launch();
 }
 

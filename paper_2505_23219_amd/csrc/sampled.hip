@@ -2,6 +2,8 @@
 //
 // Every node is judged at once as if the walk came there: k_sample_rows leaves maxima and sums of softmax weights of the rows' segments,
 // k_sample_nodes which child of each node is accepted, or which token is drawn there, and k_sample_walk goes from the root down.
+// Where drafts have probabilities, k_sample_first tries every node's first child, which takes no more than the rows' sums; that leaves
+// few nodes that the walk can come to, and of those k_sample_rest sums up what a first rejection leaves, over the segments again.
 //
 // Weights exp((l - m) / T) have arguments in 64 bits and 24 bits themselves; sums are 64 bits.  So a sum over a row is off by some
 // 2^-24 / sqrt(V) of its largest terms, by random roundings of single weights, and what 64 bits would accept or draw is
@@ -12,35 +14,52 @@ namespace ghd {
 
 constexpr int kSegment = 4096;                   // logits of a row that a workgroup takes
 constexpr int kRowThreads = 256, kPerThread = kSegment / kRowThreads;
-constexpr int kNodeThreads = 1024, kNodeWaves = kNodeThreads / 64;
+constexpr int kNodeThreads = 512, kNodeWaves = kNodeThreads / 64, kSide = kSegment / kNodeThreads;
 constexpr int kMaxSegments = 64;                 // of the largest vocabulary, 262144
+constexpr int kKeep = 64;                        // tokens that a thread of a node's workgroup keeps the weights of
+constexpr double kLog2e = 1.4426950408889634;
 
-// 2^x for x <= 0 in 64 bits' range
-__device__ __forceinline__ double power_of(double x)
-{
-    const double n = rint(x);
-    return ldexp((double)__builtin_amdgcn_exp2f((float)(x - n)), (int)fmax(n, -2000.0));
-}
-// The weight of a logit against a maximum, c = log2 e / T.  NaN and minus infinity have none; where the maximum is infinity only such
-// logits have one.
-__device__ __forceinline__ double weight_of(float l, float m, double c)
-{
-    if (!(l > -INFINITY)) return 0.0;
-    if (l == m) return 1.0;
-    if (m == INFINITY) return 0.0;
-    return power_of(((double)l - (double)m) * c);
-}
+// Softmax weights of a row: 2^((l - m) c), c = log2 e / T.  NaN and minus infinity have none; where the maximum is
+// infinity only such logits have one.
+struct Weights {
+    double c, off;
+    float top;
+    __device__ __forceinline__ Weights(float m, double c) : c(c), off(-(double)m * c), top(m) {}
+    // (fmax takes the number of a number and NaN; 2^-1100 is 0)
+    __device__ __forceinline__ double exponent(float l) const { return fmax(fma((double)l, c, off), -1100.0); }
+    __device__ __forceinline__ double operator()(float l) const
+    {
+        if (!(fabsf(top) < INFINITY)) return top > 0.f && l == top ? 1.0 : 0.0;
+        const double x = exponent(l), n = rint(x);
+        return ldexp((double)__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
+    }
+    // in 32 bits' range
+    __device__ __forceinline__ float low(float l) const
+    {
+        if (!(fabsf(top) < INFINITY)) return top > 0.f && l == top ? 1.f : 0.f;
+        const double x = exponent(l), n = rint(x);
+        return ldexpf(__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
+    }
+};
 
 struct Segment {
     double sum;                                  // of weights against the segment's maximum
-    float top;
-    int last;                                    // of the tokens that have a weight; -1: none has
+    float top, unused;
+};
+struct Rest {
+    double p, q;                                 // what the first rejection leaves: sums of max(p - q, 0) and q without the token
 };
 struct NodeResult {
     int taken, token;                            // accepted child or -1, and the token drawn where there is none
 };
+struct First {
+    double one, one_q;                           // one over the sums of the target's and the draft's row, 0 where those are
+    float top, top_q;                            // their maxima
+    int child, accepted;                         // the first child whose token is in the vocabulary, or GHD_MAX_M
+};
 
-__device__ __forceinline__ double wave_sum(double x)
+template <class T>
+__device__ __forceinline__ T wave_sum(T x)
 {
     for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
     return x;
@@ -56,39 +75,80 @@ __device__ __forceinline__ int wave_max_of(int x)
     return x;
 }
 
-// child c's parent, if c is one of the tree's nodes
-__device__ __forceinline__ bool child_of(const SampleArgs& a, int c, int node) { return c > node && c < a.M && a.parent[c] == node; }
+// Node c as a child: asked for before it is known whose child it is.
+struct Child {
+    int c, parent, token;
+    __device__ __forceinline__ Child(const SampleArgs& a, int c) : c(c), parent(a.parent[min(c, a.M - 1)]), token(a.tokens[min(c, a.M - 1)]) {}
+    __device__ __forceinline__ bool of(const SampleArgs& a, int node) const { return c > node && c < a.M && parent == node; }
+};
+__device__ __forceinline__ bool in_vocabulary(const SampleArgs& a, int t) { return t >= 0 && t < a.V; }
+__device__ __forceinline__ double u_of(float u) { return u > 0.f ? (double)u : 0.0; }
+__device__ __forceinline__ int draft_row(const SampleArgs& a, int node)
+{
+    return a.q_row ? min(max(a.q_row[node], 0), a.q_rows - 1) : node;
+}
 
-// Target rows (blockIdx.y < M) without the tokens of the node's children, where drafts have no probabilities; draft rows.
+// A row's maximum and one over its sum, from its segments' (a lane has one); 0 where no token has a weight.
+struct RowSum {
+    float top, mine;                             // mine: the lane's segment's
+    double one, part;                            // part: the lane's segment's sum against the row's maximum
+    __device__ __forceinline__ RowSum(const Segment* seg, int segments, int lane, double c)
+    {
+        Segment s = {0.0, -INFINITY, 0.f};
+        if (lane < segments) s = seg[lane];
+        mine = s.top;
+        top = wave_max_of(s.top);
+        part = s.sum * Weights(top, c)(s.top);
+        const double sum = wave_sum(part);
+        one = sum > 0.0 ? 1.0 / sum : 0.0;
+    }
+};
+
+// Target rows (blockIdx.y < M), without the tokens of the node's children where drafts have no probabilities; draft rows.
+// Bound: the bytes of the logits.
 __global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segment* __restrict__ seg)
 {
     __shared__ uint32_t s_out[kSegment / 32];
     __shared__ double s_sum[kRowThreads / 64];
     __shared__ float s_top[kRowThreads / 64];
-    __shared__ int s_last[kRowThreads / 64];
     const int tid = threadIdx.x, y = blockIdx.y, lo = blockIdx.x * kSegment, segments = gridDim.x;
     const bool target = y < a.M;
-    const float* row = target ? a.logits + (size_t)y * a.V : a.q_logits + (size_t)(y - a.M) * a.V;
-    const double c = 1.4426950408889634 / (double)(target ? a.temperature : a.q_temperature);
+    const float* row = (target ? a.logits + (size_t)y * a.V : a.q_logits + (size_t)(y - a.M) * a.V) + lo;
+    const int n = min(a.V - lo, kSegment);
+    const double c = kLog2e / (double)(target ? a.temperature : a.q_temperature);
+    const Child child(a, tid);
     float l[kPerThread];
+    // four neighbours a load where the row allows it
+    const bool wide = ((uintptr_t)row & 15) == 0 && n == kSegment;
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-        const int t = lo + i * kRowThreads + tid;
-        l[i] = t < a.V ? row[t] : -INFINITY;
+        for (int i = 0; i < kPerThread / 4; ++i) {
+            const floatx4 v = ((const floatx4*)row)[i * kRowThreads + tid];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) l[4 * i + e] = v[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const int t = (i / 4 * kRowThreads + tid) * 4 + i % 4;
+            l[i] = t < n ? row[t] : -INFINITY;
+        }
     }
     if (target && !a.q_logits) {
         if (tid < kSegment / 32) s_out[tid] = 0;
         __syncthreads();
-        if (tid < GHD_MAX_M && child_of(a, tid, y)) {
-            const int t = a.tokens[tid];
-            if (t >= lo && t < lo + kSegment) atomicOr(&s_out[(t - lo) >> 5], 1u << ((t - lo) & 31));
+        bool any = false;
+        if (tid < GHD_MAX_M && child.of(a, y)) {
+            const int t = child.token;
+            any = t >= lo && t < lo + kSegment;
+            if (any) atomicOr(&s_out[(t - lo) >> 5], 1u << ((t - lo) & 31));
         }
-        __syncthreads();
+        if (__syncthreads_or(any))
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) {
-            const int t = i * kRowThreads + tid;
-            if (s_out[t >> 5] >> (t & 31) & 1) l[i] = -INFINITY;
-        }
+            for (int i = 0; i < kPerThread; ++i) {
+                const int t = (i / 4 * kRowThreads + tid) * 4 + i % 4;
+                if (s_out[t >> 5] >> (t & 31) & 1) l[i] = -INFINITY;
+            }
     }
     float top = -INFINITY;
 #pragma unroll
@@ -98,291 +158,412 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segme
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kRowThreads / 64; ++w) top = fmaxf(top, s_top[w]);
+    const Weights weight(top, c);
     double sum = 0.0;
-    int last = -1;
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-        const double x = weight_of(l[i], top, c);
-        sum += x;
-        if (x > 0.0) last = lo + i * kRowThreads + tid;
-    }
+    for (int i = 0; i < kPerThread; ++i) sum += (double)weight.low(l[i]);
     sum = wave_sum(sum);
-    last = wave_max_of(last);
-    if ((tid & 63) == 0) {
-        s_sum[tid >> 6] = sum;
-        s_last[tid >> 6] = last;
-    }
+    if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
     __syncthreads();
     if (tid == 0) {
-        Segment s = {0.0, top, -1};
-        for (int w = 0; w < kRowThreads / 64; ++w) {
-            s.sum += s_sum[w];
-            s.last = max(s.last, s_last[w]);
-        }
-        seg[(size_t)y * segments + blockIdx.x] = s;
+        sum = 0.0;
+        for (int w = 0; w < kRowThreads / 64; ++w) sum += s_sum[w];
+        seg[(size_t)y * segments + blockIdx.x] = {sum, top, 0.f};
     }
 }
 
-// What a workgroup knows of a row: its maximum and, before every segment, the sum of weights against that
-struct Row {
-    float top;
-    double sum, at[kMaxSegments];                // at: a segment's factor, then the sum before it
+// A wavefront a node: its rows' sums, and whether its first child is accepted.
+__global__ __launch_bounds__(64) void k_sample_first(SampleArgs a, const Segment* __restrict__ seg, int segments, First* __restrict__ out)
+{
+    const int lane = threadIdx.x, node = blockIdx.x, qr = draft_row(a, node);
+    const Child low(a, lane), high(a, lane + 64);
+    const double c = kLog2e / (double)a.temperature, cq = kLog2e / (double)a.q_temperature;
+    const uint64_t in_low = __ballot(low.of(a, node) && in_vocabulary(a, low.token)), in_high = __ballot(high.of(a, node) && in_vocabulary(a, high.token));
+    const int at = in_low ? (int)__builtin_ctzll(in_low) : in_high ? (int)__builtin_ctzll(in_high) : 0;
+    const int x = __shfl(in_low ? low.token : high.token, at), child = in_low ? at : in_high ? at + 64 : GHD_MAX_M;
+    float lp = 0.f, lq = 0.f, u = 0.f;
+    if (child < GHD_MAX_M) {
+        lp = a.logits[(size_t)node * a.V + x];
+        lq = a.q_logits[(size_t)qr * a.V + x];
+        u = a.u[child];
+    }
+    const RowSum p(seg + (size_t)node * segments, segments, lane, c), q(seg + (size_t)(a.M + qr) * segments, segments, lane, cq);
+    if (lane != 0) return;
+    const double px = Weights(p.top, c)(lp) * p.one, qx = Weights(q.top, cq)(lq) * q.one;
+    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(u) * qx < px};
+}
+
+// Can the walk come to a node?  By what its ancestors' first children are: accepted, no other child of theirs is tried, rejected, not
+// they.  All threads of a workgroup (128 or more), pointers doubled.
+struct Reach {
+    int up[GHD_MAX_M], lost[GHD_MAX_M];
+};
+__device__ __forceinline__ bool reached(const SampleArgs& a, const First* first, int node, Reach& s)
+{
+    const int i = threadIdx.x;
+    int up = -1, lost = 0;
+    if (i < a.M) {
+        const int p = a.parent[i];
+        if (p >= 0 && p < i) {
+            up = p;
+            lost = (first[p].child == i) != (first[p].accepted != 0);
+        } else {
+            lost = i != 0;
+        }
+    }
+    while (__syncthreads_or(up >= 0)) {
+        if (i < GHD_MAX_M) {
+            s.up[i] = up;
+            s.lost[i] = lost;
+        }
+        __syncthreads();
+        if (up >= 0) {
+            lost |= s.lost[up];
+            up = s.up[up];
+        }
+    }
+    if (i < GHD_MAX_M) s.lost[i] = lost;
+    __syncthreads();
+    return s.lost[node] == 0;
+}
+
+// What is left of a segment when the first child of a node is rejected: then beta is 1.
+__global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, const Segment* __restrict__ seg, const First* __restrict__ firsts,
+                                                             Rest* __restrict__ rest)
+{
+    __shared__ Reach s_reach;
+    __shared__ double s_sum[2][kRowThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, node = blockIdx.y, lo = blockIdx.x * kSegment, segments = gridDim.x;
+    const First first = firsts[node];
+    if (first.child == GHD_MAX_M || first.accepted || !reached(a, firsts, node, s_reach)) return;
+    const int x = a.tokens[first.child], qr = draft_row(a, node);
+    const float *row = a.logits + (size_t)node * a.V, *q_row = a.q_logits + (size_t)qr * a.V;
+    const int n = min(a.V - lo, kSegment);
+    float lp[kPerThread], lq[kPerThread];
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+        const int t = lo + min(i * kRowThreads + tid, n - 1);
+        lp[i] = row[t];
+        lq[i] = q_row[t];
+    }
+    const Weights wp(first.top, kLog2e / (double)a.temperature), wq(first.top_q, kLog2e / (double)a.q_temperature);
+    double s = 0.0, r = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+        const int t = i * kRowThreads + tid;
+        const bool is = t < n && lo + t != x;
+        const double qt = is ? wq(lq[i]) * first.one_q : 0.0;
+        s += is ? fmax(wp(lp[i]) * first.one - qt, 0.0) : 0.0;
+        r += qt;
+    }
+    s = wave_sum(s);
+    r = wave_sum(r);
+    if (lane == 0) {
+        s_sum[0][tid >> 6] = s;
+        s_sum[1][tid >> 6] = r;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        Rest all = {0.0, 0.0};
+        for (int w = 0; w < kRowThreads / 64; ++w) {
+            all.p += s_sum[0][w];
+            all.q += s_sum[1][w];
+        }
+        rest[(size_t)node * segments + blockIdx.x] = all;
+    }
+}
+
+// What a node's workgroup shares.
+struct NodeShared {
+    int child[GHD_MAX_M], token[GHD_MAX_M], kids, taken, place[kNodeWaves], last[kNodeWaves];
+    double u0, u[GHD_MAX_M], weight[GHD_MAX_M], part[2][kNodeWaves], sums[kKeep / kSide][kNodeWaves];
+    Reach reach;
+    uint32_t out[kMaxSegments * kSegment / 32];  // a bit for each token that has been rejected
+    __device__ __forceinline__ bool rejected(int t) const { return out[t >> 5] >> (t & 31) & 1; }
 };
 
-__device__ __forceinline__ double u_of(float u) { return u > 0.f ? (double)u : 0.0; }
+// The token at which the running sum of weights passes u[0] of all.  part: what the lane's segment has in all (each wavefront has
+// them all); weight(t): a token's.  Called by all threads; thread 0 has the result, -1 where no token has a weight.
+template <class Weight>
+__device__ __forceinline__ int draw_from_segments(const SampleArgs& a, NodeShared& s, double part, int segments, const Weight& weight)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    double upto = part;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const double o = __shfl_up(upto, off);
+        if (lane >= off) upto += o;
+    }
+    const double goal = s.u0 * __shfl(upto, 63);
+    const uint64_t over = __ballot(part > 0.0 && upto > goal), some = __ballot(part > 0.0);
+    if (some == 0) return -1;
+    const int at = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some);
+    // a thread has some neighbours of it
+    double w[kSide], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kSide; ++e) {
+        const int t = at * kSegment + tid * kSide + e;
+        w[e] = t < a.V ? weight(t) : 0.0;
+        sum += w[e];
+    }
+    double run = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const double o = __shfl_up(run, off);
+        if (lane >= off) run += o;
+    }
+    __syncthreads();
+    if (lane == 63) s.part[0][wave] = run;
+    __syncthreads();
+    double before = (at > 0 ? __shfl(upto, at - 1) : 0.0) + run - sum;
+    for (int v = 0; v < wave; ++v) before += s.part[0][v];
+    // the first that passes, or the last that has a weight (the segment's own sum was larger by a rounding)
+    int first = 0x7fffffff, last = -1;
+#pragma unroll
+    for (int e = 0; e < kSide; ++e) {
+        before += w[e];
+        if (!(w[e] > 0.0)) continue;
+        last = at * kSegment + tid * kSide + e;
+        if (before > goal && first == 0x7fffffff) first = last;
+    }
+    first = -wave_max_of(-first);
+    last = wave_max_of(last);
+    if (lane == 0) {
+        s.place[wave] = first;
+        s.last[wave] = last;
+    }
+    __syncthreads();
+    for (int v = 0; v < kNodeWaves; ++v) {
+        first = min(first, s.place[v]);
+        last = max(last, s.last[v]);
+    }
+    return first != 0x7fffffff ? first : last;
+}
 
 // One workgroup a node.
-__global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, const Segment* __restrict__ seg, int segments,
-                                                               NodeResult* __restrict__ out)
+template <bool DRAFTS>
+__global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, const Segment* __restrict__ seg, const First* __restrict__ firsts,
+                                                               const Rest* __restrict__ rest, int segments, NodeResult* __restrict__ out)
 {
-    __shared__ int s_child[GHD_MAX_M], s_token[GHD_MAX_M];
-    __shared__ double s_weight[GHD_MAX_M], s_part[3][kNodeWaves];
-    __shared__ int s_kids, s_taken, s_last[kNodeWaves];
-    __shared__ float s_top;
-    __shared__ uint32_t s_out[kSegment / 32];
+    __shared__ NodeShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, node = blockIdx.x;
+    if constexpr (DRAFTS) {
+        if (firsts[node].accepted) {
+            if (tid == 0) out[node] = {firsts[node].child, -1};
+            return;
+        }
+        if (!reached(a, firsts, node, s.reach)) return;            // (the walk does not look at it)
+    }
     const float* row = a.logits + (size_t)node * a.V;
-    const Segment* mine = seg + (size_t)node * segments;
-    const double c = 1.4426950408889634 / (double)a.temperature;
+    const double c = kLog2e / (double)a.temperature;
     // children, in order
     if (wave == 0) {
+        const Child some[2] = {Child(a, lane), Child(a, lane + 64)};
+        const float u[2] = {a.u[min(lane, a.M - 1)], a.u[min(lane + 64, a.M - 1)]};
         int n = 0;
-        for (int h = 0; h < GHD_MAX_M / 64; ++h) {
-            const bool is = child_of(a, h * 64 + lane, node);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool is = some[h].of(a, node);
             const uint64_t with = __ballot(is);
             if (is) {
                 const int k = n + __popcll(with & ((1ull << lane) - 1));
-                s_child[k] = h * 64 + lane;
-                s_token[k] = a.tokens[h * 64 + lane];
+                s.child[k] = some[h].c;
+                s.token[k] = some[h].token;
+                s.u[k] = u_of(u[h]);
             }
             n += __popcll(with);
         }
         if (lane == 0) {
-            s_kids = n;
-            s_taken = -1;
+            s.kids = n;
+            s.u0 = u_of(u[0]);
         }
     }
+    for (int i = tid; i < (a.V + 31) / 32; i += kNodeThreads) s.out[i] = 0;
+    const RowSum p(seg + (size_t)node * segments, segments, lane, c);
     __syncthreads();
-    const int kids = s_kids;
-    auto there = [&](int t) { return t >= 0 && t < a.V; };
+    const int kids = s.kids;
+    auto twice = [&](int k) {                    // whether child k's token was an earlier child's
+        bool is = false;
+        for (int j = 0; j < k; ++j) is = is || s.token[j] == s.token[k];
+        return is;
+    };
+    auto finish = [&](int taken, int token) {
+        if (tid == 0) out[node] = {taken, token};
+    };
 
-    if (!a.q_logits || kids == 0) {
-        // Drafts without probabilities: a child is accepted if u (what is left) < its weight.  What is left before a child: the
-        // tokens that no child has, and the weights of this child and those after it.
+    if constexpr (!DRAFTS) {
+        // A child is accepted if u (what is left) < its weight.  What is left before a child: the tokens that no child has, and the
+        // weights of this child and those after it.
         if (wave == 0) {
-            float top = -INFINITY;
-            for (int s = lane; s < segments; s += 64) top = fmaxf(top, mine[s].top);
+            float top = p.top;
             for (int k = lane; k < kids; k += 64)
-                if (there(s_token[k])) top = fmaxf(top, row[s_token[k]]);
+                if (in_vocabulary(a, s.token[k])) top = fmaxf(top, row[s.token[k]]);
             top = wave_max_of(top);
-            double rest = 0.0;
-            for (int s = lane; s < segments; s += 64) rest += mine[s].sum * weight_of(mine[s].top, top, c);
-            rest = wave_sum(rest);
-            for (int k = lane; k < kids; k += 64) {
-                double w = there(s_token[k]) ? weight_of(row[s_token[k]], top, c) : 0.0;
-                for (int j = 0; j < k; ++j)
-                    if (s_token[j] == s_token[k]) w = 0.0;     // it was rejected before
-                s_weight[k] = w;
-            }
+            const Weights weight(top, c);
+            const double others = p.one > 0.0 ? weight(p.top) / p.one : 0.0;
+            for (int k = lane; k < kids; k += 64)
+                s.weight[k] = in_vocabulary(a, s.token[k]) && !twice(k) ? weight(row[s.token[k]]) : 0.0;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             int first = GHD_MAX_M;
             for (int k = lane; k < kids; k += 64) {
-                double left = rest;
-                for (int j = kids - 1; j >= k; --j) left += s_weight[j];
-                if (u_of(a.u[s_child[k]]) * left < s_weight[k]) first = min(first, k);
+                double left = others;
+                for (int j = kids - 1; j >= k; --j) left += s.weight[j];
+                if (s.u[k] * left < s.weight[k]) first = min(first, k);
             }
             first = -wave_max_of(-first);
-            if (lane == 0) {
-                s_top = top;
-                s_part[0][0] = rest;
-                s_taken = first < GHD_MAX_M ? s_child[first] : -1;
-            }
+            if (lane == 0) s.taken = first < GHD_MAX_M ? s.child[first] : -1;
         }
         __syncthreads();
-        if (s_taken >= 0) {
-            if (tid == 0) out[node] = {s_taken, -1};
-            return;
+        if (s.taken >= 0) return finish(s.taken, -1);
+        if (tid < kids && in_vocabulary(a, s.token[tid])) atomicOr(&s.out[s.token[tid] >> 5], 1u << (s.token[tid] & 31));
+        __syncthreads();
+        const Weights weight(p.top, c);
+        const int token = draw_from_segments(a, s, p.part, segments, [&](int t) { return s.rejected(t) ? 0.0 : weight(row[t]); });
+        return finish(-1, token);
+    } else {
+        const Weights wp(p.top, c);
+        if (kids == 0) {
+            const int token = draw_from_segments(a, s, p.part, segments, [&](int t) { return wp(row[t]); });
+            return finish(-1, token);
         }
-        // the segment in which the sum passes u, then the place
-        const double goal = u_of(a.u[0]) * s_part[0][0];
-        __shared__ int s_seg;
-        __shared__ double s_before;
-        if (tid == 0) {
-            double sum = 0.0;
-            int at = -1;
-            s_seg = -1;
-            for (int s = 0; s < segments; ++s) {
-                const double w = mine[s].sum * weight_of(mine[s].top, s_top, c);
-                if (w > 0.0) {
-                    at = s;
-                    s_before = sum;
-                    if (sum + w > goal) break;
+        // After some rejections what is left is alpha (p - beta q)+ of the tokens not rejected, and what is left of q its other tokens:
+        // two sums over the row for each rejection.
+        const int qr = draft_row(a, node);
+        const float* q_row = a.q_logits + (size_t)qr * a.V;
+        const double cq = kLog2e / (double)a.q_temperature;
+        const First q = firsts[node];
+        const Weights wq(q.top_q, cq);
+        auto p_of = [&](int t) { return wp(row[t]) * p.one; };
+        auto q_of = [&](int t) { return wq(q_row[t]) * q.one_q; };
+        // A thread has every 512th token.  Of vocabularies up to 32768 it keeps the weights, 0 of what was rejected; what is left
+        // may be less than 32 bits' weights show: then they are worked out anew each time, as those of larger vocabularies are.
+        const bool small = a.V <= kKeep * kNodeThreads;
+        float keep_p[kKeep], keep_q[kKeep];
+        bool kept = false;
+        double alpha = 1.0, beta = 0.0, rest_q = q.one_q > 0.0 ? 1.0 : 0.0;
+        Rest first = {0.0, 0.0};                 // the lane's segment's, of what the first rejection leaves
+        int tried = 0, k = 0;
+        for (; k < kids; ++k) {
+            const int x = s.token[k];
+            if (!in_vocabulary(a, x)) continue;
+            const bool gone = twice(k);
+            const double px = gone ? 0.0 : fmax(alpha * (p_of(x) - beta * q_of(x)), 0.0), qx = gone || !(rest_q > 0.0) ? 0.0 : q_of(x) / rest_q;
+            if (s.u[k] * qx < px) break;
+            __syncthreads();                     // (the last round's bits and sums have been read)
+            if (tid == 0) s.out[x >> 5] |= 1u << (x & 31);
+            __syncthreads();
+            const double next = rest_q > 0.0 ? beta + 1.0 / (alpha * rest_q) : beta;
+            double all, all_q;
+            if (tried++ == 0 && rest_q > 0.0) {
+                if (lane < segments) first = rest[(size_t)node * segments + lane];
+                all = wave_sum(first.p);
+                all_q = wave_sum(first.q);
+            } else {
+                const bool shows = rest_q > 1e-25 && alpha < 1e25;
+                if (small && shows && !kept) {
+                    int me = tid;                // (here and now: otherwise all addresses would be kept, too)
+                    asm volatile("" : "+v"(me));
+#pragma unroll
+                    for (int i = 0; i < kKeep; ++i) {
+                        const int t = i * kNodeThreads + me, in = min(t, a.V - 1);
+                        keep_p[i] = row[in];
+                        keep_q[i] = q_row[in];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < kKeep; ++i) {
+                        const int t = i * kNodeThreads + me;
+                        const bool is = t < a.V && !s.rejected(min(t, a.V - 1));
+                        keep_p[i] = is ? wp.low(keep_p[i]) : 0.f;
+                        keep_q[i] = is ? wq.low(keep_q[i]) : 0.f;
+                        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                sum += w;
+                kept = small && shows;
+                double sp = 0.0, sq = 0.0;
+                if (kept) {
+                    // in weights against the maxima: p - (beta one_q / one) q, the factor in two parts, and sums of a few in 32 bits
+                    const double by = next * q.one_q / p.one;
+                    const float by_high = (float)by, by_low = (float)(by - (double)by_high);
+#pragma unroll
+                    for (int i0 = 0; i0 < kKeep; i0 += 8) {
+                        float some = 0.f, some_q = 0.f;
+#pragma unroll
+                        for (int i = i0; i < i0 + 8; ++i) {
+                            if (i * kNodeThreads + tid == x) keep_p[i] = keep_q[i] = 0.f;
+                            some += fmaxf(fmaf(-by_low, keep_q[i], fmaf(-by_high, keep_q[i], keep_p[i])), 0.f);
+                            some_q += keep_q[i];
+                        }
+                        sp += (double)some;
+                        sq += (double)some_q;
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    sp *= p.one;
+                    sq *= q.one_q;
+                } else {
+                    for (int t = tid; t < a.V; t += kNodeThreads) {
+                        if (s.rejected(t)) continue;
+                        const double qt = q_of(t);
+                        sp += fmax(p_of(t) - next * qt, 0.0);
+                        sq += qt;
+                    }
+                }
+                sp = wave_sum(sp);
+                sq = wave_sum(sq);
+                if (lane == 0) {
+                    s.part[0][wave] = sp;
+                    s.part[1][wave] = sq;
+                }
+                __syncthreads();
+                all = all_q = 0.0;
+                for (int v = 0; v < kNodeWaves; ++v) {
+                    all += s.part[0][v];
+                    all_q += s.part[1][v];
+                }
             }
-            s_seg = at;
+            if (all > 0.0) {
+                alpha = 1.0 / all;
+                beta = next;
+            }
+            rest_q = all_q;
         }
-        if (tid < kSegment / 32) s_out[tid] = 0;
-        __syncthreads();
-        if (s_seg < 0) {                         // no token has a weight
-            if (tid == 0) out[node] = {-1, -1};
-            return;
-        }
-        const int lo = s_seg * kSegment;
-        const float top = mine[s_seg].top;
-        const double factor = weight_of(top, s_top, c);
-        if (tid < kids && s_token[tid] >= lo && s_token[tid] < lo + kSegment)
-            atomicOr(&s_out[(s_token[tid] - lo) >> 5], 1u << ((s_token[tid] - lo) & 31));
-        __syncthreads();
-        // a thread has four neighbours
-        double w[4], sum = 0.0;
+        if (k < kids) return finish(s.child[k], -1);
+        auto left_of = [&](int t) { return s.rejected(t) ? 0.0 : fmax(p_of(t) - beta * q_of(t), 0.0); };
+        // sums of segments: none rejected, or one, they are there
+        double part = 0.0;
+        if (tried == 0 || beta == 0.0) {
+            part = p.part * p.one;
+        } else if (tried == 1) {
+            part = first.p;
+        } else if (kept) {
+            const double by = beta * q.one_q / p.one;
+            const float by_high = (float)by, by_low = (float)(by - (double)by_high);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int j = tid * 4 + e, t = lo + j;
-            w[e] = t < a.V && !(s_out[j >> 5] >> (j & 31) & 1) ? weight_of(row[t], top, c) * factor : 0.0;
-            sum += w[e];
-        }
-        double upto = sum;
-        for (int off = 1; off < 64; off *= 2) {
-            const double o = __shfl_up(upto, off);
-            if (lane >= off) upto += o;
-        }
-        if (lane == 63) s_part[1][wave] = upto;
-        __syncthreads();
-        double before = s_before + upto - sum;
-        for (int v = 0; v < wave; ++v) before += s_part[1][v];
-        int place = 0x7fffffff;
+            for (int v = 0; v < kKeep / kSide; ++v) {
+                float some = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            before += w[e];
-            if (w[e] > 0.0 && before > goal && place == 0x7fffffff) place = lo + tid * 4 + e;
+                for (int i = kSide * v; i < kSide * (v + 1); ++i) some += fmaxf(fmaf(-by_low, keep_q[i], fmaf(-by_high, keep_q[i], keep_p[i])), 0.f);
+                const double w = wave_sum((double)some * p.one);
+                if (lane == 0) s.sums[v][wave] = w;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __syncthreads();
+            if (lane < segments)
+                for (int i = 0; i < kNodeWaves; ++i) part += s.sums[lane][i];
+        } else {
+            for (int v = 0; v < segments; ++v) {
+                double w = 0.0;
+                for (int t = v * kSegment + tid; t < min((v + 1) * kSegment, a.V); t += kNodeThreads) w += left_of(t);
+                w = wave_sum(w);
+                __syncthreads();
+                if (lane == 0) s.part[0][wave] = w;
+                __syncthreads();
+                if (v == lane)
+                    for (int i = 0; i < kNodeWaves; ++i) part += s.part[0][i];
+            }
         }
-        place = -wave_max_of(-place);
-        if (lane == 0) s_last[wave] = place;
-        __syncthreads();
-        if (tid == 0) {
-            for (int v = 0; v < kNodeWaves; ++v) place = min(place, s_last[v]);
-            out[node] = {-1, place == 0x7fffffff ? mine[s_seg].last : place};
-        }
-        return;
+        return finish(-1, draw_from_segments(a, s, part, segments, left_of));
     }
-
-    // Drafts from probabilities: after some rejections what is left is alpha (p - beta q)+ of the tokens not rejected, and what is left of
-    // q its other tokens; one sum over the row for each rejection.
-    const int qr = a.q_row ? min(max(a.q_row[node], 0), a.q_rows - 1) : node;
-    const float* q_row = a.q_logits + (size_t)qr * a.V;
-    const Segment* drafts = seg + (size_t)(a.M + qr) * segments;
-    const double cq = 1.4426950408889634 / (double)a.q_temperature;
-    float top = -INFINITY, top_q = -INFINITY;
-    for (int s = 0; s < segments; ++s) {
-        top = fmaxf(top, mine[s].top);
-        top_q = fmaxf(top_q, drafts[s].top);
-    }
-    double sum = 0.0, sum_q = 0.0;
-    for (int s = 0; s < segments; ++s) {
-        sum += mine[s].sum * weight_of(mine[s].top, top, c);
-        sum_q += drafts[s].sum * weight_of(drafts[s].top, top_q, cq);
-    }
-    const double one = sum > 0.0 ? 1.0 / sum : 0.0, one_q = sum_q > 0.0 ? 1.0 / sum_q : 0.0;
-    auto p_of = [&](int t) { return weight_of(row[t], top, c) * one; };
-    auto q_of = [&](int t) { return weight_of(q_row[t], top_q, cq) * one_q; };
-    // tokens of a wavefront: neighbours, so that sums over wavefronts are sums up to a token
-    const int per = (a.V + kNodeThreads - 1) / kNodeThreads * 64, from = min(wave * per, a.V), to = min(from + per, a.V);
-    double alpha = 1.0, beta = 0.0, rest_q = sum_q > 0.0 ? 1.0 : 0.0, part = 0.0;
-    auto rejected = [&](int t, int k) {
-        bool is = false;
-        for (int j = 0; j < k; ++j) is = is || s_token[j] == t;
-        return is;
-    };
-    int k = 0;
-    for (; k < kids; ++k) {
-        const int x = s_token[k];
-        if (!there(x)) continue;
-        const bool gone = rejected(x, k);
-        const double px = gone ? 0.0 : fmax(alpha * (p_of(x) - beta * q_of(x)), 0.0), qx = gone || !(rest_q > 0.0) ? 0.0 : q_of(x) / rest_q;
-        if (u_of(a.u[s_child[k]]) * qx < px) break;
-        const double next = rest_q > 0.0 ? beta + 1.0 / (alpha * rest_q) : beta;
-        double s = 0.0, r = 0.0;
-        for (int t = from + lane; t < to; t += 64) {
-            if (rejected(t, k + 1)) continue;
-            const double q = q_of(t);
-            s += fmax(p_of(t) - next * q, 0.0);
-            r += q;
-        }
-        s = wave_sum(s);
-        r = wave_sum(r);
-        __syncthreads();                         // (the last round's sums have been read)
-        if (lane == 0) {
-            s_part[0][wave] = s;
-            s_part[1][wave] = r;
-        }
-        __syncthreads();
-        double all = 0.0, all_q = 0.0;
-        for (int v = 0; v < kNodeWaves; ++v) {
-            all += s_part[0][v];
-            all_q += s_part[1][v];
-        }
-        if (all > 0.0) {
-            alpha = 1.0 / all;
-            beta = next;
-        }
-        rest_q = all_q;
-    }
-    if (k < kids) {
-        if (tid == 0) out[node] = {s_child[k], -1};
-        return;
-    }
-    // the draw
-    auto left_of = [&](int t) { return rejected(t, kids) ? 0.0 : fmax(p_of(t) - beta * q_of(t), 0.0); };
-    int last = -1;
-    for (int t = from + lane; t < to; t += 64) {
-        const double w = left_of(t);
-        part += w;
-        if (w > 0.0) last = t;
-    }
-    part = wave_sum(part);
-    last = wave_max_of(last);
-    __syncthreads();
-    if (lane == 0) {
-        s_part[2][wave] = part;
-        s_last[wave] = last;
-    }
-    __syncthreads();
-    double total = 0.0, before = 0.0;
-    int at = -1, end = -1;
-    for (int v = 0; v < kNodeWaves; ++v) {
-        total += s_part[2][v];
-        end = max(end, s_last[v]);
-    }
-    const double goal = u_of(a.u[0]) * total;
-    double so_far = 0.0;
-    for (int v = 0; v < kNodeWaves; ++v) {
-        if (at < 0 && so_far + s_part[2][v] > goal) {
-            at = v;
-            before = so_far;
-        }
-        so_far += s_part[2][v];
-    }
-    if (at < 0) {
-        if (tid == 0) out[node] = {-1, end};
-        return;
-    }
-    if (wave != at) return;
-    for (int t0 = from; t0 < to; t0 += 64) {
-        const double w = t0 + lane < to ? left_of(t0 + lane) : 0.0;
-        double upto = w;
-        for (int off = 1; off < 64; off *= 2) {
-            const double o = __shfl_up(upto, off);
-            if (lane >= off) upto += o;
-        }
-        const uint64_t over = __ballot(w > 0.0 && before + upto > goal);
-        if (over) {
-            if (lane == 0) out[node] = {-1, t0 + (int)__builtin_ctzll(over)};
-            return;
-        }
-        before += __shfl(upto, 63);
-    }
-    if (lane == 0) out[node] = {-1, last};       // (the wavefront's own sum was larger by a rounding)
 }
 
 __global__ __launch_bounds__(GHD_MAX_M) void k_sample_walk(const NodeResult* __restrict__ nodes, int M, int32_t* __restrict__ res)
@@ -403,22 +584,35 @@ __global__ __launch_bounds__(GHD_MAX_M) void k_sample_walk(const NodeResult* __r
 }
 
 static int sample_segments(int V) { return ceil_div(V, kSegment); }
-static size_t sample_nodes_at(int V) { return align_up((size_t)2 * GHD_MAX_M * sample_segments(V) * sizeof(Segment), 256); }
+static size_t sample_rest_at(int V) { return align_up((size_t)2 * GHD_MAX_M * sample_segments(V) * sizeof(Segment), 256); }
+static size_t sample_first_at(int V) { return sample_rest_at(V) + align_up((size_t)GHD_MAX_M * sample_segments(V) * sizeof(Rest), 256); }
+static size_t sample_nodes_at(int V) { return sample_first_at(V) + align_up(GHD_MAX_M * sizeof(First), 256); }
 
 size_t accept_sampled_bytes(int M, int V) { return sample_nodes_at(V) + align_up(GHD_MAX_M * sizeof(NodeResult), 256); }
 
 ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
 {
-    static_assert(kNodeThreads * 4 == kSegment, "a thread has four tokens of a segment");
+    static_assert(kNodeThreads * kSide == kSegment && kKeep % kSide == 0 && kMaxSegments == 64, "a segment's tokens are dealt evenly, a lane has a segment of a row");
     Segment* seg = (Segment*)ws;
+    Rest* rest = (Rest*)((char*)ws + sample_rest_at(a.V));
+    First* firsts = (First*)((char*)ws + sample_first_at(a.V));
     NodeResult* nodes = (NodeResult*)((char*)ws + sample_nodes_at(a.V));
     const int segments = sample_segments(a.V);
     hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a, seg);
     ghd_status s = check_launch();
     if (s) return s;
-    hipLaunchKernelGGL(k_sample_nodes, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, segments, nodes);
-    s = check_launch();
-    if (s) return s;
+    if (a.q_logits) {
+        hipLaunchKernelGGL(k_sample_first, dim3(a.M), dim3(64), 0, st, a, (const Segment*)seg, segments, firsts);
+        if ((s = check_launch())) return s;
+        hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, (const Segment*)seg, (const First*)firsts, rest);
+        if ((s = check_launch())) return s;
+        hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)firsts,
+                           (const Rest*)rest, segments, nodes);
+    } else {
+        hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)nullptr,
+                           (const Rest*)nullptr, segments, nodes);
+    }
+    if ((s = check_launch())) return s;
     hipLaunchKernelGGL(k_sample_walk, dim3(1), dim3(GHD_MAX_M), 0, st, (const NodeResult*)nodes, a.M, a.res);
     return check_launch();
 }

@@ -35,10 +35,11 @@ struct SelectArgs {
     Bounds bounds;
     uint32_t* keys;                  // workspace: [nkv][M][n rounded up to 4]
     int M, nkv, rep, n;
+    bool zero;                       // (the launch's) the words have to be zeros when the picks begin
     int lo, hi, keep;                // blocks [0, lo) and [hi, n) are taken, and `keep` of those between
 };
 static inline size_t select_bytes(int M, int n, int nkv) { return align_up((size_t)nkv * M * ((n + 3) & ~3) * 4, 256) + 256; }
-ghd_status launch_block_select(const SelectArgs& a, int d, hipStream_t st);
+ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st);
 
 struct SparseArgs {
     half_t* out;

@@ -13,93 +13,134 @@ namespace ghd {
 
 typedef uint32_t uint4_ __attribute__((ext_vector_type(4)));
 
-constexpr int kSparseWaves = 4, kSparseThreads = kSparseWaves * 64;
-constexpr int kList = 1024;                      // blocks of a workgroup's list: the host divides a head's so that they fit
-
 // How a launch is divided: rows in `blocks` blocks, what a block of rows reads in `splits` parts.
 struct SparseCut {
     int rows, blocks, splits;                    // rows: tiles of 16 in a block
 };
 
-// The blocks that tokens i0 .. i1 (at most 64 of them) have selected, then the `tail` that all read: [lo, hi) of them, in order, to the
-// list, with a bit for each of the tokens.  Returns how many.
+constexpr int kList = 1024;                      // blocks of a workgroup's list: the host divides a head's so that they fit
 struct SparseList {
-    uint64_t bits[kList];
+    uint64_t bits[kList];                        // a bit for each of the workgroup's tokens
     int32_t block[kList];
-    int32_t part[kSparseWaves];
+    int32_t part[8];
 };
-__device__ __forceinline__ int sparse_list(const SparseArgs& a, SparseList& s, int head, int i0, int i1, int tail, int split, int splits)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, words = (a.M + 63) / 64, n = a.n;
-    const int w0 = i0 >> 6, w1 = i1 >> 6, shift = i0 & 63;
-    const uint64_t keep = i1 - i0 >= 63 ? ~0ull : (1ull << (i1 - i0 + 1)) - 1;
-    const uint64_t* sel = a.sel + (size_t)head * words * n;
-    auto bits_of = [&](int b) {
-        uint64_t x = sel[(size_t)w0 * n + b] >> shift;
-        if (w1 != w0) x |= sel[(size_t)w1 * n + b] << (64 - shift);      // (w1 != w0: shift is not 0)
+
+// What a workgroup reads: the blocks that its tokens i0 .. i1 (at most 64) have selected, then the `tail` that all read.  Words of
+// the selection are asked for when a workgroup begins; every workgroup of a row block puts the blocks in the same order,
+// a thread's one behind the other, and takes its share.
+template <int THREADS>
+struct SparseScan {
+    static constexpr int kKept = 4;              // words of a thread that stay in registers
+    const uint64_t *lo, *hi;
+    uint64_t keep, word[kKept];
+    int n, shift;
+    __device__ __forceinline__ SparseScan(const SparseArgs& a, int head, int i0, int i1) : n(a.n), shift(i0 & 63)
+    {
+        const int words = (a.M + 63) / 64;
+        lo = a.sel + ((size_t)head * words + (i0 >> 6)) * n;
+        hi = i1 >> 6 != i0 >> 6 ? lo + n : nullptr;      // (then shift is not 0)
+        keep = i1 - i0 >= 63 ? ~0ull : (1ull << (i1 - i0 + 1)) - 1;
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) {
+            const int b = threadIdx.x + j * THREADS;
+            word[j] = b < n ? at(b) : 0;
+        }
+    }
+    __device__ __forceinline__ uint64_t at(int b) const
+    {
+        uint64_t x = lo[b] >> shift;
+        if (hi) x |= hi[b] << (64 - shift);
         return x & keep;
-    };
-    // how many there are: a thread counts neighbours
-    const int per = (n + kSparseThreads - 1) / kSparseThreads, b0 = min(tid * per, n), b1 = min(b0 + per, n);
-    int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += bits_of(b) != 0;
-    int before = mine;
-    for (int off = 1; off < 64; off *= 2) {
-        const int o = __shfl_up(before, off);
-        if (lane >= off) before += o;
     }
-    if (lane == 63) s.part[wave] = before;
-    __syncthreads();
-    before -= mine;
-    int all = 0;
-    for (int w = 0; w < kSparseWaves; ++w) {
-        if (w < wave) before += s.part[w];
-        all += s.part[w];
-    }
-    const int total = all + tail, lo = (int)((int64_t)total * split / splits), hi = (int)((int64_t)total * (split + 1) / splits);
-    if (before < hi && before + mine > lo)
-        for (int b = b0; b < b1; ++b) {
-            const uint64_t x = bits_of(b);
-            if (x == 0) continue;
-            if (before >= lo && before < hi) {
-                s.bits[before - lo] = x;
-                s.block[before - lo] = b;
+    // shares of `splits` to the list; returns how many blocks this one has, and how many come before the tail's in all
+    __device__ __forceinline__ int list(SparseList& s, int tail, int split, int splits, int& before_tail) const
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) mine += word[j] != 0;
+        for (int b = tid + kKept * THREADS; b < n; b += THREADS) mine += at(b) != 0;
+        int before = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const int o = __shfl_up(before, off);
+            if (lane >= off) before += o;
+        }
+        if (lane == 63) s.part[wave] = before;
+        __syncthreads();
+        before -= mine;
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            const int c = s.part[w];
+            if (w < wave) before += c;
+            all += c;
+        }
+        const int total = all + tail, first = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
+        auto put = [&](int b, uint64_t x) {
+            if (x == 0) return;
+            if (before >= first && before < end) {
+                s.bits[before - first] = x;
+                s.block[before - first] = b;
             }
             ++before;
+        };
+        if (mine != 0 && before < end && before + mine > first) {
+#pragma unroll
+            for (int j = 0; j < kKept; ++j) put(tid + j * THREADS, word[j]);
+            for (int b = tid + kKept * THREADS; b < n; b += THREADS) put(b, at(b));
         }
-    if (tid < tail && all + tid >= lo && all + tid < hi) {
-        s.bits[all + tid - lo] = 0;
-        s.block[all + tid - lo] = n + tid;
+        if (tid < tail && all + tid >= first && all + tid < end) {
+            s.bits[all + tid - first] = 0;
+            s.block[all + tid - first] = n + tid;
+        }
+        before_tail = all - first;
+        return end - first;
     }
-    __syncthreads();
-    return hi - lo;
-}
+};
 
-// 32 keys, as a wavefront's operands: operand row r of half h is key 8 (r / 4) + 4 h + r % 4, so that a lane's 8 scores of a column
-// are those of keys 8 g .. 8 g + 7, the probabilities it holds in the second product.
+// 32 keys as a wavefront's operands: operand row r of half h is key 8 (r / 4) + 4 h + r % 4, so that a lane's 8 scores of a column
+// are those of keys 8 g .. 8 g + 7, the probabilities it holds in the second product.  A unit's rows lie at a uniform address, a
+// lane's share at a 32-bit offset.
 template <int D>
 struct SparseUnit {
     half8 k[2][D / 32], v[D / 16];
-    __device__ __forceinline__ void load(const SparseArgs& a, int head, int key0, int lane)
+    // (there: how many of the unit's keys there are; others are read as the last of them)
+    __device__ __forceinline__ void load_k(const SparseArgs& a, int head, int key0, int there, int lane)
     {
-        const int g = lane >> 4, col = lane & 15, total = a.kv_len + a.M;
-        const half_t* kp = a.k + head * a.k_head + g * 8;
+        const int key = 8 * ((lane & 15) >> 2) + (lane & 3);
+        const char* base = (const char*)(a.k + head * a.k_head + key0 * a.k_tok);
+        if (there >= 32) {
+            const uint32_t at = (uint32_t)key * (uint32_t)(2 * a.k_tok) + (lane >> 4) * 16;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s)
-                k[h][s] = *(const half8*)(kp + (int64_t)min(key0 + 8 * (col >> 2) + 4 * h + (col & 3), total - 1) * a.k_tok + s * 32);
-        const half_t* vp = a.v + head * a.v_head + min(key0 + 8 * g, (total - 1) & ~7);
+                for (int s = 0; s < D / 32; ++s) k[h][s] = *(const half8*)(base + h * 8 * a.k_tok + s * 64 + at);
+        } else {
 #pragma unroll
-        for (int ct = 0; ct < D / 16; ++ct) v[ct] = *(const half8*)(vp + (int64_t)(ct * 16 + col) * a.v_ch);
-        if (key0 + 32 <= total) return;
-        // rows that are not there may hold anything, and 0 times anything is no 0
-        const int there = total - key0 - 8 * g;
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t at = (uint32_t)min(key + 4 * h, there - 1) * (uint32_t)(2 * a.k_tok) + (lane >> 4) * 16;
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) k[h][s] = *(const half8*)(base + s * 64 + at);
+            }
+        }
+    }
+    __device__ __forceinline__ void load_v(const SparseArgs& a, int head, int key0, int there, int lane)
+    {
+        const char* base = (const char*)(a.v + head * a.v_head + key0);
+        const uint32_t at = (uint32_t)(lane & 15) * (uint32_t)(2 * a.v_ch) + min(8 * (lane >> 4), (there - 1) & ~7) * 2;
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) v[ct] = *(const half8*)(base + (int64_t)ct * 32 * a.v_ch + at);
+    }
+    // Rows that are not there may hold anything, and 0 times anything is no 0
+    __device__ __forceinline__ void clean(int there, int lane)
+    {
+        const int mine = there - 8 * (lane >> 4);
 #pragma unroll
         for (int ct = 0; ct < D / 16; ++ct) {
             uint4_ w = __builtin_bit_cast(uint4_, v[ct]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) w[p] &= (there > 2 * p ? 0xffffu : 0u) | (there > 2 * p + 1 ? 0xffff0000u : 0u);
+            for (int p = 0; p < 4; ++p) w[p] &= (mine > 2 * p ? 0xffffu : 0u) | (mine > 2 * p + 1 ? 0xffff0000u : 0u);
             v[ct] = __builtin_bit_cast(half8, w);
         }
     }
@@ -108,96 +149,47 @@ struct SparseUnit {
 // A row tile's state over the keys so far.
 template <int D>
 struct SparseState {
-    floatx4 o[D / 16], l;              // l: the sum of the rounded probabilities, by a product with ones; four times the same
-    float m;
+    floatx4 o[D / 16];
+    float m, l;                        // l: the sum of the lane's own rounded probabilities
     __device__ __forceinline__ void clear()
     {
         m = -INFINITY;
-        l = (floatx4){0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
 #pragma unroll
         for (int ct = 0; ct < D / 16; ++ct) o[ct] = (floatx4){0.f, 0.f, 0.f, 0.f};
     }
     // scores (of the lane's 8 keys, c makes powers of two of them) to probabilities
     __device__ __forceinline__ half8 powers(const floatx4 (&s)[2], float c)
     {
+        // (of the maximum that NaN passes through: fmaxf first takes every score through an instruction that quiets NaN)
         float top = s[0][0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[e >> 2][e & 3]);
         top = max_over_groups(top) * c;
-        if (__ballot(top > m + 8.f || m == -INFINITY)) {
-            const float now = top > m + 8.f || m == -INFINITY ? fmaxf(m, top) : m, r = m == now ? 1.f : fast_exp2(m - now);
+        // (m is minus infinity until a key is seen; m + 8 then is, too)
+        if (__ballot(top > m + 8.f)) {
+            const float now = top > m + 8.f ? top : m, r = m == now ? 1.f : fast_exp2(m - now);
             l *= r;
 #pragma unroll
             for (int ct = 0; ct < D / 16; ++ct) o[ct] *= r;
             m = now;
         }
         const float off = m == -INFINITY ? 0.f : -m;
-        half8 p;
+        half2_ p[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (half_t)fast_exp2(fmaf(s[e >> 2][e & 3], c, off));
+        for (int e = 0; e < 4; ++e) {
+            floatx2 x;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) x[u] = fast_exp2(fmaf(s[e >> 1][2 * (e & 1) + u], c, off));
+            p[e] = __builtin_convertvector(x, half2_);
+        }
+        const half8 all = {p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
         const half_t one = (half_t)1.f;
-        l = __builtin_amdgcn_mfma_f32_16x16x32_f16((half8){one, one, one, one, one, one, one, one}, p, l, 0, 0, 0);
-        return p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l = __builtin_amdgcn_fdot2(p[e], (half2_){one, one}, l, false);
+        return all;
     }
 };
-
-// The rows of a workgroup, and which of a unit's keys a row sees.
-struct SparseRows {
-    int row0, R, i0;
-    __device__ __forceinline__ int token(const SparseArgs& a, int r, int col) const { return min((row0 + r * 16 + col) / a.rep, a.M - 1); }
-    // a bit for each of the lane's 8 keys
-    __device__ __forceinline__ uint32_t sees(const SparseArgs& a, const SparseList& list, const uint64_t* s_mask, int entry, int key0, int r,
-                                             int lane) const
-    {
-        const int i = token(a, r, lane & 15);
-        if (list.block[entry] < a.n) return list.bits[entry] >> (i - i0) & 1 ? 0xffu : 0u;
-        return seen_keys((const uint32_t*)(s_mask + 2 * i), key0 + (lane >> 4) * 8, a.kv_len, a.kv_len + a.M);
-    }
-};
-
-// One unit into the states.  PLAIN: every row meets all of the unit's values, those that it does not see with the
-// probability 0; an infinity or NaN there is no 0 then.  Otherwise a row takes the values it sees, one by one.
-template <int D, int RT, bool PLAIN>
-__device__ __forceinline__ void sparse_unit(const SparseArgs& a, const SparseList& list, const uint64_t* s_mask, const SparseRows& rows, int head,
-                                            const half8* s_q, SparseState<D> (&st)[RT], const SparseUnit<D>& u, int entry, int key0, float c,
-                                            int lane)
-{
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        floatx4 s[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
-                s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(u.k[h][ks], s_q[(r * (D / 32) + ks) * 64 + lane], s[h], 0, 0, 0);
-        }
-        const uint32_t see = rows.sees(a, list, s_mask, entry, key0, r, lane);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = see >> e & 1 ? s[e >> 2][e & 3] : -INFINITY;
-        const half8 p = st[r].powers(s, c);
-        if constexpr (PLAIN) {
-#pragma unroll
-            for (int ct = 0; ct < D / 16; ++ct) st[r].o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(u.v[ct], p, st[r].o[ct], 0, 0, 0);
-        } else {
-            const int col = lane & 15, g = lane >> 4, total = a.kv_len + a.M;
-            for (int key = 0; key < 32; ++key) {
-                const int from = col + 16 * (key >> 3);
-                float mine = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) mine = (key & 7) == e ? (float)p[e] : mine;
-                const float pk = __shfl(mine, from);
-                const bool seen = __shfl((int)see, from) >> (key & 7) & 1;
-                if (!seen) continue;
-                const half_t* vp = a.v + head * a.v_head + min(key0 + key, total - 1) + (int64_t)(4 * g) * a.v_ch;
-#pragma unroll
-                for (int ct = 0; ct < D / 16; ++ct)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) st[r].o[ct][e] += pk * (float)vp[(int64_t)(ct * 16 + e) * a.v_ch];
-            }
-        }
-    }
-}
 
 // a row's output from the sums and their divisor; a row that sees no key gives zeros
 __device__ __forceinline__ void sparse_out(const SparseArgs& a, int head, int row, int d, int ct, int g, floatx4 o, float l)
@@ -211,45 +203,138 @@ __device__ __forceinline__ void sparse_out(const SparseArgs& a, int head, int ro
 }
 
 template <int D, int RT>
-__global__ __launch_bounds__(kSparseThreads) void k_sparse_attention(SparseArgs a, SparseCut cut)
+struct SparseShape {
+    static constexpr int kWaves = RT == 1 ? 4 : 8, kThreads = kWaves * 64, CT = D / 16, KS = D / 32, kFrags = RT * CT,
+                         kRound = kFrags < 16 ? kFrags : 16;           // fragments that meet at a time
+    static constexpr size_t kLds = (size_t)kWaves * kRound * 1024;      // queries first, states at the end
+};
+
+template <int D, int RT>
+__global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse_attention(SparseArgs a, SparseCut cut)
 {
-    constexpr int CT = D / 16, KS = D / 32, kRound = 8;
+    typedef SparseShape<D, RT> S;
+    constexpr int CT = S::CT, KS = S::KS, W = S::kWaves;
     __shared__ SparseList list;
     __shared__ uint64_t s_mask[2 * GHD_MAX_M];
-    __shared__ half8 s_q[RT * KS * 64];
-    __shared__ floatx2 s_ml[kSparseWaves][RT * 16];
-    __shared__ floatx4 s_o[kSparseWaves][kRound][64];
+    __shared__ floatx2 s_ml[W][RT * 16];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    const int split = blockIdx.x, block = blockIdx.y, head = blockIdx.z;
-    SparseRows rows;
-    rows.row0 = block * RT * 16;
-    rows.R = a.M * a.rep;
-    rows.i0 = rows.row0 / a.rep;
-    const int tail0 = a.n * kBlock, tail = (a.kv_len + a.M - tail0 + kBlock - 1) / kBlock;
-    if (wave == 0 && a.parent)
-        store_masks(tree_nodes<2, true>(a.parent[min(lane, a.M - 1)], a.parent[min(lane + 64, a.M - 1)], a.M, lane), a.M, lane, s_mask);
-    if (!a.parent)
-        for (int e = threadIdx.x; e < 2 * a.M; e += kSparseThreads) s_mask[e] = a.mask[e];
-    for (int f = wave; f < RT * KS; f += kSparseWaves) {
-        const int row = rows.row0 + f / KS * 16 + col, token = row / a.rep;
-        half8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row < rows.R) x = *(const half8*)(a.q + ((size_t)token * a.nh + head * a.rep + row - token * a.rep) * D + f % KS * 32 + g * 8);
-        s_q[f * 64 + lane] = a.scale < 0.f ? -x : x;
+    // 8 XCDs by blocks, by parts in eights: the row blocks of a part of a head's keys share an L2
+    const int item = blockIdx.y * 8 + (blockIdx.x & 7);
+    if (item >= a.nkv * cut.splits) return;
+    const int block = blockIdx.x >> 3, head = item / cut.splits, split = item - head * cut.splits;
+    const int row0 = block * RT * 16, R = a.M * a.rep, i0 = row0 / a.rep, i1 = min((row0 + RT * 16 - 1) / a.rep, a.M - 1);
+    const int total = a.kv_len + a.M, tail = (total - a.n * kBlock + kBlock - 1) / kBlock;
+    const SparseScan<S::kThreads> scan(a, head, i0, i1);
+    constexpr int kMine = (RT * KS + W - 1) / W;                   // operands of q that a wavefront brings
+    half8 x[kMine];
+#pragma unroll
+    for (int f = 0; f < kMine; ++f) {
+        const int frag = f * W + wave, row = row0 + frag / KS * 16 + col, token = row / a.rep;
+        x[f] = (half8){0, 0, 0, 0, 0, 0, 0, 0};
+        if (frag < RT * KS && row < R)
+            x[f] = *(const half8*)(a.q + ((size_t)token * a.nh + head * a.rep + row - token * a.rep) * D + frag % KS * 32 + g * 8);
     }
-    const int count = sparse_list(a, list, head, rows.i0, min((rows.row0 + RT * 16 - 1) / a.rep, a.M - 1), tail, split, cut.splits);
+    int up0 = 0, up1 = 0;
+    if (wave == 0 && a.parent) {
+        up0 = a.parent[min(lane, a.M - 1)];
+        up1 = a.parent[min(lane + 64, a.M - 1)];
+    }
+    int before_tail;
+    const int count = scan.list(list, tail, split, cut.splits, before_tail);
+    if (before_tail < count) {                                     // it has some of the rows behind the blocks
+        if (!a.parent)
+            for (int e = threadIdx.x; e < 2 * a.M; e += S::kThreads) s_mask[e] = a.mask[e];
+        else if (wave == 0)
+            store_masks(tree_nodes<2, true>(up0, up1, a.M, lane), a.M, lane, s_mask);
+    }
+#pragma unroll
+    for (int f = 0; f < kMine; ++f)
+        if (f * W + wave < RT * KS) *(half8*)(lds + (f * W + wave) * 1024 + lane * 16) = a.scale < 0.f ? -x[f] : x[f];
+    __syncthreads();
+    auto query = [&](int r, int s) { return *(const half8*)(lds + (r * KS + s) * 1024 + lane * 16); };
     // scores to powers of two; above 0, so that minus infinity stays that
     const float c = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
-    SparseState<D> st[RT];
+    uint32_t tokens = 0;                                           // of a lane's columns, 8 bits each
+    auto token = [&](int r) { return (int)(tokens >> 8 * r & 255); };
+    uint64_t tile_bits[RT];                                        // of a tile's tokens
 #pragma unroll
-    for (int r = 0; r < RT; ++r) st[r].clear();
-    auto key_of = [&](int u) { return list.block[u >> 1] * kBlock + (u & 1) * 32; };
+    for (int r = 0; r < RT; ++r) {
+        tokens |= (uint32_t)min((row0 + r * 16 + col) / a.rep, a.M - 1) << 8 * r;
+        const int from = (row0 + r * 16) / a.rep - i0, to = min((row0 + r * 16 + 15) / a.rep, a.M - 1) - i0;
+        tile_bits[r] = from > to ? 0 : (to - from >= 63 ? ~0ull : (1ull << (to - from + 1)) - 1) << from;
+    }
+    SparseState<D> st[RT];
+    const int units = 2 * count;
+    auto key_of = [&](int u) { return __builtin_amdgcn_readfirstlane(list.block[u >> 1]) * kBlock + (u & 1) * 32; };
+    // One pass over the wavefront's units.  PLAIN: every row meets all of a unit's values, those that it does not see with
+    // the probability 0; an infinity or NaN there is no 0 then.  Otherwise a row takes the values that it sees one by one.
     auto pass = [&](auto plain) {
-        for (int u = wave; u < 2 * count; u += kSparseWaves) {
-            const int key0 = key_of(u);
-            if (key0 >= a.kv_len + a.M) continue;
-            SparseUnit<D> unit;
-            unit.load(a, head, key0, lane);
-            sparse_unit<D, RT, decltype(plain)::value>(a, list, s_mask, rows, head, s_q, st, unit, u >> 1, key0, c, lane);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) st[r].clear();
+        int u = wave;
+        if (u >= units) return;
+        SparseUnit<D> unit;
+        int key0 = key_of(u);
+        unit.load_k(a, head, key0, max(1, min(32, total - key0)), lane);
+        unit.load_v(a, head, key0, max(1, min(32, total - key0)), lane);
+        for (;;) {
+            const int next = u + W < units ? u + W : u, next0 = key_of(next), there = total - key0;
+            const int next_there = max(1, min(32, total - next0));
+            const bool rest = key0 >= a.n * kBlock;                // behind the blocks
+            const uint64_t bits = rest ? ~0ull : ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(list.bits[u >> 1] >> 32)) << 32) |
+                                                     (uint32_t)__builtin_amdgcn_readfirstlane((int)list.bits[u >> 1]);
+            if (there < 32) unit.clean(there, lane);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const bool met = (bits & tile_bits[r]) != 0;
+                half8 p;
+                uint32_t see = 0;
+                if (met) {
+                    floatx4 s[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks)
+                            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(unit.k[h][ks], query(r, ks), s[h], 0, 0, 0);
+                    }
+                    see = rest ? seen_keys((const uint32_t*)(s_mask + 2 * token(r)), key0 + g * 8, a.kv_len, total)
+                               : bits >> (token(r) - i0) & 1 ? 0xffu : 0u;
+                    if (rest || (bits & tile_bits[r]) != tile_bits[r])
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = see >> e & 1 ? s[e >> 2][e & 3] : -INFINITY;
+                    p = st[r].powers(s, c);
+                }
+                if (r == RT - 1) unit.load_k(a, head, next0, next_there, lane);
+                if (!met) continue;
+                if constexpr (decltype(plain)::value) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) st[r].o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(unit.v[ct], p, st[r].o[ct], 0, 0, 0);
+                } else {
+#pragma unroll 1
+                    for (int key = 0; key < 32; ++key) {
+                        const int from = col + 16 * (key >> 3);
+                        float mine = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mine = (key & 7) == e ? (float)p[e] : mine;
+                        const float pk = __shfl(mine, from);
+                        if (__shfl((int)see, from) >> (key & 7) & 1) {
+                            const half_t* vp = a.v + head * a.v_head + min(key0 + key, total - 1) + (int64_t)(4 * g) * a.v_ch;
+#pragma unroll
+                            for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) st[r].o[ct][e] += pk * (float)vp[(int64_t)(ct * 16 + e) * a.v_ch];
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                    }
+                }
+            }
+            if (next == u) break;
+            unit.load_v(a, head, next0, next_there, lane);
+            u = next;
+            key0 = next0;
         }
     };
     pass(std::true_type{});
@@ -260,71 +345,117 @@ __global__ __launch_bounds__(kSparseThreads) void k_sparse_attention(SparseArgs 
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(st[r].o[ct][e]) < INFINITY);
-    if (__ballot(odd)) {
+    if (__builtin_expect(__ballot(odd) != 0, 0)) pass(std::false_type{});
+    // the wavefronts' states meet in LDS, some fragments at a time, each added up by one wavefront
 #pragma unroll
-        for (int r = 0; r < RT; ++r) st[r].clear();
-        pass(std::false_type{});
+    for (int r = 0; r < RT; ++r) {
+        const float l = sum_over_groups(st[r].l);
+        if (g == 0) s_ml[wave][r * 16 + col] = (floatx2){st[r].m, l};
     }
-    // the wavefronts' states meet in LDS, some fragments at a time
-    if (g == 0)
+    const size_t unit0 = (((size_t)head * cut.blocks + block) * cut.splits + split) * RT;
+    floatx4* const part = (floatx4*)lds + lane;                    // [wave][fragment][64]
 #pragma unroll
-        for (int r = 0; r < RT; ++r) s_ml[wave][r * 16 + col] = (floatx2){st[r].m, st[r].l[0]};
-    const size_t unit = (((size_t)head * cut.blocks + block) * cut.splits + split) * RT;
-#pragma unroll
-    for (int f0 = 0; f0 < RT * CT; f0 += kRound) {
+    for (int f0 = 0; f0 < S::kFrags; f0 += S::kRound) {
         __syncthreads();
 #pragma unroll
-        for (int f = 0; f < kRound && f0 + f < RT * CT; ++f) s_o[wave][f][lane] = st[(f0 + f) / CT].o[(f0 + f) % CT];
+        for (int f = f0; f < f0 + S::kRound && f < S::kFrags; ++f) part[(wave * S::kRound + f - f0) * 64] = st[f / CT].o[f % CT];
         __syncthreads();
-        for (int f = f0 + wave; f < f0 + kRound && f < RT * CT; f += kSparseWaves) {
-            const int r = f / CT, ct = f % CT, row = rows.row0 + r * 16 + col;
+#pragma unroll 2
+        for (int e = wave; e < S::kRound && f0 + e < S::kFrags; e += W) {
+            const int f = f0 + e, r = f / CT, ct = f % CT, row = row0 + r * 16 + col;
             float m = -INFINITY, l = 0.f;
+            floatx2 ml[W];
             floatx4 o = {0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < kSparseWaves; ++w) m = fmaxf(m, s_ml[w][r * 16 + col][0]);
-            for (int w = 0; w < kSparseWaves; ++w) {
-                const floatx2 ml = s_ml[w][r * 16 + col];
-                const float by = fast_exp2(ml[0] - (m == -INFINITY ? 0.f : m));
-                l += ml[1] * by;
-                o += s_o[w][f - f0][lane] * by;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                ml[w] = s_ml[w][r * 16 + col];
+                m = fmaxf(m, ml[w][0]);
             }
+            const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float by = fast_exp2(ml[w][0] - off);
+                l += ml[w][1] * by;
+                o += part[(w * S::kRound + e) * 64] * by;
+            }
+            if (row >= R) continue;
             if (cut.splits > 1) {
-                ((floatx4*)a.o_part)[((unit + r) * CT + ct) * 64 + lane] = o;
-                if (ct == 0 && g == 0) ((floatx2*)a.ml_part)[(unit + r) * 16 + col] = (floatx2){m, l};
-            } else if (row < rows.R) {
+                ((floatx4*)a.o_part)[((unit0 + r) * CT + ct) * 64 + lane] = o;
+                if (ct == 0 && g == 0) ((floatx2*)a.ml_part)[(unit0 + r) * 16 + col] = (floatx2){m, l};
+            } else {
                 sparse_out(a, head, row, D, ct, g, o, l);
             }
         }
     }
 }
 
-// Parts to rows: a wavefront has a fragment, 16 channels by 16 rows, and its parts in order.
+// Parts to rows: four wavefronts take the parts of a fragment, 16 channels by 16 rows, in turn, eight requests at a time.
 template <int D>
 __global__ __launch_bounds__(256) void k_sparse_join(SparseArgs a, SparseCut cut)
 {
-    constexpr int CT = D / 16;
-    const int lane = threadIdx.x & 63, f = blockIdx.x * 4 + (threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    const int ct = f % CT, rt = f / CT, head = blockIdx.z, block = blockIdx.y, row = (block * cut.rows + rt) * 16 + col;
-    if (rt >= cut.rows) return;
+    constexpr int CT = D / 16, kAt = 8;
+    __shared__ floatx4 s_o[4][64];
+    __shared__ floatx2 s_ml[4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    const int ct = blockIdx.x % CT, rt = blockIdx.x / CT, block = blockIdx.y, head = blockIdx.z, row = (block * cut.rows + rt) * 16 + col;
+    if ((block * cut.rows + rt) * 16 >= a.M * a.rep) return;
+    const bool is = row < a.M * a.rep;                             // (no part has written the others)
     const size_t unit0 = ((size_t)head * cut.blocks + block) * cut.splits;
     float m = -INFINITY, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < cut.splits; ++p) {
-        const size_t unit = (unit0 + p) * cut.rows + rt;
-        const floatx2 ml = ((const floatx2*)a.ml_part)[unit * 16 + col];
-        const floatx4 v = ((const floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane];
-        const float now = fmaxf(m, ml[0]), off = now == -INFINITY ? 0.f : now, was = fast_exp2(m - off), by = fast_exp2(ml[0] - off);
-        l = l * was + ml[1] * by;
-        o = o * was + v * by;
-        m = now;
+    for (int p0 = wave; p0 < cut.splits; p0 += 4 * kAt) {
+        floatx2 ml[kAt];
+        floatx4 v[kAt];
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < kAt; ++j) {
+            const int part = p0 + 4 * j;
+            const size_t unit = (unit0 + min(part, cut.splits - 1)) * cut.rows + rt;
+            ml[j] = (floatx2){-INFINITY, 0.f};
+            v[j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+            if (is && part < cut.splits) {
+                ml[j] = ((const floatx2*)a.ml_part)[unit * 16 + col];
+                v[j] = ((const floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kAt; ++j) top = fmaxf(top, ml[j][0]);
+        const float off = top == -INFINITY ? 0.f : top, r = fast_exp2(m - off);
+        l *= r;
+        o *= r;
+#pragma unroll
+        for (int j = 0; j < kAt; ++j) {
+            const float by = fast_exp2(ml[j][0] - off);
+            l += ml[j][1] * by;
+            o += v[j] * by;
+        }
+        m = top;
     }
-    if (row < a.M * a.rep) sparse_out(a, head, row, D, ct, g, o, l);
+    s_o[wave][lane] = o;
+    if (g == 0) s_ml[wave][col] = (floatx2){m, l};
+    __syncthreads();
+    if (wave != 0 || !is) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, s_ml[w][col][0]);
+    const float off = top == -INFINITY ? 0.f : top;
+    l = 0.f;
+    o = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float by = fast_exp2(s_ml[w][col][0] - off);
+        l += s_ml[w][col][1] * by;
+        o += s_o[w][lane] * by;
+    }
+    sparse_out(a, head, row, D, ct, g, o, l);
 }
 
 static SparseCut sparse_cut(int M, int kv_len, int nh, int nkv, int d)
 {
-    const int tiles = ceil_div(M * (nh / nkv), 16), rows = tiles == 1 ? 1 : 2, blocks = ceil_div(tiles, rows), n = kv_len / kBlock;
+    // (four tiles of 128 channels do not fit the registers)
+    const int tiles = ceil_div(M * (nh / nkv), 16), blocks = ceil_div(tiles, d == 128 ? 3 : 4), rows = ceil_div(tiles, blocks), n = kv_len / kBlock;
     const int most = n + ceil_div(kv_len + M - n * kBlock, kBlock);      // blocks that a row can read
-    const int splits = std::max(ceil_div(most, kList), std::min(most, std::max(1, 512 / (nkv * blocks))));
+    const int splits = std::max(ceil_div(most, kList), std::min(most, std::max(1, 256 / (nkv * blocks))));
     return {rows, blocks, splits};
 }
 
@@ -332,23 +463,33 @@ static size_t sparse_units(const SparseCut& c, int nkv) { return c.splits == 1 ?
 static size_t sparse_o_bytes(size_t units, int d) { return align_up(units * 16 * d * 4, 256); }
 static size_t sparse_bytes(size_t units, int d) { return std::max<size_t>(256, sparse_o_bytes(units, d) + align_up(units * 128, 256)); }
 
-// The most that a call of up to M tokens over up to kv_len rows takes, whatever its cut: parts are at most 512 workgroups of two
-// tiles of rows and a part reads a block, or as many as a list's length makes of them.
+// The most that a call of up to M tokens over up to kv_len rows takes, whatever its cut: parts are at most 256 workgroups of four
+// tiles of rows and a part reads a block, or as many as a list's length makes of them; blocks end up to three tiles behind the rows.
 size_t sparse_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
 {
-    const size_t tiles = ceil_div(M * (nh / nkv), 16) + 1, most = kv_len / kBlock + 1 + ceil_div(M, kBlock);
+    const size_t tiles = ceil_div(M * (nh / nkv), 16) + 3, most = kv_len / kBlock + 1 + ceil_div(M, kBlock);
     return sparse_bytes(std::max(std::min<size_t>(1024, nkv * tiles * most), most > kList ? nkv * tiles * ((most + kList - 1) / kList) : 0), d);
+}
+
+template <int D, int RT>
+static ghd_status sparse_rows(const SparseArgs& a, const SparseCut& c, hipStream_t st)
+{
+    typedef SparseShape<D, RT> S;
+    const ghd_status s = launch_resident_checked((const void*)k_sparse_attention<D, RT>, S::kThreads, S::kLds, nullptr);
+    if (s) return s;
+    hipLaunchKernelGGL((k_sparse_attention<D, RT>), dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(S::kThreads), S::kLds, st, a, c);
+    return check_launch();
 }
 
 template <int D>
 static ghd_status sparse_of(const SparseArgs& a, const SparseCut& c, hipStream_t st)
 {
-    const dim3 grid(c.splits, c.blocks, a.nkv);
-    if (c.rows == 1) hipLaunchKernelGGL((k_sparse_attention<D, 1>), grid, dim3(kSparseThreads), 0, st, a, c);
-    else hipLaunchKernelGGL((k_sparse_attention<D, 2>), grid, dim3(kSparseThreads), 0, st, a, c);
-    const ghd_status s = check_launch();
+    const ghd_status s = c.rows == 1   ? sparse_rows<D, 1>(a, c, st)
+                         : c.rows == 2 ? sparse_rows<D, 2>(a, c, st)
+                         : c.rows == 3 ? sparse_rows<D, 3>(a, c, st)
+                                       : sparse_rows<D, D == 128 ? 3 : 4>(a, c, st);
     if (s || c.splits == 1) return s;
-    hipLaunchKernelGGL(k_sparse_join<D>, dim3(ceil_div(c.rows * (D / 16), 4), c.blocks, a.nkv), dim3(256), 0, st, a, c);
+    hipLaunchKernelGGL(k_sparse_join<D>, dim3(c.rows * (D / 16), c.blocks, a.nkv), dim3(256), 0, st, a, c);
     return check_launch();
 }
 

@@ -157,7 +157,7 @@ def test_they_are_refused_without_assertions_too():
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
     class Elsewhere:
-        is_cuda, dtype, shape, device = True, torch.float16, (2, 2, 64), "cuda:1"
+        dtype, shape, device = torch.float16, (2, 2, 64), "cuda:1"
 
         def is_contiguous(self):
             return True
@@ -168,5 +168,7 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         def stride(self):
             return (128, 64, 1)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    with pytest.raises(ValueError, match="current device, cuda:0"):
-        B._here("q", Elsewhere(), torch.float16)
+    with pytest.raises(ValueError, match="cuda:0"):
+        B._here("q", Elsewhere(), torch.float16, None, 0)
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        B._stream_of(1)
