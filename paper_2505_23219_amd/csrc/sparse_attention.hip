@@ -19,47 +19,63 @@ struct SparseCut {
 };
 
 constexpr int kList = 1024;                      // blocks of a workgroup's list: the host divides a head's so that they fit
+template <bool WIDE>
 struct SparseList {
-    uint64_t bits[kList];                        // a bit for each of the workgroup's tokens
+    uint64_t bits[WIDE ? 2 : 1][kList];          // a bit for each of the workgroup's tokens
     int32_t block[kList];
     int32_t part[8];
 };
 
-// What a workgroup reads: the blocks that its tokens i0 .. i1 (at most 64) have selected, then the `tail` that all read.  Words of
-// the selection are asked for when a workgroup begins; every workgroup of a row block puts the blocks in the same order,
+// What a workgroup reads: the blocks that its tokens i0 .. i1 (at most 64, or with WIDE all 128) have selected, then the `tail` that
+// all read.  Words of the selection are asked for when a workgroup begins; every workgroup of a row block puts the blocks in the same order,
 // a thread's one behind the other, and takes its share.
-template <int THREADS>
+template <int THREADS, bool WIDE>
 struct SparseScan {
-    static constexpr int kKept = 4;              // words of a thread that stay in registers
+    static constexpr int kKept = 4;              // blocks of a thread whose words stay in registers
+    struct Word {
+        uint64_t x, y;
+        __device__ __forceinline__ bool some() const { return (x | (WIDE ? y : 0)) != 0; }
+    };
     const uint64_t *lo, *hi;
-    uint64_t keep, word[kKept];
+    uint64_t keep, keep_hi;
+    Word word[kKept];
     int n, shift;
-    __device__ __forceinline__ SparseScan(const SparseArgs& a, int head, int i0, int i1) : n(a.n), shift(i0 & 63)
+    bool apart;                                  // (WIDE) the second word is one of its own
+    __device__ __forceinline__ SparseScan(const SparseArgs& a, int head, int i0, int i1) : n(a.n), shift(i0 & 63), apart(i1 - i0 >= 64)
     {
-        const int words = (a.M + 63) / 64;
+        const int words = (a.M + 63) / 64, more = i1 - i0;
         lo = a.sel + ((size_t)head * words + (i0 >> 6)) * n;
-        hi = i1 >> 6 != i0 >> 6 ? lo + n : nullptr;      // (then shift is not 0)
-        keep = i1 - i0 >= 63 ? ~0ull : (1ull << (i1 - i0 + 1)) - 1;
+        hi = i1 >> 6 != i0 >> 6 ? lo + n : nullptr;      // (then shift is not 0, or the tokens are all 65 to 128 of them)
+        keep = more >= 63 ? ~0ull : (1ull << (more + 1)) - 1;
+        keep_hi = more >= 127 ? ~0ull : more >= 64 ? (1ull << (more - 63)) - 1 : 0;
 #pragma unroll
-        for (int j = 0; j < kKept; ++j) {
-            const int b = threadIdx.x + j * THREADS;
-            word[j] = b < n ? at(b) : 0;
-        }
+        for (int j = 0; j < kKept; ++j) word[j] = {0, 0};
+        if (n == 0) return;
+        // (all requests before the first is waited for)
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) word[j].x = lo[min((int)threadIdx.x + j * THREADS, n - 1)];
+        if (hi)
+#pragma unroll
+            for (int j = 0; j < kKept; ++j) word[j].y = hi[min((int)threadIdx.x + j * THREADS, n - 1)];
     }
-    __device__ __forceinline__ uint64_t at(int b) const
+    // the tokens' bits of two words as they lie
+    __device__ __forceinline__ Word tokens(uint64_t x, uint64_t y) const
     {
-        uint64_t x = lo[b] >> shift;
-        if (hi) x |= hi[b] << (64 - shift);
-        return x & keep;
+        if (WIDE && apart) return {x & keep, y & keep_hi};
+        return {(x >> shift | (hi ? y << (64 - shift) : 0)) & keep, 0};
     }
+    __device__ __forceinline__ Word at(int b) const { return tokens(lo[b], hi ? hi[b] : 0); }
     // shares of `splits` to the list; returns how many blocks this one has, and how many come before the tail's in all
-    __device__ __forceinline__ int list(SparseList& s, int tail, int split, int splits, int& before_tail) const
+    __device__ __forceinline__ int list(SparseList<WIDE>& s, int tail, int split, int splits, int& before_tail)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         int mine = 0;
 #pragma unroll
-        for (int j = 0; j < kKept; ++j) mine += word[j] != 0;
-        for (int b = tid + kKept * THREADS; b < n; b += THREADS) mine += at(b) != 0;
+        for (int j = 0; j < kKept; ++j) {
+            word[j] = tid + j * THREADS < n ? tokens(word[j].x, word[j].y) : Word{0, 0};
+            mine += word[j].some();
+        }
+        for (int b = tid + kKept * THREADS; b < n; b += THREADS) mine += at(b).some();
         int before = mine;
 #pragma unroll
         for (int off = 1; off < 64; off *= 2) {
@@ -77,10 +93,11 @@ struct SparseScan {
             all += c;
         }
         const int total = all + tail, first = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
-        auto put = [&](int b, uint64_t x) {
-            if (x == 0) return;
+        auto put = [&](int b, const Word& w) {
+            if (!w.some()) return;
             if (before >= first && before < end) {
-                s.bits[before - first] = x;
+                s.bits[0][before - first] = w.x;
+                if constexpr (WIDE) s.bits[1][before - first] = w.y;
                 s.block[before - first] = b;
             }
             ++before;
@@ -90,10 +107,7 @@ struct SparseScan {
             for (int j = 0; j < kKept; ++j) put(tid + j * THREADS, word[j]);
             for (int b = tid + kKept * THREADS; b < n; b += THREADS) put(b, at(b));
         }
-        if (tid < tail && all + tid >= first && all + tid < end) {
-            s.bits[all + tid - first] = 0;
-            s.block[all + tid - first] = n + tid;
-        }
+        if (tid < tail && all + tid >= first && all + tid < end) s.block[all + tid - first] = n + tid;
         before_tail = all - first;
         return end - first;
     }
@@ -191,6 +205,65 @@ struct SparseState {
     }
 };
 
+// The values that a row sees, one by one: for units that hold an infinity or NaN, which times the probability 0 is no 0.
+template <int D>
+__device__ __forceinline__ void values_one_by_one(const SparseArgs& a, int head, SparseState<D>& st, half8 p, uint32_t see, int key0, int lane)
+{
+    const int col = lane & 15, g = lane >> 4, total = a.kv_len + a.M;
+#pragma unroll 1
+    for (int key = 0; key < 32; ++key) {
+        const int from = col + 16 * (key >> 3);
+        float mine = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine = (key & 7) == e ? (float)p[e] : mine;
+        const float pk = __shfl(mine, from);
+        if (__shfl((int)see, from) >> (key & 7) & 1) {
+            const half_t* vp = a.v + head * a.v_head + min(key0 + key, total - 1) + (int64_t)(4 * g) * a.v_ch;
+#pragma unroll
+            for (int ct = 0; ct < D / 16; ++ct) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.o[ct][e] += pk * (float)vp[(int64_t)(ct * 16 + e) * a.v_ch];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+}
+template <int D, int RT>
+__device__ __forceinline__ bool not_finite(const SparseState<D> (&st)[RT])
+{
+    bool odd = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(st[r].o[ct][e]) < INFINITY);
+    return odd;
+}
+
+// Which token a column is, and which of a workgroup's tokens a tile of rows has.
+__device__ __forceinline__ int token_of(const SparseArgs& a, int row) { return min(row / a.rep, a.M - 1); }
+__device__ __forceinline__ uint64_t tile_tokens(const SparseArgs& a, int row0, int i0)
+{
+    const int from = row0 / a.rep - i0, to = token_of(a, row0 + 15) - i0;
+    return from > to ? 0 : (to - from >= 63 ? ~0ull : (1ull << (to - from + 1)) - 1) << from;
+}
+__device__ __forceinline__ uint64_t uniform64(uint64_t x)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+// a row's share of q as an operand; where there is no row, the last one's
+template <int D>
+__device__ __forceinline__ half8 sparse_query(const SparseArgs& a, int head, int row, int s, int g)
+{
+    row = min(row, a.M * a.rep - 1);
+    const int token = row / a.rep;
+    const half8 x = *(const half8*)(a.q + ((size_t)token * a.nh + head * a.rep + row - token * a.rep) * D + s * 32 + g * 8);
+    return a.scale < 0.f ? -x : x;
+}
+// scores to powers of two; above 0, so that minus infinity stays that
+__device__ __forceinline__ float sparse_power(float scale) { return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f); }
+
 // a row's output from the sums and their divisor; a row that sees no key gives zeros
 __device__ __forceinline__ void sparse_out(const SparseArgs& a, int head, int row, int d, int ct, int g, floatx4 o, float l)
 {
@@ -214,7 +287,7 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
 {
     typedef SparseShape<D, RT> S;
     constexpr int CT = S::CT, KS = S::KS, W = S::kWaves;
-    __shared__ SparseList list;
+    __shared__ SparseList<false> list;
     __shared__ uint64_t s_mask[2 * GHD_MAX_M];
     __shared__ floatx2 s_ml[W][RT * 16];
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -225,15 +298,13 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
     const int block = blockIdx.x >> 3, head = item / cut.splits, split = item - head * cut.splits;
     const int row0 = block * RT * 16, R = a.M * a.rep, i0 = row0 / a.rep, i1 = min((row0 + RT * 16 - 1) / a.rep, a.M - 1);
     const int total = a.kv_len + a.M, tail = (total - a.n * kBlock + kBlock - 1) / kBlock;
-    const SparseScan<S::kThreads> scan(a, head, i0, i1);
+    SparseScan<S::kThreads, false> scan(a, head, i0, i1);
     constexpr int kMine = (RT * KS + W - 1) / W;                   // operands of q that a wavefront brings
     half8 x[kMine];
 #pragma unroll
     for (int f = 0; f < kMine; ++f) {
-        const int frag = f * W + wave, row = row0 + frag / KS * 16 + col, token = row / a.rep;
-        x[f] = (half8){0, 0, 0, 0, 0, 0, 0, 0};
-        if (frag < RT * KS && row < R)
-            x[f] = *(const half8*)(a.q + ((size_t)token * a.nh + head * a.rep + row - token * a.rep) * D + frag % KS * 32 + g * 8);
+        const int frag = min(f * W + wave, RT * KS - 1);
+        x[f] = sparse_query<D>(a, head, row0 + frag / KS * 16 + col, frag % KS, g);
     }
     int up0 = 0, up1 = 0;
     if (wave == 0 && a.parent) {
@@ -250,19 +321,17 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
     }
 #pragma unroll
     for (int f = 0; f < kMine; ++f)
-        if (f * W + wave < RT * KS) *(half8*)(lds + (f * W + wave) * 1024 + lane * 16) = a.scale < 0.f ? -x[f] : x[f];
+        if (f * W + wave < RT * KS) *(half8*)(lds + (f * W + wave) * 1024 + lane * 16) = x[f];
     __syncthreads();
     auto query = [&](int r, int s) { return *(const half8*)(lds + (r * KS + s) * 1024 + lane * 16); };
-    // scores to powers of two; above 0, so that minus infinity stays that
-    const float c = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+    const float c = sparse_power(a.scale);
     uint32_t tokens = 0;                                           // of a lane's columns, 8 bits each
     auto token = [&](int r) { return (int)(tokens >> 8 * r & 255); };
-    uint64_t tile_bits[RT];                                        // of a tile's tokens
+    uint64_t tile_bits[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        tokens |= (uint32_t)min((row0 + r * 16 + col) / a.rep, a.M - 1) << 8 * r;
-        const int from = (row0 + r * 16) / a.rep - i0, to = min((row0 + r * 16 + 15) / a.rep, a.M - 1) - i0;
-        tile_bits[r] = from > to ? 0 : (to - from >= 63 ? ~0ull : (1ull << (to - from + 1)) - 1) << from;
+        tokens |= (uint32_t)token_of(a, row0 + r * 16 + col) << 8 * r;
+        tile_bits[r] = tile_tokens(a, row0 + r * 16, i0);
     }
     SparseState<D> st[RT];
     const int units = 2 * count;
@@ -282,8 +351,7 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
             const int next = u + W < units ? u + W : u, next0 = key_of(next), there = total - key0;
             const int next_there = max(1, min(32, total - next0));
             const bool rest = key0 >= a.n * kBlock;                // behind the blocks
-            const uint64_t bits = rest ? ~0ull : ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(list.bits[u >> 1] >> 32)) << 32) |
-                                                     (uint32_t)__builtin_amdgcn_readfirstlane((int)list.bits[u >> 1]);
+            const uint64_t bits = rest ? ~0ull : uniform64(list.bits[0][u >> 1]);
             if (there < 32) unit.clean(there, lane);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
@@ -312,23 +380,7 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) st[r].o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(unit.v[ct], p, st[r].o[ct], 0, 0, 0);
                 } else {
-#pragma unroll 1
-                    for (int key = 0; key < 32; ++key) {
-                        const int from = col + 16 * (key >> 3);
-                        float mine = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) mine = (key & 7) == e ? (float)p[e] : mine;
-                        const float pk = __shfl(mine, from);
-                        if (__shfl((int)see, from) >> (key & 7) & 1) {
-                            const half_t* vp = a.v + head * a.v_head + min(key0 + key, total - 1) + (int64_t)(4 * g) * a.v_ch;
-#pragma unroll
-                            for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) st[r].o[ct][e] += pk * (float)vp[(int64_t)(ct * 16 + e) * a.v_ch];
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        }
-                    }
+                    values_one_by_one<D>(a, head, st[r], p, see, key0, lane);
                 }
             }
             if (next == u) break;
@@ -338,14 +390,7 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
         }
     };
     pass(std::true_type{});
-    bool odd = false;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(st[r].o[ct][e]) < INFINITY);
-    if (__builtin_expect(__ballot(odd) != 0, 0)) pass(std::false_type{});
+    if (__builtin_expect(__ballot(not_finite<D, RT>(st)) != 0, 0)) pass(std::false_type{});
     // the wavefronts' states meet in LDS, some fragments at a time, each added up by one wavefront
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -385,6 +430,233 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
             } else {
                 sparse_out(a, head, row, D, ct, g, o, l);
             }
+        }
+    }
+}
+
+// ---- more rows ----------------------------------------------------------------------------
+// What a compute unit reads from the L2 has a bound of its own (some 35 GB/s here), so above 32 rows a block of keys is read once for all rows of
+// a workgroup: straight to LDS, four blocks of 64 keys on their way, while eight wavefronts - four groups of rows, each RT tiles of
+// 16, by halves of a block - take their operands from there.
+constexpr int kStages = 4;
+template <int D>
+struct StagedShape {
+    static constexpr int kHalf = 128 * D, kStage = 2 * kHalf;     // bytes of a block's keys (as many of values), and of both
+    static constexpr int kPieces = D / 64;                         // KiB of each that a wavefront brings
+    static constexpr size_t kLds = kStages * kStage;
+};
+
+// A KiB of the LDS is 4 (or 8) rows of K or 8 channels of V^T; the 16-byte pieces of a row lie in an order of their own (piece p of row r in place
+// p ^ f(r)), so that the 16 rows that an operand takes the same piece of are spread over all banks.
+template <int D>
+struct StagedBlock {
+    uint32_t k_row, k_piece, v_ch, v_piece;                        // what the lane brings
+    uint32_t k_at, v_at;                                           // where it finds its operands, but for the k-step's piece
+    __device__ __forceinline__ StagedBlock(int wave, int lane)
+    {
+        constexpr int kLanes = D / 8, kRows = 64 / kLanes;         // lanes of a row, rows of a KiB
+        const int col = lane & 15;
+        k_row = wave * StagedShape<D>::kPieces * kRows + lane / kLanes;
+        k_piece = lane % kLanes;
+        v_ch = wave * StagedShape<D>::kPieces * 8 + lane / 8;
+        v_piece = lane % 8;
+        k_at = (uint32_t)((col >> 2) * 8 + (col & 3)) * (D * 2);
+        v_at = StagedShape<D>::kHalf + (uint32_t)col * 128;
+    }
+    // f of a row of K: the column that has it, by twos where a row is 128 bytes
+    __device__ __forceinline__ static uint32_t k_turn(uint32_t key)
+    {
+        const uint32_t col = (key & 3) | (key >> 3 & 3) << 2;
+        return D == 128 ? col : col >> 1;
+    }
+    __device__ __forceinline__ void request(const SparseArgs& a, int head, int block, int wave, uint32_t lds) const
+    {
+        constexpr int kRows = 512 / D, kPieces = StagedShape<D>::kPieces;
+        const int there = a.kv_len + a.M - block * kBlock;         // rows of the block, and behind it
+        const auto k = (GLOBAL const char*)gp(a.k + head * a.k_head + (int64_t)block * kBlock * a.k_tok);
+        const auto v = (GLOBAL const char*)gp(a.v + head * a.v_head + (int64_t)block * kBlock);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t key = k_row + i * kRows;
+            to_lds(k, (uint32_t)min((int)key, there - 1) * (uint32_t)(2 * a.k_tok) + (k_piece ^ k_turn(key)) * 16, lds + (wave * kPieces + i) * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t ch = v_ch + i * 8;
+            to_lds(v, ch * (uint32_t)(2 * a.v_ch) + min((v_piece ^ (ch >> 1 & 7)) * 16, (uint32_t)((there - 1) >> 3) * 16),
+                   lds + StagedShape<D>::kHalf + (wave * kPieces + i) * 1024);
+        }
+    }
+    __device__ __forceinline__ half8 key(const char* at, int half, int h, int s, int lane) const
+    {
+        const uint32_t col = lane & 15, turn = D == 128 ? col : col >> 1;
+        return *(const half8*)(at + k_at + (half * 32 + h * 4) * (D * 2) + ((s * 4 + (lane >> 4)) ^ turn) * 16);
+    }
+    __device__ __forceinline__ half8 value(const char* at, int half, int ct, int lane) const
+    {
+        return *(const half8*)(at + v_at + ct * 2048 + ((half * 4 + (lane >> 4)) ^ (lane & 15) >> 1) * 16);
+    }
+};
+
+template <int D, int RT>
+__global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCut cut)
+{
+    constexpr int CT = D / 16, KS = D / 32, W = 8, kLoads = 2 * StagedShape<D>::kPieces;
+    constexpr bool WIDE = RT > 1;
+    __shared__ SparseList<WIDE> list;
+    __shared__ uint64_t s_mask[2 * GHD_MAX_M];
+    __shared__ floatx2 s_ml[W][RT * 16];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
+    const int item = blockIdx.y * 8 + (blockIdx.x & 7);
+    if (item >= a.nkv * cut.splits) return;
+    const int block = blockIdx.x >> 3, head = item / cut.splits, split = item - head * cut.splits;
+    const int row0 = block * RT * 64, R = a.M * a.rep, i0 = row0 / a.rep, i1 = token_of(a, row0 + RT * 64 - 1);
+    const int total = a.kv_len + a.M, tail = (total - a.n * kBlock + kBlock - 1) / kBlock;
+    const int group = wave >> 1, half = wave & 1, my_row = row0 + group * RT * 16;
+    SparseScan<512, WIDE> scan(a, head, i0, i1);
+    half8 q[RT][KS];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[r][s] = sparse_query<D>(a, head, my_row + r * 16 + col, s, g);
+    int up0 = 0, up1 = 0;
+    if (wave == 0 && a.parent) {
+        up0 = a.parent[min(lane, a.M - 1)];
+        up1 = a.parent[min(lane + 64, a.M - 1)];
+    }
+    int before_tail;
+    const int count = scan.list(list, tail, split, cut.splits, before_tail);
+    __syncthreads();
+    const StagedBlock<D> staged(wave, lane);
+    auto request = [&](int i) {
+        staged.request(a, head, __builtin_amdgcn_readfirstlane(list.block[i]), wave, lds0 + (uint32_t)(i & (kStages - 1)) * StagedShape<D>::kStage);
+    };
+    // (the queries are there before that: otherwise they are waited for together with all of these)
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[r][s]));
+    for (int i = 0; i < min(count, kStages - 1); ++i) request(i);
+    if (before_tail < count) {
+        if (!a.parent)
+            for (int e = threadIdx.x; e < 2 * a.M; e += 512) s_mask[e] = a.mask[e];
+        else if (wave == 0)
+            store_masks(tree_nodes<2, true>(up0, up1, a.M, lane), a.M, lane, s_mask);
+    }
+    const float c = sparse_power(a.scale);
+    // (128 tokens are in two words: of a group of 32 rows in one of them)
+    const bool second = my_row / a.rep - i0 >= 64;
+    const int base = i0 + (second ? 64 : 0);
+    int token[RT];
+    uint64_t tile_bits[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        token[r] = token_of(a, my_row + r * 16 + col);
+        tile_bits[r] = my_row + r * 16 < R ? tile_tokens(a, my_row + r * 16, base) : 0;
+    }
+    SparseState<D> st[RT];
+    auto pass = [&](auto plain) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) st[r].clear();
+        for (int i = 0; i < count; ++i) {
+            // a barrier a block: it is there for everybody, and everybody is done with the one before, whose place is requested into
+            const int young = min(count - 1 - i, kStages - 2);
+            if (young == 2) wait_loads<2 * kLoads>();
+            else if (young == 1) wait_loads<kLoads>();
+            else wait_loads<0>();
+            pin_order();
+            barrier_lds();
+            if (i + kStages - 1 < count) request(i + kStages - 1);
+            const int at = __builtin_amdgcn_readfirstlane(list.block[i]), key0 = at * kBlock + half * 32, there = total - key0;
+            const bool rest = at >= a.n;
+            const uint64_t bits = rest ? ~0ull : uniform64(list.bits[WIDE && second][i]);
+            uint64_t mine = 0;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) mine |= tile_bits[r];
+            if (there <= 0 || (bits & mine) == 0) continue;
+            const char* const buf = lds + (i & (kStages - 1)) * StagedShape<D>::kStage;
+            half8 k[2][KS], v[CT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) k[h][s] = staged.key(buf, half, h, s, lane);
+            __builtin_amdgcn_sched_barrier(0);
+            half8 p[RT];
+            uint32_t see[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                floatx4 s[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[h][ks], q[r][ks], s[h], 0, 0, 0);
+                }
+                if (r == 0) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) v[ct] = staged.value(buf, half, ct, lane);
+                }
+                see[r] = rest ? seen_keys((const uint32_t*)(s_mask + 2 * token[r]), key0 + g * 8, a.kv_len, total)
+                              : bits >> (max(token[r] - base, 0) & 63) & 1 ? 0xffu : 0u;
+                if (rest || (bits & tile_bits[r]) != tile_bits[r])
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = see[r] >> e & 1 ? s[e >> 2][e & 3] : -INFINITY;
+                p[r] = st[r].powers(s, c);
+            }
+            if (there < 32) {
+                // rows that are not there may hold anything, and 0 times anything is no 0
+                const int some = there - 8 * g;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    uint4_ w = __builtin_bit_cast(uint4_, v[ct]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] &= (some > 2 * e ? 0xffffu : 0u) | (some > 2 * e + 1 ? 0xffff0000u : 0u);
+                    v[ct] = __builtin_bit_cast(half8, w);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if constexpr (decltype(plain)::value) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) st[r].o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[ct], p[r], st[r].o[ct], 0, 0, 0);
+                } else {
+                    values_one_by_one<D>(a, head, st[r], p[r], see[r], key0, lane);
+                }
+            }
+        }
+    };
+    pass(std::true_type{});
+    if (__builtin_expect(__syncthreads_or(not_finite<D, RT>(st)), 0)) {
+        for (int i = 0; i < min(count, kStages - 1); ++i) request(i);
+        pass(std::false_type{});
+    }
+    // the two wavefronts of a group meet in LDS, each adds up half of the fragments
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float l = sum_over_groups(st[r].l);
+        if (g == 0) s_ml[wave][r * 16 + col] = (floatx2){st[r].m, l};
+    }
+    __syncthreads();
+    floatx4* const part = (floatx4*)lds + lane;                    // [wave][fragment][64]
+#pragma unroll
+    for (int f = 0; f < RT * CT; ++f) part[(wave * RT * CT + f) * 64] = st[f / CT].o[f % CT];
+    __syncthreads();
+    const size_t unit0 = (((size_t)head * cut.blocks + block) * cut.splits + split) * (RT * 4) + group * RT;
+#pragma unroll 2
+    for (int f = half; f < RT * CT; f += 2) {
+        const int r = f / CT, ct = f % CT, row = my_row + r * 16 + col;
+        const floatx2 x = s_ml[wave & ~1][r * 16 + col], y = s_ml[wave | 1][r * 16 + col];
+        const float m = fmaxf(x[0], y[0]), off = m == -INFINITY ? 0.f : m, bx = fast_exp2(x[0] - off), by = fast_exp2(y[0] - off);
+        const float l = x[1] * bx + y[1] * by;
+        const floatx4 o = part[((wave & ~1) * RT * CT + f) * 64] * bx + part[((wave | 1) * RT * CT + f) * 64] * by;
+        if (row >= R) continue;
+        if (cut.splits > 1) {
+            ((floatx4*)a.o_part)[((unit0 + r) * CT + ct) * 64 + lane] = o;
+            if (ct == 0 && g == 0) ((floatx2*)a.ml_part)[(unit0 + r) * 16 + col] = (floatx2){m, l};
+        } else {
+            sparse_out(a, head, row, D, ct, g, o, l);
         }
     }
 }
@@ -450,44 +722,72 @@ __global__ __launch_bounds__(256) void k_sparse_join(SparseArgs a, SparseCut cut
     sparse_out(a, head, row, D, ct, g, o, l);
 }
 
+// What is estimated to be fastest of blocks of 1, 2 (wavefronts by themselves), 4 and 8 tiles of rows (through LDS) and of parts
+// that make 128 or 256 workgroups, in us: a launch takes `fixed`, every round of the workgroups on an XCD's 32 compute units `round` and for
+// each block of keys of a part `block`, a second launch `join` and what it reads and writes.  Fitted to 2178 calls (1 to 128 tokens, 2 to 40
+// key heads, 777 to 16384 rows; off by 5% in the mean); the fastest of a call's cuts is missed by 1.2% in the mean, 23% at
+// the most.  A token's blocks are on the device: a row block is taken to read 64, which is what decides between the cuts best.
 static SparseCut sparse_cut(int M, int kv_len, int nh, int nkv, int d)
 {
-    // (four tiles of 128 channels do not fit the registers)
-    const int tiles = ceil_div(M * (nh / nkv), 16), blocks = ceil_div(tiles, d == 128 ? 3 : 4), rows = ceil_div(tiles, blocks), n = kv_len / kBlock;
+    static const struct {
+        int rows;
+        float fixed, round, block, join, mb;
+    } kinds[2][4] = {{{1, 4.5f, 0.f, .48f, 3.1f, 1.f}, {2, 2.6f, 3.7f, .48f, 2.9f, .83f}, {4, 7.5f, .6f, .78f, 1.f, .53f}, {8, 4.f, 3.2f, 1.18f, 2.6f, .61f}},
+                     {{1, 3.9f, 0.f, .95f, 3.7f, .83f}, {2, 2.9f, 4.f, .98f, 2.8f, .75f}, {4, 5.4f, 3.3f, 1.08f, 1.f, .62f}, {8, 7.f, 2.6f, 1.5f, 3.f, .49f}}};
+    const int tiles = ceil_div(M * (nh / nkv), 16), n = kv_len / kBlock;
     const int most = n + ceil_div(kv_len + M - n * kBlock, kBlock);      // blocks that a row can read
-    const int splits = std::max(ceil_div(most, kList), std::min(most, std::max(1, 256 / (nkv * blocks))));
-    return {rows, blocks, splits};
+    SparseCut best = {};
+    float least = 0.f;
+    for (const auto& k : kinds[d == 128]) {
+        if (k.rows == 1 ? tiles > 4 : k.rows >= 2 * tiles) continue;
+        const int blocks = ceil_div(tiles, k.rows), items = nkv * blocks;
+        for (int wgs = 128; wgs <= 256; wgs += 128) {
+            const int splits = std::max(ceil_div(most, kList), std::min(most, std::max(1, wgs / items)));
+            const int on_xcd = ceil_div(nkv * splits, 8) * blocks;
+            // (of workgroups of one tile, four wavefronts, a compute unit has several)
+            const float rounds = k.rows == 1 ? std::max(1.f, on_xcd / 32.f) : (float)ceil_div(on_xcd, 32);
+            float us = k.fixed + rounds * (k.round + ceil_div(std::min(most, 64), splits) * k.block);
+            if (splits > 1) us += k.join + k.mb * 64e-6f * items * splits * k.rows * d;
+            if (least == 0.f || us < least) {
+                least = us;
+                best = {k.rows, blocks, splits};
+            }
+        }
+    }
+    return best;
 }
 
 static size_t sparse_units(const SparseCut& c, int nkv) { return c.splits == 1 ? 0 : (size_t)nkv * c.blocks * c.splits * c.rows; }
 static size_t sparse_o_bytes(size_t units, int d) { return align_up(units * 16 * d * 4, 256); }
 static size_t sparse_bytes(size_t units, int d) { return std::max<size_t>(256, sparse_o_bytes(units, d) + align_up(units * 128, 256)); }
 
-// The most that a call of up to M tokens over up to kv_len rows takes, whatever its cut: parts are at most 256 workgroups of four
-// tiles of rows and a part reads a block, or as many as a list's length makes of them; blocks end up to three tiles behind the rows.
+// The most that a call of up to M tokens over up to kv_len rows takes, whatever its cut: parts are at most 256 workgroups of eight
+// tiles of rows and a part reads a block, or as many as a list's length makes of them; blocks end up to seven tiles behind the rows.
 size_t sparse_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
 {
-    const size_t tiles = ceil_div(M * (nh / nkv), 16) + 3, most = kv_len / kBlock + 1 + ceil_div(M, kBlock);
-    return sparse_bytes(std::max(std::min<size_t>(1024, nkv * tiles * most), most > kList ? nkv * tiles * ((most + kList - 1) / kList) : 0), d);
+    const size_t tiles = ceil_div(M * (nh / nkv), 16) + 7, most = kv_len / kBlock + 1 + ceil_div(M, kBlock);
+    return sparse_bytes(std::max(std::min<size_t>(2048, nkv * tiles * most), most > kList ? nkv * tiles * ((most + kList - 1) / kList) : 0), d);
 }
 
-template <int D, int RT>
+template <int D, int RT, bool STAGED>
 static ghd_status sparse_rows(const SparseArgs& a, const SparseCut& c, hipStream_t st)
 {
-    typedef SparseShape<D, RT> S;
-    const ghd_status s = launch_resident_checked((const void*)k_sparse_attention<D, RT>, S::kThreads, S::kLds, nullptr);
+    void (*const kernel)(SparseArgs, SparseCut) = STAGED ? k_sparse_staged<D, RT> : k_sparse_attention<D, RT>;
+    const int threads = STAGED ? 512 : SparseShape<D, RT>::kThreads;
+    const size_t lds = STAGED ? StagedShape<D>::kLds : SparseShape<D, RT>::kLds;
+    const ghd_status s = launch_resident_checked((const void*)kernel, threads, lds, nullptr);
     if (s) return s;
-    hipLaunchKernelGGL((k_sparse_attention<D, RT>), dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(S::kThreads), S::kLds, st, a, c);
+    hipLaunchKernelGGL(kernel, dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(threads), lds, st, a, c);
     return check_launch();
 }
 
 template <int D>
 static ghd_status sparse_of(const SparseArgs& a, const SparseCut& c, hipStream_t st)
 {
-    const ghd_status s = c.rows == 1   ? sparse_rows<D, 1>(a, c, st)
-                         : c.rows == 2 ? sparse_rows<D, 2>(a, c, st)
-                         : c.rows == 3 ? sparse_rows<D, 3>(a, c, st)
-                                       : sparse_rows<D, D == 128 ? 3 : 4>(a, c, st);
+    const ghd_status s = c.rows == 1   ? sparse_rows<D, 1, false>(a, c, st)
+                         : c.rows == 2 ? sparse_rows<D, 2, false>(a, c, st)
+                         : c.rows == 4 ? sparse_rows<D, 1, true>(a, c, st)
+                                       : sparse_rows<D, 2, true>(a, c, st);
     if (s || c.splits == 1) return s;
     hipLaunchKernelGGL(k_sparse_join<D>, dim3(c.rows * (D / 16), c.blocks, a.nkv), dim3(256), 0, st, a, c);
     return check_launch();
