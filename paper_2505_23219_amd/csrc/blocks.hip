@@ -126,14 +126,12 @@ __device__ __forceinline__ void query_codes(const half8 (&x)[2], half2_ first, h
 }
 
 // Blocks are the rows of the product, 16 tokens of one query head its columns.  A wavefront keeps the codes of TILES tiles of 16 blocks in
-// registers and goes through the query heads.
-template <int D, int TILES>
-__global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
+// registers (tiles `step` blocks apart) and goes through the query heads.  to(b, keys): blocks b .. b + 3 of the lane's token.
+template <int D, int TILES, class Store>
+__device__ __forceinline__ void block_scores(const SelectArgs& a, int head, int m, int b0, int step, int lane, const Store& to)
 {
     constexpr int KS = 2 * D / 64;               // k-steps: the first half of them HI, the second LO
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int b0 = (blockIdx.x * 4 + wave) * TILES * 16, head = blockIdx.y, m = blockIdx.z * 16 + col;
-    if (b0 >= a.n) return;
+    const int g = lane >> 4, col = lane & 15;
     half8 x[KS / 2][2];
     const half_t* q = a.q + ((size_t)min(m, a.M - 1) * a.nkv + head) * a.rep * D + g * 16;
     auto ask_for = [&]() {
@@ -149,16 +147,14 @@ __global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            code[t][s] = *(const int4_*)(a.bounds.codes + (row0 + min(b0 + t * 16 + col, a.n - 1)) * 2 * D + s * 64 + g * 16);
+            code[t][s] = *(const int4_*)(a.bounds.codes + (row0 + min(b0 + t * step + col, a.n - 1)) * 2 * D + s * 64 + g * 16);
     floatx4 unit[TILES], best[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         best[t] = (floatx4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) unit[t][r] = a.bounds.units[row0 + min(b0 + t * 16 + 4 * g + r, a.n - 1)];
+        for (int r = 0; r < 4; ++r) unit[t][r] = a.bounds.units[row0 + min(b0 + t * step + 4 * g + r, a.n - 1)];
     }
-    if (a.zero && blockIdx.z == 0 && lane < TILES * 16 && b0 + lane < a.n)       // the picks set bits
-        for (int w = 0; w < (a.M + 63) / 64; ++w) a.sel[((size_t)head * ((a.M + 63) / 64) + w) * a.n + b0 + lane] = 0;
     for (int h = 0; h < a.rep; ++h) {
         typedef uint16_t ushort2_ __attribute__((ext_vector_type(2)));
         ushort2_ size = {0, 0};
@@ -196,18 +192,27 @@ __global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
             for (int r = 0; r < 4; ++r) best[t][r] = fmaxf(best[t][r], (float)sum[r] * step);
         }
     }
-    if (m >= a.M) return;
-    const int n4 = (a.n + 3) & ~3;
-    uint32_t* to = a.keys + ((size_t)head * a.M + m) * n4;
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-        const int b = b0 + t * 16 + 4 * g;
-        if (b >= n4) continue;
         uint4_ key;
 #pragma unroll
         for (int r = 0; r < 4; ++r) key[r] = score_key(unit[t][r] < INFINITY ? best[t][r] * unit[t][r] : INFINITY);
-        *(uint4_*)(to + b) = key;
+        to(b0 + t * step + 4 * g, key);
     }
+}
+
+template <int D, int TILES>
+__global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = (blockIdx.x * 4 + wave) * TILES * 16, head = blockIdx.y, m = blockIdx.z * 16 + (lane & 15);
+    if (b0 >= a.n) return;
+    if (a.zero && blockIdx.z == 0 && lane < TILES * 16 && b0 + lane < a.n)       // the picks set bits
+        for (int w = 0; w < (a.M + 63) / 64; ++w) a.sel[((size_t)head * ((a.M + 63) / 64) + w) * a.n + b0 + lane] = 0;
+    const int n4 = (a.n + 3) & ~3;
+    uint32_t* keys = a.keys + ((size_t)head * a.M + m) * n4;
+    block_scores<D, TILES>(a, head, m, b0, 16, lane, [&](int b, uint4_ key) {
+        if (m < a.M && b < n4) *(uint4_*)(keys + b) = key;
+    });
 }
 
 // ---- picks -------------------------------------------------------------------------------
@@ -365,8 +370,46 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
     }
 }
 
-// A workgroup has eight tokens, a byte of the words, and the blocks' bytes in LDS; the last tokens' workgroup writes what is left of
-// the words, too.  64 tokens of 32 heads over 512 blocks: 8.2 us, a workgroup a token and its bits set by atomic operations 15.8.
+// Eight tokens' bits, a byte of the blocks' words: from LDS to their place; the last tokens' workgroup writes what is left of the words, too.
+__device__ __forceinline__ void store_eight(const SelectArgs& a, int head, int m0, const uint32_t* s_bits, int tid)
+{
+    uint64_t* words = a.sel + ((size_t)head * ((a.M + 63) / 64) + m0 / 64) * a.n;
+    uint8_t* to = (uint8_t*)words + m0 % 64 / 8;
+    const int left = m0 + 8 >= a.M ? 8 - m0 % 64 / 8 : 1;          // bytes of a word that are this workgroup's
+    for (int b = tid; b < a.n; b += 512) {
+        const uint8_t x = (uint8_t)(s_bits[b >> 2] >> 8 * (b & 3));
+        if (left == 8) {
+            words[b] = x;
+        } else {
+            to[(size_t)8 * b] = x;
+            for (int i = 1; i < left; ++i) to[(size_t)8 * b + i] = 0;
+        }
+    }
+}
+
+// Scores and picks of few blocks in one launch: a workgroup has eight tokens of a head, whose scores stay in LDS.
+constexpr int kFewBlocks = 512;
+template <int D>
+__global__ __launch_bounds__(512) void k_block_few(SelectArgs a)
+{
+    __shared__ PickShared<64> s[8];
+    __shared__ __attribute__((aligned(16))) uint32_t s_key[8][kFewBlocks + 4];
+    __shared__ uint32_t s_bits[kFewBlocks / 4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), head = blockIdx.x, m0 = blockIdx.y * 8, m = m0 + wave;
+    if (tid < kFewBlocks / 4) s_bits[tid] = 0;
+    auto keep = [&](int b, uint4_ key) {
+        if ((lane & 15) < 8) *(uint4_*)(s_key[lane & 7] + b) = key;
+    };
+    // (all of a wavefront's tiles are asked for at once: two at a time, 64 tokens of 32 heads took .. us)
+    if (a.n > 128) block_scores<D, kFewBlocks / 128>(a, head, m0 + (lane & 7), wave * 16, 128, lane, keep);
+    else if (wave * 16 < a.n) block_scores<D, 1>(a, head, m0 + (lane & 7), wave * 16, 128, lane, keep);
+    __syncthreads();
+    if (m < a.M) pick_blocks<64, kFewBlocks / 64>(a, s[wave], s_key[wave], lane, [&](int b) { atomicOr(&s_bits[b >> 2], 1u << (8 * (b & 3) + wave)); });
+    __syncthreads();
+    store_eight(a, head, m0, s_bits, tid);
+}
+
+// A workgroup has eight tokens.  64 tokens of 32 heads over 512 blocks: 8.2 us, a workgroup a token and its bits set by atomic operations 15.8.
 constexpr int kPickBytes = 2048;                 // blocks
 template <int KEPT>
 __global__ __launch_bounds__(512) void k_block_pick_eight(SelectArgs a)
@@ -380,17 +423,7 @@ __global__ __launch_bounds__(512) void k_block_pick_eight(SelectArgs a)
         pick_blocks<64, KEPT>(a, s[wave], a.keys + ((size_t)head * a.M + m) * ((a.n + 3) & ~3), tid & 63,
                               [&](int b) { atomicOr(&s_bits[b >> 2], 1u << (8 * (b & 3) + wave)); });
     __syncthreads();
-    uint8_t* to = (uint8_t*)(a.sel + ((size_t)head * ((a.M + 63) / 64) + m0 / 64) * a.n) + m0 % 64 / 8;
-    const int left = m0 + 8 >= a.M ? 8 - m0 % 64 / 8 : 1;          // bytes of a word that are this workgroup's
-    for (int b = tid; b < a.n; b += 512) {
-        const uint8_t x = (uint8_t)(s_bits[b >> 2] >> 8 * (b & 3));
-        if (left == 8) {
-            a.sel[((size_t)head * ((a.M + 63) / 64) + m0 / 64) * a.n + b] = x;
-        } else {
-            to[(size_t)8 * b] = x;
-            for (int i = 1; i < left; ++i) to[(size_t)8 * b + i] = 0;
-        }
-    }
+    store_eight(a, head, m0, s_bits, tid);
 }
 
 // A workgroup has a token; the words are zeros before (k_block_scores).
@@ -426,10 +459,16 @@ ghd_status launch_block_bounds_read(float* hi, float* lo, Bounds from, int first
 ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
 {
     if (a.n == 0) return GHD_OK;
+    if (a.n <= kFewBlocks) {
+        const dim3 teams(a.nkv, ceil_div(a.M, 8));                  // (a head's tokens on one XCD, where its codes are)
+        if (d == 128) hipLaunchKernelGGL(k_block_few<128>, teams, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL(k_block_few<64>, teams, dim3(512), 0, st, a);
+        return check_launch();
+    }
     // a wavefront has 64 blocks, or 16 where there would be fewer than four wavefronts for each compute unit
     const int tiles = ceil_div(a.M, 16), per = (int64_t)ceil_div(a.n, 64) * a.nkv * tiles >= 1024 ? 4 : 1;
     const dim3 grid(ceil_div(a.n, 64 * per), a.nkv, tiles);
-    const bool eight = a.n <= kPickBytes && (a.M > 4 || a.n <= 512);
+    const bool eight = a.n <= kPickBytes && a.M > 4;
     a.zero = !eight;
     if (d == 128) {
         if (per == 4) hipLaunchKernelGGL((k_block_scores<128, 4>), grid, dim3(256), 0, st, a);
@@ -443,8 +482,7 @@ ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
     const int range = a.hi - a.lo;
     if (eight) {
         const dim3 teams(ceil_div(a.M, 8), a.nkv);
-        if (range <= 64 * 8) hipLaunchKernelGGL(k_block_pick_eight<8>, teams, dim3(512), 0, st, a);
-        else if (range <= 64 * 16) hipLaunchKernelGGL(k_block_pick_eight<16>, teams, dim3(512), 0, st, a);
+        if (range <= 64 * 16) hipLaunchKernelGGL(k_block_pick_eight<16>, teams, dim3(512), 0, st, a);
         else hipLaunchKernelGGL(k_block_pick_eight<32>, teams, dim3(512), 0, st, a);
     } else if (range <= 1024 * 4) {
         hipLaunchKernelGGL(k_block_pick<4>, dim3(a.M, a.nkv), dim3(1024), 0, st, a);

@@ -1,7 +1,7 @@
 // Acceptance of drafted tokens against the target's probabilities from given random numbers (include/ghd.h has the rule).
 //
 // Every node is judged at once as if the walk came there: k_sample_rows leaves maxima and sums of softmax weights of the rows' segments,
-// k_sample_nodes which child of each node is accepted, or which token is drawn there, and k_sample_walk goes from the root down.
+// k_sample_nodes which child of each node is accepted, or which token is drawn there; its last workgroup goes from the root down.
 // Where drafts have probabilities, k_sample_first tries every node's first child, which takes no more than the rows' sums; that leaves
 // few nodes that the walk can come to, and of those k_sample_rest sums up what a first rejection leaves, over the segments again.
 //
@@ -48,9 +48,6 @@ struct Segment {
 };
 struct Rest {
     double p, q;                                 // what the first rejection leaves: sums of max(p - q, 0) and q without the token
-};
-struct NodeResult {
-    int taken, token;                            // accepted child or -1, and the token drawn where there is none
 };
 struct First {
     double one, one_q;                           // one over the sums of the target's and the draft's row, 0 where those are
@@ -106,12 +103,13 @@ struct RowSum {
 
 // Target rows (blockIdx.y < M), without the tokens of the node's children where drafts have no probabilities; draft rows.
 // Bound: the bytes of the logits.
-__global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segment* __restrict__ seg)
+__global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segment* __restrict__ seg, uint32_t* __restrict__ arrived)
 {
     __shared__ uint32_t s_out[kSegment / 32];
     __shared__ double s_sum[kRowThreads / 64];
     __shared__ float s_top[kRowThreads / 64];
     const int tid = threadIdx.x, y = blockIdx.y, lo = blockIdx.x * kSegment, segments = gridDim.x;
+    if (y == 0 && blockIdx.x == 0 && tid == 0) *arrived = 0;
     const bool target = y < a.M;
     const float* row = (target ? a.logits + (size_t)y * a.V : a.q_logits + (size_t)(y - a.M) * a.V) + lo;
     const int n = min(a.V - lo, kSegment);
@@ -275,7 +273,7 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, const
 
 // What a node's workgroup shares.
 struct NodeShared {
-    int child[GHD_MAX_M], token[GHD_MAX_M], kids, taken, place[kNodeWaves], last[kNodeWaves];
+    int child[GHD_MAX_M], token[GHD_MAX_M], kids, taken, final, place[kNodeWaves], last[kNodeWaves];
     double u0, u[GHD_MAX_M], weight[GHD_MAX_M], part[2][kNodeWaves], sums[kKeep / kSide][kNodeWaves];
     Reach reach;
     uint32_t out[kMaxSegments * kSegment / 32];  // a bit for each token that has been rejected
@@ -340,19 +338,48 @@ __device__ __forceinline__ int draw_from_segments(const SampleArgs& a, NodeShare
     return first != 0x7fffffff ? first : last;
 }
 
+// A node's result - the accepted child or -1, and the token drawn where there is none - and, from the workgroup that is last to have
+// one, the walk.  Results and their count are atomics of the device's scope, which pass the XCDs' own caches; a workgroup counts itself when
+// its result has been acknowledged.  (A launch of its own for the walk: 3 us of the host and as much of the GPU.)
+__device__ __forceinline__ void node_is_done(const SampleArgs& a, NodeShared& s, uint64_t* nodes, uint32_t* arrived, int node, int taken, int token)
+{
+    const int tid = threadIdx.x;
+    __syncthreads();                             // (all of it is done with the inputs, where the result may be written)
+    if (tid == 0) {
+        __hip_atomic_store(nodes + node, (uint64_t)(uint32_t)token << 32 | (uint32_t)taken, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        s.final = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.M - 1;
+    }
+    __syncthreads();
+    if (!s.final) return;
+    if (tid < a.M) {
+        const uint64_t r = __hip_atomic_load(nodes + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s.child[tid] = (int)(uint32_t)r;
+        s.token[tid] = (int)(r >> 32);
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    int at = 0, len = 1;
+    a.res[2] = 0;
+    // (a child comes after its node and is one of the tree's: at most M steps, whatever nodes hold that the walk does not come to)
+    for (; s.child[at] > at && s.child[at] < a.M; ++len) {
+        at = s.child[at];
+        a.res[2 + len] = at;
+    }
+    a.res[0] = len;
+    a.res[1] = s.token[at];
+}
+
 // One workgroup a node.
 template <bool DRAFTS>
 __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, const Segment* __restrict__ seg, const First* __restrict__ firsts,
-                                                               const Rest* __restrict__ rest, int segments, NodeResult* __restrict__ out)
+                                                               const Rest* __restrict__ rest, int segments, uint64_t* nodes, uint32_t* arrived)
 {
     __shared__ NodeShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, node = blockIdx.x;
     if constexpr (DRAFTS) {
-        if (firsts[node].accepted) {
-            if (tid == 0) out[node] = {firsts[node].child, -1};
-            return;
-        }
-        if (!reached(a, firsts, node, s.reach)) return;            // (the walk does not look at it)
+        if (firsts[node].accepted) return node_is_done(a, s, nodes, arrived, node, firsts[node].child, -1);
+        if (!reached(a, firsts, node, s.reach)) return node_is_done(a, s, nodes, arrived, node, -1, -1);
     }
     const float* row = a.logits + (size_t)node * a.V;
     const double c = kLog2e / (double)a.temperature;
@@ -387,9 +414,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
         for (int j = 0; j < k; ++j) is = is || s.token[j] == s.token[k];
         return is;
     };
-    auto finish = [&](int taken, int token) {
-        if (tid == 0) out[node] = {taken, token};
-    };
+    auto finish = [&](int taken, int token) { node_is_done(a, s, nodes, arrived, node, taken, token); };
 
     if constexpr (!DRAFTS) {
         // A child is accepted if u (what is left) < its weight.  What is left before a child: the tokens that no child has, and the
@@ -566,29 +591,12 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
     }
 }
 
-__global__ __launch_bounds__(GHD_MAX_M) void k_sample_walk(const NodeResult* __restrict__ nodes, int M, int32_t* __restrict__ res)
-{
-    __shared__ NodeResult s_node[GHD_MAX_M];
-    const int tid = threadIdx.x;
-    if (tid < M) s_node[tid] = nodes[tid];
-    __syncthreads();
-    if (tid != 0) return;
-    int node = 0, len = 1;
-    res[2] = 0;
-    for (; s_node[node].taken > node; ++len) {   // (a child comes after its node: at most M steps)
-        node = s_node[node].taken;
-        res[2 + len] = node;
-    }
-    res[0] = len;
-    res[1] = s_node[node].token;
-}
-
 static int sample_segments(int V) { return ceil_div(V, kSegment); }
 static size_t sample_rest_at(int V) { return align_up((size_t)2 * GHD_MAX_M * sample_segments(V) * sizeof(Segment), 256); }
 static size_t sample_first_at(int V) { return sample_rest_at(V) + align_up((size_t)GHD_MAX_M * sample_segments(V) * sizeof(Rest), 256); }
 static size_t sample_nodes_at(int V) { return sample_first_at(V) + align_up(GHD_MAX_M * sizeof(First), 256); }
 
-size_t accept_sampled_bytes(int M, int V) { return sample_nodes_at(V) + align_up(GHD_MAX_M * sizeof(NodeResult), 256); }
+size_t accept_sampled_bytes(int M, int V) { return sample_nodes_at(V) + GHD_MAX_M * 8 + 256; }
 
 ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
 {
@@ -596,9 +604,10 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
     Segment* seg = (Segment*)ws;
     Rest* rest = (Rest*)((char*)ws + sample_rest_at(a.V));
     First* firsts = (First*)((char*)ws + sample_first_at(a.V));
-    NodeResult* nodes = (NodeResult*)((char*)ws + sample_nodes_at(a.V));
+    uint64_t* nodes = (uint64_t*)((char*)ws + sample_nodes_at(a.V));
+    uint32_t* arrived = (uint32_t*)(nodes + GHD_MAX_M);
     const int segments = sample_segments(a.V);
-    hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a, seg);
+    hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a, seg, arrived);
     ghd_status s = check_launch();
     if (s) return s;
     if (a.q_logits) {
@@ -607,13 +616,11 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
         hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, (const Segment*)seg, (const First*)firsts, rest);
         if ((s = check_launch())) return s;
         hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)firsts,
-                           (const Rest*)rest, segments, nodes);
+                           (const Rest*)rest, segments, nodes, arrived);
     } else {
         hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)nullptr,
-                           (const Rest*)nullptr, segments, nodes);
+                           (const Rest*)nullptr, segments, nodes, arrived);
     }
-    if ((s = check_launch())) return s;
-    hipLaunchKernelGGL(k_sample_walk, dim3(1), dim3(GHD_MAX_M), 0, st, (const NodeResult*)nodes, a.M, a.res);
     return check_launch();
 }
 
