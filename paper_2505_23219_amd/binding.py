@@ -784,10 +784,12 @@ def ghd_block_bounds_read(bounds: BlockBounds, block0: int, blocks: int, hi: Opt
     """What the bounds stand for: float [nkv, blocks, d], largest and smallest key of each channel."""
     shape, dev = (bounds.nkv, blocks, bounds.d), bounds.data.get_device()
     data = _here("bounds", bounds.data, torch.uint8, None, dev)
-    if hi is None:
-        hi = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
-    if lo is None:
-        lo = torch.empty(shape, dtype=torch.float32, device=bounds.data.device)
+    if hi is None and lo is None:
+        hi, lo = torch.empty((2,) + shape, dtype=torch.float32, device=bounds.data.device).unbind(0)
+    elif hi is None:
+        hi = torch.empty_like(lo)
+    elif lo is None:
+        lo = torch.empty_like(hi)
     st = (_lib or lib()).ghd_block_bounds_read(_here("hi", hi, torch.float32, shape, dev), _here("lo", lo, torch.float32, shape, dev), data,
                                                block0, blocks, bounds.nkv, bounds.d, bounds.capacity, _stream_of(dev))
     if st:

@@ -53,6 +53,7 @@ struct First {
     double one, one_q;                           // one over the sums of the target's and the draft's row, 0 where those are
     float top, top_q;                            // their maxima
     int child, accepted;                         // the first child whose token is in the vocabulary, or GHD_MAX_M
+    int reached, unused;                         // k_sample_rest's, where it is not accepted: whether the walk can come to the node
 };
 
 template <class T>
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(64) void k_sample_first(SampleArgs a, const Segment
     const RowSum p(seg + (size_t)node * segments, segments, lane, c), q(seg + (size_t)(a.M + qr) * segments, segments, lane, cq);
     if (lane != 0) return;
     const double px = Weights(p.top, c)(lp) * p.one, qx = Weights(q.top, cq)(lq) * q.one;
-    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(u) * qx < px};
+    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(u) * qx < px, 0, 0};
 }
 
 // Can the walk come to a node?  By what its ancestors' first children are: accepted, no other child of theirs is tried, rejected, not
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(64) void k_sample_first(SampleArgs a, const Segment
 struct Reach {
     int up[GHD_MAX_M], lost[GHD_MAX_M];
 };
-__device__ __forceinline__ bool reached(const SampleArgs& a, const First* first, int node, Reach& s)
+__device__ __forceinline__ bool can_be_reached(const SampleArgs& a, const First* first, int node, Reach& s)
 {
     const int i = threadIdx.x;
     int up = -1, lost = 0;
@@ -226,14 +227,16 @@ __device__ __forceinline__ bool reached(const SampleArgs& a, const First* first,
 }
 
 // What is left of a segment when the first child of a node is rejected: then beta is 1.
-__global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, const Segment* __restrict__ seg, const First* __restrict__ firsts,
-                                                             Rest* __restrict__ rest)
+__global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First* firsts, Rest* __restrict__ rest)
 {
     __shared__ Reach s_reach;
     __shared__ double s_sum[2][kRowThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, node = blockIdx.y, lo = blockIdx.x * kSegment, segments = gridDim.x;
     const First first = firsts[node];
-    if (first.child == GHD_MAX_M || first.accepted || !reached(a, firsts, node, s_reach)) return;
+    if (first.accepted || (first.child == GHD_MAX_M && blockIdx.x != 0)) return;
+    const bool reached = can_be_reached(a, firsts, node, s_reach);
+    if (blockIdx.x == 0 && tid == 0) firsts[node].reached = reached;
+    if (first.child == GHD_MAX_M || !reached) return;
     const int x = a.tokens[first.child], qr = draft_row(a, node);
     const float *row = a.logits + (size_t)node * a.V, *q_row = a.q_logits + (size_t)qr * a.V;
     const int n = min(a.V - lo, kSegment);
@@ -275,7 +278,6 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, const
 struct NodeShared {
     int child[GHD_MAX_M], token[GHD_MAX_M], kids, taken, final, place[kNodeWaves], last[kNodeWaves];
     double u0, u[GHD_MAX_M], weight[GHD_MAX_M], part[2][kNodeWaves], sums[kKeep / kSide][kNodeWaves];
-    Reach reach;
     uint32_t out[kMaxSegments * kSegment / 32];  // a bit for each token that has been rejected
     __device__ __forceinline__ bool rejected(int t) const { return out[t >> 5] >> (t & 31) & 1; }
 };
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, node = blockIdx.x;
     if constexpr (DRAFTS) {
         if (firsts[node].accepted) return node_is_done(a, s, nodes, arrived, node, firsts[node].child, -1);
-        if (!reached(a, firsts, node, s.reach)) return node_is_done(a, s, nodes, arrived, node, -1, -1);
+        if (!firsts[node].reached) return node_is_done(a, s, nodes, arrived, node, -1, -1);
     }
     const float* row = a.logits + (size_t)node * a.V;
     const double c = kLog2e / (double)a.temperature;
@@ -613,7 +615,7 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
     if (a.q_logits) {
         hipLaunchKernelGGL(k_sample_first, dim3(a.M), dim3(64), 0, st, a, (const Segment*)seg, segments, firsts);
         if ((s = check_launch())) return s;
-        hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, (const Segment*)seg, (const First*)firsts, rest);
+        hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, firsts, rest);
         if ((s = check_launch())) return s;
         hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)firsts,
                            (const Rest*)rest, segments, nodes, arrived);
