@@ -53,6 +53,13 @@ struct SparseArgs {
     float scale;
 };
 size_t sparse_attention_bytes(int M, int kv_len, int nh, int nkv, int d);
+// Halves of the `count` blocks of a list that hold rows: the last block may end in its first half (`total` rows are there, and a block's
+// first).
+__host__ __device__ static inline int sparse_halves(int count, int last_block, int total)
+{
+    return 2 * count - (count > 0 && last_block * kBlock + kBlock / 2 >= total);
+}
+void sparse_attention_on_host(int M, int kv_len, int nh, int nkv, int d, int64_t* out4);
 ghd_status launch_sparse_attention(SparseArgs a, int d, void* ws, size_t ws_bytes, hipStream_t st);    // GHD_ERR_WORKSPACE: too small
 
 struct SampleArgs {

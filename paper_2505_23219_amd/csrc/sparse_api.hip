@@ -207,4 +207,14 @@ ghd_status ghd_accept_sampled(const float* logits, const int32_t* tokens_dev, co
     return launch_accept_sampled(a, ws, (hipStream_t)stream);
 }
 
+/* Test support (not part of the documented ABI): out4 = {tiles of 16 rows in a block of an attention call, blocks of a key head, parts of
+ * what a block reads, bytes of workspace that it needs}. */
+void ghd_debug_sparse_attention(int M, int kv_len, int nh, int nkv, int d, int64_t* out4)
+{
+    sparse_attention_on_host(M, kv_len, nh, nkv, d, out4);
+}
+
+/* Halves of blocks that a list of `count` blocks, the last of them `last_block`, gives the wavefronts. */
+int ghd_debug_sparse_halves(int count, int last_block, int total) { return sparse_halves(count, last_block, total); }
+
 }  // extern "C"

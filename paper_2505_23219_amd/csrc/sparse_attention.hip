@@ -119,7 +119,7 @@ struct SparseScan {
 template <int D>
 struct SparseUnit {
     half8 k[2][D / 32], v[D / 16];
-    // (there: how many of the unit's keys there are; others are read as the last of them)
+    // (there: how many of the unit's keys there are, one at least; others are read as the last of them)
     __device__ __forceinline__ void load_k(const SparseArgs& a, int head, int key0, int there, int lane)
     {
         const int key = 8 * ((lane & 15) >> 2) + (lane & 3);
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
         tile_bits[r] = tile_tokens(a, row0 + r * 16, i0);
     }
     SparseState<D> st[RT];
-    const int units = 2 * count;
+    const int units = sparse_halves(count, list.block[max(count - 1, 0)], total);
     auto key_of = [&](int u) { return __builtin_amdgcn_readfirstlane(list.block[u >> 1]) * kBlock + (u & 1) * 32; };
     // One pass over the wavefront's units.  PLAIN: every row meets all of a unit's values, those that it does not see with
     // the probability 0; an infinity or NaN there is no 0 then.  Otherwise a row takes the values that it sees one by one.
@@ -345,11 +345,11 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
         if (u >= units) return;
         SparseUnit<D> unit;
         int key0 = key_of(u);
-        unit.load_k(a, head, key0, max(1, min(32, total - key0)), lane);
-        unit.load_v(a, head, key0, max(1, min(32, total - key0)), lane);
+        unit.load_k(a, head, key0, min(32, total - key0), lane);
+        unit.load_v(a, head, key0, min(32, total - key0), lane);
         for (;;) {
             const int next = u + W < units ? u + W : u, next0 = key_of(next), there = total - key0;
-            const int next_there = max(1, min(32, total - next0));
+            const int next_there = min(32, total - next0);
             const bool rest = key0 >= a.n * kBlock;                // behind the blocks
             const uint64_t bits = rest ? ~0ull : uniform64(list.bits[0][u >> 1]);
             if (there < 32) unit.clean(there, lane);
@@ -767,6 +767,15 @@ size_t sparse_attention_bytes(int M, int kv_len, int nh, int nkv, int d)
 {
     const size_t tiles = ceil_div(M * (nh / nkv), 16) + 7, most = kv_len / kBlock + 1 + ceil_div(M, kBlock);
     return sparse_bytes(std::max(std::min<size_t>(2048, nkv * tiles * most), most > kList ? nkv * tiles * ((most + kList - 1) / kList) : 0), d);
+}
+
+void sparse_attention_on_host(int M, int kv_len, int nh, int nkv, int d, int64_t* out4)
+{
+    const SparseCut c = sparse_cut(M, kv_len, nh, nkv, d);
+    out4[0] = c.rows;
+    out4[1] = c.blocks;
+    out4[2] = c.splits;
+    out4[3] = sparse_bytes(sparse_units(c, nkv), d);
 }
 
 template <int D, int RT, bool STAGED>
