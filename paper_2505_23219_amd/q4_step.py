@@ -1,10 +1,10 @@
 """A decoder stack with weights and cache in 4 bits, verified a token tree at a time.
 
-    python -m paper_2505_23219_amd.q4_step [--shape tiny|7b|13b] [--layers L] [--tokens N] [--kv-heads N]
+    python -m paper_2505_23219_amd.q4_step [--shape tiny|7b|13b] [--layers L] [--tokens N] [--kv-heads N] [--temperature T]
 
 The linear layers, the cache and its attention, acceptance and commit are the library's
-(ghd_linear_q4, ghd_kv_append_q4, ghd_tree_attention_q4, ghd_accept_greedy_static,
-ghd_commit_path_q4, ghd_embed); the norms, the residual and the SwiGLU between them are torch
+(ghd_linear_q4, ghd_kv_append_q4, ghd_tree_attention_q4, ghd_accept_greedy_static or, with a temperature,
+ghd_accept_sampled, ghd_commit_path_q4, ghd_embed); the norms, the residual and the SwiGLU between them are torch
 elementwise operations in fp32, each rounded once to the fp16 that the next linear layer reads.
 Run as a module it decodes from random weights, one token a step and then with drafted trees, and
 prints how many steps each took and whether they wrote the same tokens.  (Sums of a tree are taken in
@@ -110,14 +110,16 @@ class Q4Stack:
         B.ghd_commit_path_q4(self.cache, res, M, kv_len)
 
 
-def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: Sequence[int], draft=None
-           ) -> Tuple[List[int], int, float]:
-    """At least `count` tokens behind `first`, greedily: (tokens, steps, seconds).  parent: the tree of
-    every step; draft(written) -> the tokens of its nodes 1 .. M - 1 (none for a tree of one node)."""
+def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: Sequence[int], draft=None, temperature: float = 0.0,
+           generator: Optional[torch.Generator] = None) -> Tuple[List[int], int, float]:
+    """At least `count` tokens behind `first`: (tokens, steps, seconds).  parent: the tree of every step;
+    draft(written) -> the tokens of its nodes 1 .. M - 1 (none for a tree of one node).  Greedily, or, with a
+    temperature above 0, as sampled token by token from softmax(logits / temperature) with numbers of `generator`."""
     M = len(parent)
     tree = torch.tensor(parent, dtype=torch.int32, device=table.device)
     res = torch.empty(2 + M, dtype=torch.int32, device=table.device)
     amax = torch.empty(M, dtype=torch.int32, device=table.device)
+    room = B.workspace(B.ghd_accept_sampled_workspace_bytes(M, stack.shape.V), table.device) if temperature > 0 else None
     written: List[int] = []
     kv_len = steps = 0
     root = first
@@ -126,7 +128,11 @@ def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: 
     while len(written) < count:
         nodes = torch.tensor([root] + (draft(written) if M > 1 else []), dtype=torch.int32, device=table.device)
         logits = stack.step(B.ghd_embed(table, nodes), tree, kv_len)
-        B.ghd_accept_greedy_static(logits, nodes, tree, res, amax)
+        if room is None:
+            B.ghd_accept_greedy_static(logits, nodes, tree, res, amax)
+        else:
+            u = torch.rand(M, generator=generator, device=table.device)
+            B.ghd_accept_sampled(logits, nodes, tree, u, temperature, res=res, ws=room)
         stack.commit(res, M, kv_len)
         r = res.tolist()
         taken, root = r[0], r[1]
@@ -146,6 +152,8 @@ def main() -> None:
     ap.add_argument("--kv-heads", type=int, default=0, help="0: as many as query heads")
     ap.add_argument("--tokens", type=int, default=32)
     ap.add_argument("--group", type=int, choices=(32, 64, 128), default=128)
+    ap.add_argument("--temperature", type=float, default=0.0, help="0: greedy")
+    ap.add_argument("--seed", type=int, default=0, help="of the numbers that tokens are sampled with")
     a = ap.parse_args()
     shape = wl.with_layers(shapes[a.shape], a.layers)
     parent = wl.tree_medusa(16, (4, 2, 1, 1), 1).tolist()
@@ -156,7 +164,8 @@ def main() -> None:
     table = wl.embedding_table(shape, 0, "cuda")
 
     decode(stack, table, 1, 2, [-1])                       # first calls load the kernels
-    plain, steps, sec = decode(stack, table, 1, a.tokens, [-1])
+    numbers = torch.Generator("cuda").manual_seed(a.seed)
+    plain, steps, sec = decode(stack, table, 1, a.tokens, [-1], temperature=a.temperature, generator=numbers)
     print("one token a step : %d tokens in %d steps, %.2f ms a step" % (len(plain), steps, 1e3 * sec / steps))
 
     depth = [0] * len(parent)
@@ -173,10 +182,10 @@ def main() -> None:
             out.append(plain[at] if right else (i * 7919) % shape.V)
         return out
 
-    tree, steps, sec = decode(stack, table, 1, a.tokens, parent, draft)
-    same = tree[:a.tokens] == plain[:a.tokens]
-    print("trees of %d nodes: %d tokens in %d steps, %.2f ms a step, same tokens: %s"
-          % (len(parent), len(tree), steps, 1e3 * sec / steps, same))
+    tree, steps, sec = decode(stack, table, 1, a.tokens, parent, draft, a.temperature, numbers)
+    # (sampled runs have numbers of their own, and so tokens)
+    end = "" if a.temperature > 0 else ", same tokens: %s" % (tree[:a.tokens] == plain[:a.tokens])
+    print("trees of %d nodes: %d tokens in %d steps, %.2f ms a step%s" % (len(parent), len(tree), steps, 1e3 * sec / steps, end))
 
 
 if __name__ == "__main__":
