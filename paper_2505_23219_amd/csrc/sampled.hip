@@ -22,11 +22,12 @@ constexpr double kLog2e = 1.4426950408889634;
 // Softmax weights of a row: 2^((l - m) c), c = log2 e / T.  NaN and minus infinity have none; where the maximum is
 // infinity only such logits have one.
 struct Weights {
-    double c, off;
+    double c, from;
     float top;
-    __device__ __forceinline__ Weights(float m, double c) : c(c), off(-(double)m * c), top(m) {}
-    // (fmax takes the number of a number and NaN; 2^-1100 is 0)
-    __device__ __forceinline__ double exponent(float l) const { return fmax(fma((double)l, c, off), -1100.0); }
+    __device__ __forceinline__ Weights(float m, double c) : c(c), from((double)m), top(m) {}
+    // (The difference is exact, or all but: l c - m c in one instruction is off by 2^-53 of m c, which at a temperature of 1e-15 is
+    // no small exponent.  fmax takes the number of a number and NaN; 2^-1100 is 0.)
+    __device__ __forceinline__ double exponent(float l) const { return fmax(((double)l - from) * c, -1100.0); }
     __device__ __forceinline__ double operator()(float l) const
     {
         if (!(fabsf(top) < INFINITY)) return top > 0.f && l == top ? 1.0 : 0.0;

@@ -100,9 +100,10 @@ ghd_status ghd_block_select(uint64_t* sel_dev, const void* q, const void* bounds
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!at16(ws)) return GHD_ERR_ALIGN;
     if (ws_bytes < select_bytes(M, n, nkv)) return GHD_ERR_WORKSPACE;
-    const size_t held = (size_t)nkv * ceil_div(M, 64) * n * 8;
-    if (meet(sel_dev, held, q, (size_t)M * nh * d * 2) || meet(sel_dev, held, bounds, bounds_bytes(nkv, d, capacity / kBlock)) ||
-        meet(sel_dev, held, ws, select_bytes(M, n, nkv)))
+    const size_t held = (size_t)nkv * ceil_div(M, 64) * n * 8, q_bytes = (size_t)M * nh * d * 2, used = select_bytes(M, n, nkv);
+    const size_t b_bytes = bounds_bytes(nkv, d, capacity / kBlock);
+    if (meet(sel_dev, held, q, q_bytes) || meet(sel_dev, held, bounds, b_bytes) || meet(sel_dev, held, ws, used) || meet(ws, used, q, q_bytes) ||
+        meet(ws, used, bounds, b_bytes))
         return GHD_ERR_SHAPE;
     SelectArgs a = {};
     a.sel = sel_dev;
@@ -142,11 +143,19 @@ ghd_status ghd_sparse_attention(void* out, const void* q, const void* k_cache, c
         return GHD_ERR_ALIGN;
     if (!ws) return GHD_ERR_WORKSPACE;
     if (!at16(ws)) return GHD_ERR_ALIGN;
-    const size_t held = (size_t)M * nh * d * 2;
-    if ((out != q && meet(out, held, q, held)) || meet(out, held, k_cache, k_bytes(nkv, rows, d, k_stride_head, k_stride_tok)) ||
-        meet(out, held, v_cache, v_bytes(nkv, rows, d, v_stride_head, v_stride_ch)) ||
-        meet(out, held, sel_dev, (size_t)nkv * ceil_div(M, 64) * n * 8) || meet(out, held, parent_dev, (size_t)M * 4) ||
-        meet(out, held, mask_dev, (size_t)M * 16) || meet(out, held, ws, ws_bytes))
+    // neither what is written nor the workspace meets what is read (out may be q: a workgroup writes the rows that it has read)
+    int64_t cut[4];
+    sparse_attention_on_host(M, kv_len, nh, nkv, d, cut);
+    const size_t held = (size_t)M * nh * d * 2, used = cut[3] < (int64_t)ws_bytes ? cut[3] : ws_bytes;
+    const struct {
+        const void* p;
+        size_t n;
+    } read[] = {{q, held}, {k_cache, k_bytes(nkv, rows, d, k_stride_head, k_stride_tok)}, {v_cache, v_bytes(nkv, rows, d, v_stride_head, v_stride_ch)},
+                {sel_dev, (size_t)nkv * ceil_div(M, 64) * n * 8}, {parent_dev, (size_t)M * 4}, {mask_dev, (size_t)M * 16}};
+    for (const auto& r : read)
+        if ((r.p != out && meet(out, held, r.p, r.n)) || meet(ws, used, r.p, r.n)) return GHD_ERR_SHAPE;
+    if (meet(out, held, ws, used) || out == k_cache || out == v_cache || out == (const void*)sel_dev || out == (const void*)parent_dev ||
+        out == (const void*)mask_dev)
         return GHD_ERR_SHAPE;
     SparseArgs a = {};
     a.out = (half_t*)out;
@@ -190,7 +199,11 @@ ghd_status ghd_accept_sampled(const float* logits, const int32_t* tokens_dev, co
         return GHD_ERR_ALIGN;
     if (!ws || ws_bytes < accept_sampled_bytes(M, V)) return GHD_ERR_WORKSPACE;
     if (!at16(ws)) return GHD_ERR_ALIGN;
-    if (meet(res_dev, (size_t)(2 + M) * 4, ws, accept_sampled_bytes(M, V))) return GHD_ERR_SHAPE;
+    // (the result is written when all else has been read: it may lie where an input is)
+    const size_t used = accept_sampled_bytes(M, V), row = (size_t)V * 4, ints = (size_t)M * 4;
+    if (meet(ws, used, res_dev, ints + 8) || meet(ws, used, logits, M * row) || meet(ws, used, q_logits, q_rows * row) || meet(ws, used, tokens_dev, ints) ||
+        meet(ws, used, parent_dev, ints) || meet(ws, used, u_dev, ints) || meet(ws, used, q_row_dev, ints))
+        return GHD_ERR_SHAPE;
     SampleArgs a = {};
     a.logits = logits;
     a.q_logits = q_logits;

@@ -228,16 +228,20 @@ __device__ __forceinline__ void values_one_by_one(const SparseArgs& a, int head,
         }
     }
 }
+// Has a row met such a value?  (Its sum of probabilities is finite then; otherwise it is the scores that are not.)
 template <int D, int RT>
 __device__ __forceinline__ bool not_finite(const SparseState<D> (&st)[RT])
 {
     bool odd = false;
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int r = 0; r < RT; ++r) {
+        bool mine = false;
 #pragma unroll
         for (int ct = 0; ct < D / 16; ++ct)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(st[r].o[ct][e]) < INFINITY);
+            for (int e = 0; e < 4; ++e) mine = mine || !(fabsf(st[r].o[ct][e]) < INFINITY);
+        odd = odd || (mine && fabsf(sum_over_groups(st[r].l)) < INFINITY);
+    }
     return odd;
 }
 

@@ -133,6 +133,18 @@ def test_sharp_and_flat():
         _check(_case(8, 3000, "random", "rows", seed, 0.7), 0.7, q_T=1.3)
 
 
+@pytest.mark.parametrize("T", [1e-10, 1e-15, 1e-20, 1e-38])
+def test_next_to_no_temperature(T):
+    """The likeliest token has all of the probability, at whatever height its logit is."""
+    for draft in ("none", "rows"):
+        for V in (300, 40000):
+            case = _case(12, V, "random", draft, 3)
+            case[0].add_(1000.0)
+            want = _check(case, T)
+            got = want[2:]
+            assert want[1] == int(case[0][got[-1]].argmax())
+
+
 def test_drafts_far_from_and_equal_to_the_target():
     for seed in range(8):
         case = _case(30, 700, "random", "rows", seed, near=8.0)

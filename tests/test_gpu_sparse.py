@@ -93,6 +93,7 @@ def _check_select(q, k, kd, kv_len, count, sinks, recent, **kw):
     (1, 8, 8, 128, 64, 1, 0, 0), (1, 8, 2, 128, 2000, 9, 1, 2), (5, 20, 4, 64, 1931, 7, 0, 1), (16, 4, 4, 64, 4095, 31, 2, 2),
     (17, 6, 3, 128, 1100, 5, 0, 0), (64, 2, 2, 128, 1300, 3, 1, 1), (65, 4, 1, 64, 700, 10, 1, 1), (128, 2, 2, 64, 1000, 6, 3, 3),
     (3, 16, 1, 128, 17000, 64, 1, 1), (2, 2, 2, 64, 33000, 300, 1, 1), (4, 4, 4, 128, 640, 10, 1, 1), (4, 4, 4, 128, 640, 50, 20, 20),
+    (6, 2, 1, 64, 50000, 40, 1, 1), (9, 2, 1, 64, 100000, 70, 1, 2), (70, 1, 1, 64, 140000, 20, 0, 1), (2, 2, 1, 64, 330000, 100, 1, 1),
     (2, 4, 2, 128, 700, 0, 0, 0), (2, 4, 2, 128, 700, 4, 4, 0), (2, 4, 2, 64, 700, 4, 0, 4), (1, 256, 1, 64, 300, 2, 0, 0)])
 def test_select(M, nh, nkv, d, kv_len, count, sinks, recent):
     k, _, kd, _ = _cache(nkv, kv_len + M, d, kv_len + M)
@@ -100,13 +101,14 @@ def test_select(M, nh, nkv, d, kv_len, count, sinks, recent):
     _check_select(q, k, kd, kv_len, count, sinks, recent)
 
 
+@pytest.mark.parametrize("M,n", [(3, 300), (3, 700), (9, 900), (6, 1500), (1, 5000)])
 @pytest.mark.parametrize("kinds", [1, 2, 5])
-def test_select_takes_the_lowest_of_equal_blocks(kinds):
-    n, d = 700, 64
+def test_select_takes_the_lowest_of_equal_blocks(kinds, M, n):
+    d = 64
     some = torch.randn(kinds, 64, d, generator=_gen(kinds)).half()
     k = some[torch.arange(n) * 7 % kinds].reshape(1, n * 64, d).repeat(2, 1, 1)
-    q = torch.randn(3, 2, d, generator=_gen(9)).half()
-    for count in (1, 2, 257, 300, 699):
+    q = torch.randn(M, 2, d, generator=_gen(9)).half()
+    for count in (1, 2, 257, n - 1):
         _check_select(q, k, k.cuda(), n * 64, count, 1, 0)
 
 
@@ -268,6 +270,20 @@ def test_a_bad_row_reaches_who_sees_it(M, rep, d, bad):
                     assert not torch.isfinite(mine[:, 5]).any()
                     keep = [c for c in range(d) if c != 5]
                     assert ((mine - other).abs() <= 2.0 ** -10 * (other.abs() + 0.05))[:, keep].all()
+
+
+def test_a_token_whose_queries_are_none():
+    """An infinity or NaN among a token's queries is that token's alone, bit for bit."""
+    for M, rep, d in ((3, 2, 64), (24, 1, 128), (60, 1, 128), (100, 1, 64), (128, 2, 128)):
+        _, _, kd, vd = _cache(2, 840, d, 3)
+        q = torch.randn(M, 2 * rep, d, generator=_gen(4)).half().cuda()
+        sel, (rel, _) = P.words(_selection(2, M, 10, 3, 1, pool=6)).cuda(), _relation("random", M, 1)
+        want = B.ghd_sparse_attention(q, kd, vd, sel, 700, **rel)
+        q[M // 2, 1, 5], q[M - 1, 0, 7] = math.nan, math.inf
+        got = B.ghd_sparse_attention(q, kd, vd, sel, 700, **rel)
+        same = torch.ones(M, 2 * rep, dtype=torch.bool)
+        same[M // 2, 1] = same[M - 1, 0] = False
+        assert torch.equal(got[same], want[same]) and torch.isnan(got[M // 2, 1]).all()
 
 
 def test_in_place_over_any_workspace_and_behind_it():

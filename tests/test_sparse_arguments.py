@@ -79,7 +79,13 @@ nan, inf = float("nan"), float("inf")
     (_attend, ALIGN, dict(sel=FAR[6] + 4)), (_attend, ALIGN, dict(mask=FAR[9] + 4, parent=None)), (_attend, WORKSPACE, dict(ws=None)),
     (_attend, WORKSPACE, dict(ws_bytes=0)), (_attend, ALIGN, dict(ws=FAR[8] + 8)), (_attend, SHAPE, dict(out=FAR[1] + 16)),
     (_attend, SHAPE, dict(out=FAR[2] + 4096)), (_attend, SHAPE, dict(out=FAR[4])), (_attend, SHAPE, dict(out=FAR[6])),
-    (_attend, SHAPE, dict(out=FAR[7])), (_attend, SHAPE, dict(out=FAR[8] + 256)),
+    (_attend, SHAPE, dict(out=FAR[7])), (_attend, SHAPE, dict(out=FAR[8] + 256)), (_attend, SHAPE, dict(out=FAR[2])),
+    (_attend, SHAPE, dict(ws=FAR[1] - 256)), (_attend, SHAPE, dict(ws=FAR[2] + 1024)), (_attend, SHAPE, dict(ws=FAR[4] + 1024)),
+    (_attend, SHAPE, dict(ws=FAR[6])), (_attend, SHAPE, dict(ws=FAR[7])), (_attend, SHAPE, dict(ws=FAR[9] - 256, mask=FAR[9], parent=None)),
+    (_attend, SHAPE, dict(kt=(1 << 24) + 8)), (_attend, SHAPE, dict(vc=(1 << 22) + 8)),
+    (_select, SHAPE, dict(ws=FAR[1] - 64)), (_select, SHAPE, dict(ws=FAR[2] + 16)),
+    (_accept, SHAPE, dict(ws=FAR[0] + 4096)), (_accept, SHAPE, dict(ws=FAR[6] - 64, q=FAR[6], rows=8)), (_accept, SHAPE, dict(ws=FAR[1] - 64)),
+    (_accept, SHAPE, dict(ws=FAR[2])), (_accept, SHAPE, dict(ws=FAR[3])), (_accept, SHAPE, dict(ws=FAR[7] - 256, q=FAR[6], rows=8, row=FAR[7])),
     (_accept, NULL, dict(logits=None)), (_accept, NULL, dict(tokens=None)), (_accept, NULL, dict(parent=None)), (_accept, NULL, dict(u=None)),
     (_accept, NULL, dict(res=None)), (_accept, NULL, dict(row=FAR[7])), (_accept, SHAPE, dict(M=0)), (_accept, SHAPE, dict(M=129)),
     (_accept, SHAPE, dict(V=0)), (_accept, SHAPE, dict(V=262145)), (_accept, SHAPE, dict(T=0.0)), (_accept, SHAPE, dict(T=-1.0)),
