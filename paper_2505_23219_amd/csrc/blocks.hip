@@ -1,5 +1,6 @@
 // Bounds of blocks of keys, and which blocks each drafted token reads (sparse.h has the layout, include/ghd.h the rules).
 #include "sparse.h"
+#include "wave.h"
 
 namespace ghd {
 
@@ -265,10 +266,8 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
         low = min(low, key);
         high = max(high, key);
     });
-    for (int off = 32; off > 0; off >>= 1) {
-        low = min(low, (uint32_t)__shfl_xor((int)low, off));
-        high = max(high, (uint32_t)__shfl_xor((int)high, off));
-    }
+    low = ~wave_highest(~low);
+    high = wave_highest(high);
     for (int i = tid; i < 256; i += TEAM) s.hist[i] = 0;
     if (tid == 0) s.n = 0;
     if constexpr (TEAM > 64) {
@@ -296,12 +295,7 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
             uint32_t c[4], sum = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum += c[e] = s.hist[255 - 4 * tid - e];
-            uint32_t before = sum;
-#pragma unroll
-            for (int off = 1; off < 64; off *= 2) {
-                const uint32_t o = (uint32_t)__shfl_up((int)before, off);
-                if (tid >= off) before += o;
-            }
+            uint32_t before = running_sum(sum);
             before -= sum;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

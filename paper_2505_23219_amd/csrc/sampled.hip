@@ -9,6 +9,7 @@
 // 2^-24 / sqrt(V) of its largest terms, by random roundings of single weights, and what 64 bits would accept or draw is
 // what is accepted or drawn but where a random number lies as close to a border.
 #include "sparse.h"
+#include "wave.h"
 
 namespace ghd {
 
@@ -43,6 +44,19 @@ struct Weights {
     }
 };
 
+// What the first loads need comes in the first twelve words of the arguments, which the hardware puts into scalar registers before a
+// kernel starts; the argument block, host memory, is 0.6 us away.
+#define SAMPLE_FIRST(FIFTH) const float *logits, const int32_t *tokens, const int32_t *parent, const float *u, FIFTH, int M, int V
+__device__ __forceinline__ void sample_first(SampleArgs& a, const float* logits, const int32_t* tokens, const int32_t* parent, const float* u, int M, int V)
+{
+    a.logits = logits;
+    a.tokens = tokens;
+    a.parent = parent;
+    a.u = u;
+    a.M = M;
+    a.V = V;
+}
+
 struct Segment {
     double sum;                                  // of weights against the segment's maximum
     float top, unused;
@@ -56,23 +70,6 @@ struct First {
     int child, accepted;                         // the first child whose token is in the vocabulary, or GHD_MAX_M
     int reached, unused;                         // k_sample_rest's, where it is not accepted: whether the walk can come to the node
 };
-
-template <class T>
-__device__ __forceinline__ T wave_sum(T x)
-{
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
-    return x;
-}
-__device__ __forceinline__ float wave_max_of(float x)
-{
-    for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
-    return x;
-}
-__device__ __forceinline__ int wave_max_of(int x)
-{
-    for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off));
-    return x;
-}
 
 // Node c as a child: asked for before it is known whose child it is.
 struct Child {
@@ -96,17 +93,21 @@ struct RowSum {
         Segment s = {0.0, -INFINITY, 0.f};
         if (lane < segments) s = seg[lane];
         mine = s.top;
-        top = wave_max_of(s.top);
+        top = wave_highest(s.top);
         part = s.sum * Weights(top, c)(s.top);
-        const double sum = wave_sum(part);
+        double sum = wave_sum(part);
+        asm volatile("" : "+v"(top), "+v"(sum));     // (known to be uniform they cost k_sample_nodes' loop of rejections 106 spilled registers)
         one = sum > 0.0 ? 1.0 / sum : 0.0;
     }
 };
 
 // Target rows (blockIdx.y < M), without the tokens of the node's children where drafts have no probabilities; draft rows.
 // Bound: the bytes of the logits.
-__global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segment* __restrict__ seg, uint32_t* __restrict__ arrived)
+__global__ __launch_bounds__(kRowThreads) void k_sample_rows(SAMPLE_FIRST(const float* q_logits), SampleArgs a, Segment* __restrict__ seg,
+                                                             uint32_t* __restrict__ arrived)
 {
+    sample_first(a, logits, tokens, parent, u, M, V);
+    a.q_logits = q_logits;
     __shared__ uint32_t s_out[kSegment / 32];
     __shared__ double s_sum[kRowThreads / 64];
     __shared__ float s_top[kRowThreads / 64];
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segme
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) top = fmaxf(top, l[i]);
-    top = wave_max_of(top);
+    top = wave_highest(top);
     if ((tid & 63) == 0) s_top[tid >> 6] = top;
     __syncthreads();
 #pragma unroll
@@ -162,8 +163,8 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segme
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) sum += (double)weight.low(l[i]);
-    sum = wave_sum(sum);
-    if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
+    sum = running_sum(sum);
+    if ((tid & 63) == 63) s_sum[tid >> 6] = sum;
     __syncthreads();
     if (tid == 0) {
         sum = 0.0;
@@ -173,24 +174,25 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rows(SampleArgs a, Segme
 }
 
 // A wavefront a node: its rows' sums, and whether its first child is accepted.
-__global__ __launch_bounds__(64) void k_sample_first(SampleArgs a, const Segment* __restrict__ seg, int segments, First* __restrict__ out)
+__global__ __launch_bounds__(64) void k_sample_first(SAMPLE_FIRST(const Segment* __restrict__ seg), SampleArgs a, int segments, First* __restrict__ out)
 {
+    sample_first(a, logits, tokens, parent, u, M, V);
     const int lane = threadIdx.x, node = blockIdx.x, qr = draft_row(a, node);
     const Child low(a, lane), high(a, lane + 64);
     const double c = kLog2e / (double)a.temperature, cq = kLog2e / (double)a.q_temperature;
     const uint64_t in_low = __ballot(low.of(a, node) && in_vocabulary(a, low.token)), in_high = __ballot(high.of(a, node) && in_vocabulary(a, high.token));
     const int at = in_low ? (int)__builtin_ctzll(in_low) : in_high ? (int)__builtin_ctzll(in_high) : 0;
     const int x = __shfl(in_low ? low.token : high.token, at), child = in_low ? at : in_high ? at + 64 : GHD_MAX_M;
-    float lp = 0.f, lq = 0.f, u = 0.f;
+    float lp = 0.f, lq = 0.f, number = 0.f;
     if (child < GHD_MAX_M) {
         lp = a.logits[(size_t)node * a.V + x];
         lq = a.q_logits[(size_t)qr * a.V + x];
-        u = a.u[child];
+        number = a.u[child];
     }
     const RowSum p(seg + (size_t)node * segments, segments, lane, c), q(seg + (size_t)(a.M + qr) * segments, segments, lane, cq);
     if (lane != 0) return;
     const double px = Weights(p.top, c)(lp) * p.one, qx = Weights(q.top, cq)(lq) * q.one;
-    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(u) * qx < px, 0, 0};
+    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(number) * qx < px, 0, 0};
 }
 
 // Can the walk come to a node?  By what its ancestors' first children are: accepted, no other child of theirs is tried, rejected, not
@@ -258,9 +260,9 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First
         s += is ? fmax(wp(lp[i]) * first.one - qt, 0.0) : 0.0;
         r += qt;
     }
-    s = wave_sum(s);
-    r = wave_sum(r);
-    if (lane == 0) {
+    s = running_sum(s);
+    r = running_sum(r);
+    if (lane == 63) {
         s_sum[0][tid >> 6] = s;
         s_sum[1][tid >> 6] = r;
     }
@@ -289,16 +291,11 @@ template <class Weight>
 __device__ __forceinline__ int draw_from_segments(const SampleArgs& a, NodeShared& s, double part, int segments, const Weight& weight)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    double upto = part;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const double o = __shfl_up(upto, off);
-        if (lane >= off) upto += o;
-    }
-    const double goal = s.u0 * __shfl(upto, 63);
+    const double upto = running_sum(part);
+    const double goal = s.u0 * lane_of(upto, 63);
     const uint64_t over = __ballot(part > 0.0 && upto > goal), some = __ballot(part > 0.0);
     if (some == 0) return -1;
-    const int at = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some);
+    const int at = __builtin_amdgcn_readfirstlane(over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some));
     // a thread has some neighbours of it
     double w[kSide], sum = 0.0;
 #pragma unroll
@@ -307,16 +304,11 @@ __device__ __forceinline__ int draw_from_segments(const SampleArgs& a, NodeShare
         w[e] = t < a.V ? weight(t) : 0.0;
         sum += w[e];
     }
-    double run = sum;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const double o = __shfl_up(run, off);
-        if (lane >= off) run += o;
-    }
+    const double run = running_sum(sum);
     __syncthreads();
     if (lane == 63) s.part[0][wave] = run;
     __syncthreads();
-    double before = (at > 0 ? __shfl(upto, at - 1) : 0.0) + run - sum;
+    double before = (at > 0 ? lane_of(upto, max(at - 1, 0)) : 0.0) + run - sum;
     for (int v = 0; v < wave; ++v) before += s.part[0][v];
     // the first that passes, or the last that has a weight (the segment's own sum was larger by a rounding)
     int first = 0x7fffffff, last = -1;
@@ -327,8 +319,8 @@ __device__ __forceinline__ int draw_from_segments(const SampleArgs& a, NodeShare
         last = at * kSegment + tid * kSide + e;
         if (before > goal && first == 0x7fffffff) first = last;
     }
-    first = -wave_max_of(-first);
-    last = wave_max_of(last);
+    first = -wave_highest(-first);
+    last = wave_highest(last);
     if (lane == 0) {
         s.place[wave] = first;
         s.last[wave] = last;
@@ -375,9 +367,10 @@ __device__ __forceinline__ void node_is_done(const SampleArgs& a, NodeShared& s,
 
 // One workgroup a node.
 template <bool DRAFTS>
-__global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, const Segment* __restrict__ seg, const First* __restrict__ firsts,
+__global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(const Segment* __restrict__ seg), SampleArgs a, const First* __restrict__ firsts,
                                                                const Rest* __restrict__ rest, int segments, uint64_t* nodes, uint32_t* arrived)
 {
+    sample_first(a, logits, tokens, parent, u, M, V);
     __shared__ NodeShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, node = blockIdx.x;
     if constexpr (DRAFTS) {
@@ -426,7 +419,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
             float top = p.top;
             for (int k = lane; k < kids; k += 64)
                 if (in_vocabulary(a, s.token[k])) top = fmaxf(top, row[s.token[k]]);
-            top = wave_max_of(top);
+            top = wave_highest(top);
             const Weights weight(top, c);
             const double others = p.one > 0.0 ? weight(p.top) / p.one : 0.0;
             for (int k = lane; k < kids; k += 64)
@@ -438,7 +431,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
                 for (int j = kids - 1; j >= k; --j) left += s.weight[j];
                 if (s.u[k] * left < s.weight[k]) first = min(first, k);
             }
-            first = -wave_max_of(-first);
+            first = -wave_highest(-first);
             if (lane == 0) s.taken = first < GHD_MAX_M ? s.child[first] : -1;
         }
         __syncthreads();
@@ -486,6 +479,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
                 if (lane < segments) first = rest[(size_t)node * segments + lane];
                 all = wave_sum(first.p);
                 all_q = wave_sum(first.q);
+                asm volatile("" : "+v"(all), "+v"(all_q));
             } else {
                 const bool shows = rest_q > 1e-25 && alpha < 1e25;
                 if (small && shows && !kept) {
@@ -536,9 +530,9 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
                         sq += qt;
                     }
                 }
-                sp = wave_sum(sp);
-                sq = wave_sum(sq);
-                if (lane == 0) {
+                sp = running_sum(sp);
+                sq = running_sum(sq);
+                if (lane == 63) {
                     s.part[0][wave] = sp;
                     s.part[1][wave] = sq;
                 }
@@ -571,8 +565,8 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
                 float some = 0.f;
 #pragma unroll
                 for (int i = kSide * v; i < kSide * (v + 1); ++i) some += fmaxf(fmaf(-by_low, keep_q[i], fmaf(-by_high, keep_q[i], keep_p[i])), 0.f);
-                const double w = wave_sum((double)some * p.one);
-                if (lane == 0) s.sums[v][wave] = w;
+                const double w = running_sum((double)some * p.one);
+                if (lane == 63) s.sums[v][wave] = w;
                 __builtin_amdgcn_sched_barrier(0);
             }
             __syncthreads();
@@ -582,9 +576,9 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SampleArgs a, con
             for (int v = 0; v < segments; ++v) {
                 double w = 0.0;
                 for (int t = v * kSegment + tid; t < min((v + 1) * kSegment, a.V); t += kNodeThreads) w += left_of(t);
-                w = wave_sum(w);
+                w = running_sum(w);
                 __syncthreads();
-                if (lane == 0) s.part[0][wave] = w;
+                if (lane == 63) s.part[0][wave] = w;
                 __syncthreads();
                 if (v == lane)
                     for (int i = 0; i < kNodeWaves; ++i) part += s.part[0][i];
@@ -610,18 +604,22 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
     uint64_t* nodes = (uint64_t*)((char*)ws + sample_nodes_at(a.V));
     uint32_t* arrived = (uint32_t*)(nodes + GHD_MAX_M);
     const int segments = sample_segments(a.V);
-    hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a, seg, arrived);
+    hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a.logits,
+                       a.tokens, a.parent, a.u, a.q_logits, a.M, a.V, a, seg, arrived);
     ghd_status s = check_launch();
     if (s) return s;
     if (a.q_logits) {
-        hipLaunchKernelGGL(k_sample_first, dim3(a.M), dim3(64), 0, st, a, (const Segment*)seg, segments, firsts);
+        hipLaunchKernelGGL(k_sample_first, dim3(a.M), dim3(64), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M, a.V, a, segments,
+                           firsts);
         if ((s = check_launch())) return s;
         hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, firsts, rest);
         if ((s = check_launch())) return s;
-        hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)firsts,
+        hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
+                           a.V, a, (const First*)firsts,
                            (const Rest*)rest, segments, nodes, arrived);
     } else {
-        hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a, (const Segment*)seg, (const First*)nullptr,
+        hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
+                           a.V, a, (const First*)nullptr,
                            (const Rest*)nullptr, segments, nodes, arrived);
     }
     return check_launch();

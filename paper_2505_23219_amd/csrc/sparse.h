@@ -50,7 +50,7 @@ struct SparseArgs {
     int64_t k_head, k_tok, v_head, v_ch;
     float *o_part, *ml_part;
     int M, kv_len, nh, nkv, rep, n;
-    float scale;
+    float scale, inv_rep;            // (rep, 1 / rep, n and the workspace's parts are the launch's)
 };
 size_t sparse_attention_bytes(int M, int kv_len, int nh, int nkv, int d);
 // Halves of the `count` blocks of a list that hold rows: the last block may end in its first half (`total` rows are there, and a block's

@@ -8,6 +8,7 @@
 // infinity there.
 #include "sparse.h"
 #include "attention_impl.h"
+#include "wave.h"
 
 namespace ghd {
 
@@ -16,7 +17,36 @@ typedef uint32_t uint4_ __attribute__((ext_vector_type(4)));
 // How a launch is divided: rows in `blocks` blocks, what a block of rows reads in `splits` parts.
 struct SparseCut {
     int rows, blocks, splits;                    // rows: tiles of 16 in a block
+    float inv_splits;                            // (a kernel's)
 };
+
+// What the first loads need comes in the first words of the arguments, which the hardware puts into scalar registers before a kernel
+// starts; the argument block, host memory, is 0.6 us away.
+// rows: kv_len (up to 2^21) | whether `relation` is masks << 31; heads: M | nkv - 1 << 8 | rep - 1 << 16; parts: splits | blocks << 16
+#define SPARSE_FIRST const uint64_t *sel, const half_t *q, const void *relation, uint32_t rows, uint32_t heads, uint32_t parts, float inv_rep, \
+                     float inv_splits
+__device__ __forceinline__ void sparse_first(SparseArgs& a, SparseCut& cut, SPARSE_FIRST)
+{
+    a.sel = sel;
+    a.q = q;
+    a.mask = rows >> 31 ? (const uint64_t*)relation : nullptr;
+    a.parent = rows >> 31 ? nullptr : (const int32_t*)relation;
+    a.kv_len = rows & 0x7fffffff;
+    a.n = a.kv_len / kBlock;
+    a.M = heads & 255;
+    a.nkv = (heads >> 8 & 255) + 1;
+    a.rep = (heads >> 16) + 1;
+    a.nh = a.nkv * a.rep;
+    a.inv_rep = inv_rep;
+    cut.splits = parts & 0xffff;
+    cut.blocks = parts >> 16;
+    cut.inv_splits = inv_splits;
+}
+static uint32_t sparse_heads(const SparseArgs& a) { return (uint32_t)a.M | (a.nkv - 1) << 8 | (a.rep - 1) << 16; }
+static uint32_t sparse_parts(const SparseCut& c) { return (uint32_t)c.splits | (uint32_t)c.blocks << 16; }
+// x / n of whole numbers, x below 2^20, by 1 / n: half a unit above x the quotient is at least 1 / (2 n) from a whole number, and
+// what is rounded in it is less than x / n 2^-22
+__device__ __forceinline__ int over(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
 
 constexpr int kList = 1024;                      // blocks of a workgroup's list: the host divides a head's so that they fit
 template <bool WIDE>
@@ -76,12 +106,7 @@ struct SparseScan {
             mine += word[j].some();
         }
         for (int b = tid + kKept * THREADS; b < n; b += THREADS) mine += at(b).some();
-        int before = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const int o = __shfl_up(before, off);
-            if (lane >= off) before += o;
-        }
+        int before = running_sum(mine);
         if (lane == 63) s.part[wave] = before;
         __syncthreads();
         before -= mine;
@@ -246,10 +271,10 @@ __device__ __forceinline__ bool not_finite(const SparseState<D> (&st)[RT])
 }
 
 // Which token a column is, and which of a workgroup's tokens a tile of rows has.
-__device__ __forceinline__ int token_of(const SparseArgs& a, int row) { return min(row / a.rep, a.M - 1); }
+__device__ __forceinline__ int token_of(const SparseArgs& a, int row) { return min(over(row, a.inv_rep), a.M - 1); }
 __device__ __forceinline__ uint64_t tile_tokens(const SparseArgs& a, int row0, int i0)
 {
-    const int from = row0 / a.rep - i0, to = token_of(a, row0 + 15) - i0;
+    const int from = over(row0, a.inv_rep) - i0, to = token_of(a, row0 + 15) - i0;
     return from > to ? 0 : (to - from >= 63 ? ~0ull : (1ull << (to - from + 1)) - 1) << from;
 }
 __device__ __forceinline__ uint64_t uniform64(uint64_t x)
@@ -261,7 +286,7 @@ template <int D>
 __device__ __forceinline__ half8 sparse_query(const SparseArgs& a, int head, int row, int s, int g)
 {
     row = min(row, a.M * a.rep - 1);
-    const int token = row / a.rep;
+    const int token = over(row, a.inv_rep);
     const half8 x = *(const half8*)(a.q + ((size_t)token * a.nh + head * a.rep + row - token * a.rep) * D + s * 32 + g * 8);
     return a.scale < 0.f ? -x : x;
 }
@@ -271,7 +296,7 @@ __device__ __forceinline__ float sparse_power(float scale) { return fmaxf(fabsf(
 // a row's output from the sums and their divisor; a row that sees no key gives zeros
 __device__ __forceinline__ void sparse_out(const SparseArgs& a, int head, int row, int d, int ct, int g, floatx4 o, float l)
 {
-    const int token = row / a.rep;
+    const int token = over(row, a.inv_rep);
     const float r = 1.f / l;
     half4 y;
 #pragma unroll
@@ -287,8 +312,9 @@ struct SparseShape {
 };
 
 template <int D, int RT>
-__global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse_attention(SparseArgs a, SparseCut cut)
+__global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse_attention(SPARSE_FIRST, SparseArgs a, SparseCut cut)
 {
+    sparse_first(a, cut, sel, q, relation, rows, heads, parts, inv_rep, inv_splits);
     typedef SparseShape<D, RT> S;
     constexpr int CT = S::CT, KS = S::KS, W = S::kWaves;
     __shared__ SparseList<false> list;
@@ -299,8 +325,8 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
     // 8 XCDs by blocks, by parts in eights: the row blocks of a part of a head's keys share an L2
     const int item = blockIdx.y * 8 + (blockIdx.x & 7);
     if (item >= a.nkv * cut.splits) return;
-    const int block = blockIdx.x >> 3, head = item / cut.splits, split = item - head * cut.splits;
-    const int row0 = block * RT * 16, R = a.M * a.rep, i0 = row0 / a.rep, i1 = min((row0 + RT * 16 - 1) / a.rep, a.M - 1);
+    const int block = blockIdx.x >> 3, head = __builtin_amdgcn_readfirstlane(over(item, cut.inv_splits)), split = item - head * cut.splits;
+    const int row0 = block * RT * 16, R = a.M * a.rep, i0 = over(row0, a.inv_rep), i1 = token_of(a, row0 + RT * 16 - 1);
     const int total = a.kv_len + a.M, tail = (total - a.n * kBlock + kBlock - 1) / kBlock;
     SparseScan<S::kThreads, false> scan(a, head, i0, i1);
     constexpr int kMine = (RT * KS + W - 1) / W;                   // operands of q that a wavefront brings
@@ -503,8 +529,9 @@ struct StagedBlock {
 };
 
 template <int D, int RT>
-__global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCut cut)
+__global__ __launch_bounds__(512, 2) void k_sparse_staged(SPARSE_FIRST, SparseArgs a, SparseCut cut)
 {
+    sparse_first(a, cut, sel, q, relation, rows, heads, parts, inv_rep, inv_splits);
     constexpr int CT = D / 16, KS = D / 32, W = 8, kLoads = 2 * StagedShape<D>::kPieces;
     constexpr bool WIDE = RT > 1;
     __shared__ SparseList<WIDE> list;
@@ -515,16 +542,16 @@ __global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCu
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     const int item = blockIdx.y * 8 + (blockIdx.x & 7);
     if (item >= a.nkv * cut.splits) return;
-    const int block = blockIdx.x >> 3, head = item / cut.splits, split = item - head * cut.splits;
-    const int row0 = block * RT * 64, R = a.M * a.rep, i0 = row0 / a.rep, i1 = token_of(a, row0 + RT * 64 - 1);
+    const int block = blockIdx.x >> 3, head = __builtin_amdgcn_readfirstlane(over(item, cut.inv_splits)), split = item - head * cut.splits;
+    const int row0 = block * RT * 64, R = a.M * a.rep, i0 = over(row0, a.inv_rep), i1 = token_of(a, row0 + RT * 64 - 1);
     const int total = a.kv_len + a.M, tail = (total - a.n * kBlock + kBlock - 1) / kBlock;
     const int group = wave >> 1, half = wave & 1, my_row = row0 + group * RT * 16;
     SparseScan<512, WIDE> scan(a, head, i0, i1);
-    half8 q[RT][KS];
+    half8 ask[RT][KS];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[r][s] = sparse_query<D>(a, head, my_row + r * 16 + col, s, g);
+        for (int s = 0; s < KS; ++s) ask[r][s] = sparse_query<D>(a, head, my_row + r * 16 + col, s, g);
     int up0 = 0, up1 = 0;
     if (wave == 0 && a.parent) {
         up0 = a.parent[min(lane, a.M - 1)];
@@ -541,7 +568,7 @@ __global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCu
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[r][s]));
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(ask[r][s]));
     for (int i = 0; i < min(count, kStages - 1); ++i) request(i);
     if (before_tail < count) {
         if (!a.parent)
@@ -551,7 +578,7 @@ __global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCu
     }
     const float c = sparse_power(a.scale);
     // (128 tokens are in two words: of a group of 32 rows in one of them)
-    const bool second = my_row / a.rep - i0 >= 64;
+    const bool second = over(my_row, a.inv_rep) - i0 >= 64;
     const int base = i0 + (second ? 64 : 0);
     int token[RT];
     uint64_t tile_bits[RT];
@@ -596,7 +623,7 @@ __global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCu
                 for (int h = 0; h < 2; ++h) {
                     s[h] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[h][ks], q[r][ks], s[h], 0, 0, 0);
+                    for (int ks = 0; ks < KS; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[h][ks], ask[r][ks], s[h], 0, 0, 0);
                 }
                 if (r == 0) {
 #pragma unroll
@@ -667,8 +694,14 @@ __global__ __launch_bounds__(512, 2) void k_sparse_staged(SparseArgs a, SparseCu
 
 // Parts to rows: four wavefronts take the parts of a fragment, 16 channels by 16 rows, in turn, eight requests at a time.
 template <int D>
-__global__ __launch_bounds__(256) void k_sparse_join(SparseArgs a, SparseCut cut)
+__global__ __launch_bounds__(256) void k_sparse_join(const float* o_part, const float* ml_part, half_t* out, uint32_t heads, uint32_t parts, int rows,
+                                                     float inv_rep)
 {
+    SparseArgs a = {};
+    SparseCut cut = {};
+    sparse_first(a, cut, nullptr, nullptr, nullptr, 0, heads, parts, inv_rep, 0.f);
+    a.out = out;
+    cut.rows = rows;
     constexpr int CT = D / 16, kAt = 8;
     __shared__ floatx4 s_o[4][64];
     __shared__ floatx2 s_ml[4][16];
@@ -690,8 +723,8 @@ __global__ __launch_bounds__(256) void k_sparse_join(SparseArgs a, SparseCut cut
             ml[j] = (floatx2){-INFINITY, 0.f};
             v[j] = (floatx4){0.f, 0.f, 0.f, 0.f};
             if (is && part < cut.splits) {
-                ml[j] = ((const floatx2*)a.ml_part)[unit * 16 + col];
-                v[j] = ((const floatx4*)a.o_part)[(unit * CT + ct) * 64 + lane];
+                ml[j] = ((const floatx2*)ml_part)[unit * 16 + col];
+                v[j] = ((const floatx4*)o_part)[(unit * CT + ct) * 64 + lane];
             }
         }
 #pragma unroll
@@ -754,7 +787,7 @@ static SparseCut sparse_cut(int M, int kv_len, int nh, int nkv, int d)
             if (splits > 1) us += k.join + k.mb * 64e-6f * items * splits * k.rows * d;
             if (least == 0.f || us < least) {
                 least = us;
-                best = {k.rows, blocks, splits};
+                best = {k.rows, blocks, splits, 1.f / splits};
             }
         }
     }
@@ -785,12 +818,15 @@ void sparse_attention_on_host(int M, int kv_len, int nh, int nkv, int d, int64_t
 template <int D, int RT, bool STAGED>
 static ghd_status sparse_rows(const SparseArgs& a, const SparseCut& c, hipStream_t st)
 {
-    void (*const kernel)(SparseArgs, SparseCut) = STAGED ? k_sparse_staged<D, RT> : k_sparse_attention<D, RT>;
+    void (*const kernel)(SPARSE_FIRST, SparseArgs, SparseCut) = STAGED ? k_sparse_staged<D, RT> : k_sparse_attention<D, RT>;
     const int threads = STAGED ? 512 : SparseShape<D, RT>::kThreads;
     const size_t lds = STAGED ? StagedShape<D>::kLds : SparseShape<D, RT>::kLds;
     const ghd_status s = launch_resident_checked((const void*)kernel, threads, lds, nullptr);
     if (s) return s;
-    hipLaunchKernelGGL(kernel, dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(threads), lds, st, a, c);
+    hipLaunchKernelGGL(kernel, dim3(8 * c.blocks, ceil_div(a.nkv * c.splits, 8)), dim3(threads), lds, st, a.sel, a.q,
+                       a.mask ? (const void*)a.mask : (const void*)a.parent, (uint32_t)a.kv_len | (a.mask ? 1u << 31 : 0u),
+                       sparse_heads(a), sparse_parts(c),
+                       a.inv_rep, c.inv_splits, a, c);
     return check_launch();
 }
 
@@ -802,7 +838,8 @@ static ghd_status sparse_of(const SparseArgs& a, const SparseCut& c, hipStream_t
                          : c.rows == 4 ? sparse_rows<D, 1, true>(a, c, st)
                                        : sparse_rows<D, 2, true>(a, c, st);
     if (s || c.splits == 1) return s;
-    hipLaunchKernelGGL(k_sparse_join<D>, dim3(c.rows * (D / 16), c.blocks, a.nkv), dim3(256), 0, st, a, c);
+    hipLaunchKernelGGL(k_sparse_join<D>, dim3(c.rows * (D / 16), c.blocks, a.nkv), dim3(256), 0, st, a.o_part, a.ml_part, a.out, sparse_heads(a),
+                       sparse_parts(c), c.rows, a.inv_rep);
     return check_launch();
 }
 
@@ -811,6 +848,7 @@ ghd_status launch_sparse_attention(SparseArgs a, int d, void* ws, size_t ws_byte
     const SparseCut c = sparse_cut(a.M, a.kv_len, a.nh, a.nkv, d);
     if (ws_bytes < sparse_bytes(sparse_units(c, a.nkv), d)) return GHD_ERR_WORKSPACE;
     a.rep = a.nh / a.nkv;
+    a.inv_rep = 1.f / (float)a.rep;
     a.n = a.kv_len / kBlock;
     a.o_part = (float*)ws;
     a.ml_part = (float*)((char*)ws + sparse_o_bytes(sparse_units(c, a.nkv), d));
