@@ -101,8 +101,11 @@ __device__ __forceinline__ uint32_t score_key(float t)
 
 __device__ __forceinline__ uint32_t max_over_four(uint32_t x)
 {
-    x = max(x, (uint32_t)__shfl_xor((int)x, 16));
-    return max(x, (uint32_t)__shfl_xor((int)x, 32));
+    // (rows of 16 lanes, then halves, exchanged with themselves: each lane has one of both in either register)
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
 }
 
 // 16 channels' codes, those above zero (which meet HI) and those below (which meet LO), by pairs in fp16: a number times the two
@@ -124,6 +127,18 @@ __device__ __forceinline__ void query_codes(const half8 (&x)[2], half2_ first, h
         above[w] = (int32_t)__builtin_amdgcn_perm(up[1], up[0], 0x06040200u);
         below[w] = (int32_t)__builtin_amdgcn_perm(down[1], down[0], 0x06040200u);
     }
+}
+
+// What the first loads need, in the arguments that are in scalar registers when a kernel starts (see SAMPLE_FIRST).
+#define SELECT_FIRST const half_t *q, char *codes, float *units, int blocks, int M, int nkv, int rep, int n
+__device__ __forceinline__ void select_first(SelectArgs& a, SELECT_FIRST)
+{
+    a.q = q;
+    a.bounds = {codes, units, blocks};
+    a.M = M;
+    a.nkv = nkv;
+    a.rep = rep;
+    a.n = n;
 }
 
 // Blocks are the rows of the product, 16 tokens of one query head its columns.  A wavefront keeps the codes of TILES tiles of 16 blocks in
@@ -203,8 +218,9 @@ __device__ __forceinline__ void block_scores(const SelectArgs& a, int head, int 
 }
 
 template <int D, int TILES>
-__global__ __launch_bounds__(256) void k_block_scores(SelectArgs a)
+__global__ __launch_bounds__(256) void k_block_scores(SELECT_FIRST, SelectArgs a)
 {
+    select_first(a, q, codes, units, blocks, M, nkv, rep, n);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = (blockIdx.x * 4 + wave) * TILES * 16, head = blockIdx.y, m = blockIdx.z * 16 + (lane & 15);
     if (b0 >= a.n) return;
     if (a.zero && blockIdx.z == 0 && lane < TILES * 16 && b0 + lane < a.n)       // the picks set bits
@@ -384,8 +400,9 @@ __device__ __forceinline__ void store_eight(const SelectArgs& a, int head, int m
 // Scores and picks of few blocks in one launch: a workgroup has eight tokens of a head, whose scores stay in LDS.
 constexpr int kFewBlocks = 512;
 template <int D>
-__global__ __launch_bounds__(512) void k_block_few(SelectArgs a)
+__global__ __launch_bounds__(512) void k_block_few(SELECT_FIRST, SelectArgs a)
 {
+    select_first(a, q, codes, units, blocks, M, nkv, rep, n);
     __shared__ PickShared<64> s[8];
     __shared__ __attribute__((aligned(16))) uint32_t s_key[8][kFewBlocks + 4];
     __shared__ uint32_t s_bits[kFewBlocks / 4];
@@ -455,8 +472,8 @@ ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
     if (a.n == 0) return GHD_OK;
     if (a.n <= kFewBlocks) {
         const dim3 teams(a.nkv, ceil_div(a.M, 8));                  // (a head's tokens on one XCD, where its codes are)
-        if (d == 128) hipLaunchKernelGGL(k_block_few<128>, teams, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL(k_block_few<64>, teams, dim3(512), 0, st, a);
+        if (d == 128) hipLaunchKernelGGL(k_block_few<128>, teams, dim3(512), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
+        else hipLaunchKernelGGL(k_block_few<64>, teams, dim3(512), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
         return check_launch();
     }
     // a wavefront has 64 blocks, or 16 where there would be fewer than four wavefronts for each compute unit
@@ -465,11 +482,11 @@ ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
     const bool eight = a.n <= kPickBytes && a.M > 4;
     a.zero = !eight;
     if (d == 128) {
-        if (per == 4) hipLaunchKernelGGL((k_block_scores<128, 4>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_block_scores<128, 1>), grid, dim3(256), 0, st, a);
+        if (per == 4) hipLaunchKernelGGL((k_block_scores<128, 4>), grid, dim3(256), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
+        else hipLaunchKernelGGL((k_block_scores<128, 1>), grid, dim3(256), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
     } else {
-        if (per == 4) hipLaunchKernelGGL((k_block_scores<64, 4>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_block_scores<64, 1>), grid, dim3(256), 0, st, a);
+        if (per == 4) hipLaunchKernelGGL((k_block_scores<64, 4>), grid, dim3(256), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
+        else hipLaunchKernelGGL((k_block_scores<64, 1>), grid, dim3(256), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
     }
     const ghd_status s = check_launch();
     if (s) return s;
