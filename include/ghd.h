@@ -490,8 +490,8 @@ ghd_status ghd_kv_read_q4(void *k_out, void *v_out, const ghd_kv *kv_host, int L
  * committed rows, a token's queries are scored against them, and the attention reads the
  * blocks that a token has selected, the committed rows behind the last whole block, and the drafted
  * rows that the token sees.  The cache is the one of ghd_tree_attention, with nkv key heads:
- * nh % nkv == 0, query head h reads key head h / (nh / nkv).  nh <= 256, d in {64, 128},
- * kv_len <= 2^21.  Blocks are counted from row 0; kv_len / 64 are whole.
+ * nh % nkv == 0, query head h reads key head h / (nh / nkv).  nh <= 1024, nkv <= 256, d in {64, 128},
+ * kv_len <= 2^21, k_stride_tok <= 2^24 and v_stride_ch <= 2^22 for the attention.  Blocks are counted from row 0; kv_len / 64 are whole.
  *
  * Bounds of one layer (ghd_block_bounds_bytes, 16-byte aligned), of every block and channel: HI = ceil(max
  * K / s), LO = floor(min K / s), whole numbers within -127 .. 127, s = 2^(floor(log2 a) - 6) with a the
@@ -550,7 +550,8 @@ size_t ghd_sparse_attention_workspace_bytes(int M, int kv_len, int nh, int nkv, 
  *     where that is 0 throughout), and q without x, normalised
  * Where no child is accepted the next token is the first at which the running sum of p exceeds u[0] sum(p).
  *   u_dev    float [M], in [0, 1): u[c] tries node c, u[0] draws the last token
- *   res_dev  as ghd_accept_greedy's: length, next token, path; words behind the path are not written
+ *   res_dev  as ghd_accept_greedy's: length, next token, path; words behind the path are not written.  It is
+ *            written when all has been read, and may lie where an input does
  * NaN and -infinity among logits have the probability 0; where a row holds infinity its infinities share all of it.  The next
  * token is -1 where no token has a probability.  Tokens outside of the vocabulary are rejected.
  * Weights are 24 bits, their arguments and sums 64.  V <= 262144, q_rows <= GHD_MAX_M. */

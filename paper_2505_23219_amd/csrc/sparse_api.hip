@@ -11,12 +11,12 @@ static inline bool at_word(const void* p, size_t n) { return ((uintptr_t)p & (n 
 // do two ranges of memory share a byte?
 static inline bool meet(const void* a, size_t na, const void* b, size_t nb)
 {
-    return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+    return a && b && na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
 static bool heads_ok(int nh, int nkv, int d)
 {
-    return nh >= 1 && nh <= 256 && nkv >= 1 && nh % nkv == 0 && (d == 64 || d == 128);
+    return nh >= 1 && nh <= 1024 && nkv >= 1 && nkv <= 256 && nh % nkv == 0 && (d == 64 || d == 128);
 }
 static bool rows_ok(int M, int kv_len) { return M >= 1 && M <= GHD_MAX_M && kv_len >= 0 && kv_len <= kSparseMaxRows; }
 

@@ -197,6 +197,16 @@ def test_attention(M, nh, nkv, d, kv_len, count, kind, layout):
     _check(M, nh, nkv, d, kv_len, _selection(nkv, M, n, min(count, n), M + n), kind, layout)
 
 
+@pytest.mark.parametrize("M,nh,nkv,d,kv_len", [(16, 320, 40, 128, 333), (3, 312, 39, 64, 200), (1, 1024, 1, 128, 150), (5, 1024, 256, 64, 130),
+                                               (128, 1024, 2, 64, 70)])
+def test_many_query_heads(M, nh, nkv, d, kv_len):
+    """Tokens of all heads together, 40 key heads of eight and a row of 1024 heads among them."""
+    n = kv_len // 64
+    _check(M, nh, nkv, d, kv_len, _selection(nkv, M, n, min(2, n), M), "random", "tokens")
+    k, _, kd, _ = _cache(nkv, kv_len + M, d, kv_len)
+    _check_select(torch.randn(M, nh, d, generator=_gen(M)).half(), k, kd, kv_len, 1, 0, 0)
+
+
 def test_nothing_selected_and_nothing_seen():
     sel = torch.zeros((2, 9, 4), dtype=torch.bool)
     sel[1, 2, 3] = sel[0, 4, 0] = True

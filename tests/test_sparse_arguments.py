@@ -64,7 +64,7 @@ nan, inf = float("nan"), float("inf")
     (_read, B.GHD_OK, dict(n=0, hi=None, lo=None)),
     (_select, NULL, dict(sel=None)), (_select, NULL, dict(q=None)), (_select, NULL, dict(bounds=None)), (_select, SHAPE, dict(M=0)),
     (_select, SHAPE, dict(M=129)), (_select, SHAPE, dict(kv_len=-1)), (_select, SHAPE, dict(kv_len=(1 << 21) + 1)),
-    (_select, SHAPE, dict(nh=9)), (_select, SHAPE, dict(nh=260)), (_select, SHAPE, dict(nkv=0)), (_select, SHAPE, dict(d=32)),
+    (_select, SHAPE, dict(nh=9)), (_select, SHAPE, dict(nh=1028)), (_select, SHAPE, dict(nkv=0)), (_select, SHAPE, dict(d=32)),
     (_select, CAPACITY, dict(capacity=639)), (_select, SHAPE, dict(count=1)), (_select, SHAPE, dict(count=-1, sinks=0, recent=0)),
     (_select, SHAPE, dict(sinks=-1)), (_select, SHAPE, dict(recent=-1)), (_select, SHAPE, dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1)),
     (_select, WORKSPACE, dict(ws=None)), (_select, WORKSPACE, dict(ws_bytes=100)), (_select, ALIGN, dict(ws=FAR[3] + 8)),

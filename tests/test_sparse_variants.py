@@ -64,6 +64,17 @@ def test_no_half_of_a_block_lies_behind_the_rows():
     assert f(0, 0, 5) == 0
 
 
+def test_many_query_heads_fit_what_a_launch_holds():
+    """Blocks and parts are 16 bits each, tiles of rows 2^13 at the most."""
+    for nkv, rep in ((1, 1024), (2, 512), (40, 8), (204, 5), (256, 4), (256, 1)):
+        for M, kv_len in itertools.product((1, 16, 17, 128), (0, 64, 5000, 1 << 21)):
+            for d in (64, 128):
+                room = B.ghd_sparse_attention_workspace_bytes(M, kv_len, nkv * rep, nkv, d)
+                rows, blocks, splits, need = _cut(M, nkv * rep, nkv, d, kv_len)
+                assert 0 < need <= room and blocks < 1 << 16 and splits < 1 << 16
+                assert rows * blocks * 16 >= M * rep > rows * (blocks - 1) * 16
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("M,nh,nkv,d,kv_len", CASES)
 def test_variants(M, nh, nkv, d, kv_len):
