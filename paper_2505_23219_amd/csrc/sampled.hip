@@ -17,7 +17,6 @@ constexpr int kSegment = 4096;                   // logits of a row that a workg
 constexpr int kRowThreads = 256, kPerThread = kSegment / kRowThreads;
 constexpr int kNodeThreads = 512, kNodeWaves = kNodeThreads / 64, kSide = kSegment / kNodeThreads;
 constexpr int kMaxSegments = 64;                 // of the largest vocabulary, 262144
-constexpr int kKeep = 64;                        // tokens that a thread of a node's workgroup keeps the weights of
 constexpr double kLog2e = 1.4426950408889634;
 
 // Softmax weights of a row: 2^((l - m) c), c = log2 e / T.  NaN and minus infinity have none; where the maximum is
@@ -68,7 +67,8 @@ struct First {
     double one, one_q;                           // one over the sums of the target's and the draft's row, 0 where those are
     float top, top_q;                            // their maxima
     int child, accepted;                         // the first child whose token is in the vocabulary, or GHD_MAX_M
-    int reached, unused;                         // k_sample_rest's, where it is not accepted: whether the walk can come to the node
+    int reached;                                 // k_sample_rest's, where it is not accepted: whether the walk can come to the node
+    int more;                                    // whether there is a second such child
 };
 
 // Node c as a child: asked for before it is known whose child it is.
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(64) void k_sample_first(SAMPLE_FIRST(const Segment*
     const RowSum p(seg + (size_t)node * segments, segments, lane, c), q(seg + (size_t)(a.M + qr) * segments, segments, lane, cq);
     if (lane != 0) return;
     const double px = Weights(p.top, c)(lp) * p.one, qx = Weights(q.top, cq)(lq) * q.one;
-    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(number) * qx < px, 0, 0};
+    out[node] = {p.one, q.one, p.top, q.top, child, child < GHD_MAX_M && u_of(number) * qx < px, 0, __popcll(in_low) + __popcll(in_high) > 1};
 }
 
 // Can the walk come to a node?  By what its ancestors' first children are: accepted, no other child of theirs is tried, rejected, not
@@ -229,8 +229,12 @@ __device__ __forceinline__ bool can_be_reached(const SampleArgs& a, const First*
     return s.lost[node] == 0;
 }
 
-// What is left of a segment when the first child of a node is rejected: then beta is 1.
-__global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First* firsts, Rest* __restrict__ rest)
+// Kept weights: [node][segment][target, draft][kSegment]
+__host__ __device__ __forceinline__ size_t kept_at(int node, int segments, int segment) { return ((size_t)node * segments + segment) * 2 * kSegment; }
+
+// What is left of a segment when the first child of a node is rejected: then beta is 1.  Where there are other children, the weights against
+// the rows' maxima are kept, 0 for the rejected token: another rejection goes over all of them in one workgroup.
+__global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First* firsts, Rest* __restrict__ rest, float* __restrict__ kept)
 {
     __shared__ Reach s_reach;
     __shared__ double s_sum[2][kRowThreads / 64];
@@ -252,13 +256,18 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First
     }
     const Weights wp(first.top, kLog2e / (double)a.temperature), wq(first.top_q, kLog2e / (double)a.q_temperature);
     double s = 0.0, r = 0.0;
+    float* const keep = kept + kept_at(node, segments, blockIdx.x) + tid;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
         const int t = i * kRowThreads + tid;
         const bool is = t < n && lo + t != x;
-        const double qt = is ? wq(lq[i]) * first.one_q : 0.0;
-        s += is ? fmax(wp(lp[i]) * first.one - qt, 0.0) : 0.0;
+        const double pw = is ? wp(lp[i]) : 0.0, qw = is ? wq(lq[i]) : 0.0, qt = qw * first.one_q;
+        s += fmax(pw * first.one - qt, 0.0);
         r += qt;
+        if (first.more) {
+            keep[i * kRowThreads] = (float)pw;
+            keep[kSegment + i * kRowThreads] = (float)qw;
+        }
     }
     s = running_sum(s);
     r = running_sum(r);
@@ -280,7 +289,7 @@ __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First
 // What a node's workgroup shares.
 struct NodeShared {
     int child[GHD_MAX_M], token[GHD_MAX_M], kids, taken, final, place[kNodeWaves], last[kNodeWaves];
-    double u0, u[GHD_MAX_M], weight[GHD_MAX_M], part[2][kNodeWaves], sums[kKeep / kSide][kNodeWaves];
+    double u0, u[GHD_MAX_M], weight[GHD_MAX_M], part[2][kNodeWaves], sums[kMaxSegments][kNodeWaves], p[GHD_MAX_M], q[GHD_MAX_M];
     uint32_t out[kMaxSegments * kSegment / 32];  // a bit for each token that has been rejected
     __device__ __forceinline__ bool rejected(int t) const { return out[t >> 5] >> (t & 31) & 1; }
 };
@@ -368,7 +377,7 @@ __device__ __forceinline__ void node_is_done(const SampleArgs& a, NodeShared& s,
 // One workgroup a node.
 template <bool DRAFTS>
 __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(const Segment* __restrict__ seg), SampleArgs a, const First* __restrict__ firsts,
-                                                               const Rest* __restrict__ rest, int segments, uint64_t* nodes, uint32_t* arrived)
+                                                               const Rest* __restrict__ rest, float* kept, int segments, uint64_t* nodes, uint32_t* arrived)
 {
     sample_first(a, logits, tokens, parent, u, M, V);
     __shared__ NodeShared s;
@@ -456,22 +465,57 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
         const Weights wq(q.top_q, cq);
         auto p_of = [&](int t) { return wp(row[t]) * p.one; };
         auto q_of = [&](int t) { return wq(q_row[t]) * q.one_q; };
-        // A thread has every 512th token.  Of vocabularies up to 32768 it keeps the weights, 0 of what was rejected; what is left
-        // may be less than 32 bits' weights show: then they are worked out anew each time, as those of larger vocabularies are.
-        const bool small = a.V <= kKeep * kNodeThreads;
-        float keep_p[kKeep], keep_q[kKeep];
-        bool kept = false;
+        // the children's own, nothing of a token that an earlier child has
+        if (tid < kids) {
+            const int x = s.token[tid];
+            const bool is = in_vocabulary(a, x) && !twice(tid);
+            s.p[tid] = is ? p_of(x) : 0.0;
+            s.q[tid] = is ? q_of(x) : 0.0;
+        }
+        __syncthreads();
+        // Weights in 32 bits, 0 of what was rejected, are there if a second child is; what is left may be less than those show: then
+        // they are worked out anew each time.  over_kept: of segment after segment the lane's part of p - by q, in units of the row's
+        // weights, and of q: eight tokens' in 32 bits, the factor in two parts.
+        float* const w = kept + kept_at(node, segments, 0);
+        auto over_kept = [&](double by, auto to) {
+            const float by_high = (float)by, by_low = (float)(by - (double)by_high);
+            const floatx4* from = (const floatx4*)w + tid;
+            auto some = [&](int v, const floatx4 (&x)[4]) {
+                float left = 0.f, left_q = 0.f;
+#pragma unroll
+                for (int e = 0; e < kSide; ++e) {
+                    const float pw = x[e / 4][e % 4], qw = x[2 + e / 4][e % 4];
+                    left += fmaxf(fmaf(-by_low, qw, fmaf(-by_high, qw, pw)), 0.f);
+                    left_q += qw;
+                }
+                to(v, left, left_q);
+            };
+            constexpr int kAtOnce = 4, kStep = 2 * kSegment / 4;
+            for (int v0 = 0; v0 < segments; v0 += kAtOnce) {
+                floatx4 x[kAtOnce][4];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) x[i][f] = from[(size_t)min(v0 + i, segments - 1) * kStep + f * kNodeThreads];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                    if (v0 + i < segments) some(v0 + i, x[i]);
+            }
+        };
+        bool shows = q.more;
         double alpha = 1.0, beta = 0.0, rest_q = q.one_q > 0.0 ? 1.0 : 0.0;
         Rest first = {0.0, 0.0};                 // the lane's segment's, of what the first rejection leaves
         int tried = 0, k = 0;
         for (; k < kids; ++k) {
             const int x = s.token[k];
             if (!in_vocabulary(a, x)) continue;
-            const bool gone = twice(k);
-            const double px = gone ? 0.0 : fmax(alpha * (p_of(x) - beta * q_of(x)), 0.0), qx = gone || !(rest_q > 0.0) ? 0.0 : q_of(x) / rest_q;
+            const double px = fmax(alpha * (s.p[k] - beta * s.q[k]), 0.0), qx = rest_q > 0.0 ? s.q[k] / rest_q : 0.0;
             if (s.u[k] * qx < px) break;
             __syncthreads();                     // (the last round's bits and sums have been read)
-            if (tid == 0) s.out[x >> 5] |= 1u << (x & 31);
+            if (tid == 0) {
+                s.out[x >> 5] |= 1u << (x & 31);
+                if (q.more) w[kept_at(0, segments, x / kSegment) + x % kSegment] = w[kept_at(0, segments, x / kSegment) + kSegment + x % kSegment] = 0.f;
+            }
             __syncthreads();
             const double next = rest_q > 0.0 ? beta + 1.0 / (alpha * rest_q) : beta;
             double all, all_q;
@@ -481,45 +525,13 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                 all_q = wave_sum(first.q);
                 asm volatile("" : "+v"(all), "+v"(all_q));
             } else {
-                const bool shows = rest_q > 1e-25 && alpha < 1e25;
-                if (small && shows && !kept) {
-                    int me = tid;                // (here and now: otherwise all addresses would be kept, too)
-                    asm volatile("" : "+v"(me));
-#pragma unroll
-                    for (int i = 0; i < kKeep; ++i) {
-                        const int t = i * kNodeThreads + me, in = min(t, a.V - 1);
-                        keep_p[i] = row[in];
-                        keep_q[i] = q_row[in];
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int i = 0; i < kKeep; ++i) {
-                        const int t = i * kNodeThreads + me;
-                        const bool is = t < a.V && !s.rejected(min(t, a.V - 1));
-                        keep_p[i] = is ? wp.low(keep_p[i]) : 0.f;
-                        keep_q[i] = is ? wq.low(keep_q[i]) : 0.f;
-                        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
-                kept = small && shows;
+                shows = shows && rest_q > 1e-25 && alpha < 1e25;
                 double sp = 0.0, sq = 0.0;
-                if (kept) {
-                    // in weights against the maxima: p - (beta one_q / one) q, the factor in two parts, and sums of a few in 32 bits
-                    const double by = next * q.one_q / p.one;
-                    const float by_high = (float)by, by_low = (float)(by - (double)by_high);
-#pragma unroll
-                    for (int i0 = 0; i0 < kKeep; i0 += 8) {
-                        float some = 0.f, some_q = 0.f;
-#pragma unroll
-                        for (int i = i0; i < i0 + 8; ++i) {
-                            if (i * kNodeThreads + tid == x) keep_p[i] = keep_q[i] = 0.f;
-                            some += fmaxf(fmaf(-by_low, keep_q[i], fmaf(-by_high, keep_q[i], keep_p[i])), 0.f);
-                            some_q += keep_q[i];
-                        }
-                        sp += (double)some;
-                        sq += (double)some_q;
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                if (shows) {
+                    over_kept(next * q.one_q / p.one, [&](int, float left, float left_q) {
+                        sp += (double)left;
+                        sq += (double)left_q;
+                    });
                     sp *= p.one;
                     sq *= q.one_q;
                 } else {
@@ -557,18 +569,11 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
             part = p.part * p.one;
         } else if (tried == 1) {
             part = first.p;
-        } else if (kept) {
-            const double by = beta * q.one_q / p.one;
-            const float by_high = (float)by, by_low = (float)(by - (double)by_high);
-#pragma unroll
-            for (int v = 0; v < kKeep / kSide; ++v) {
-                float some = 0.f;
-#pragma unroll
-                for (int i = kSide * v; i < kSide * (v + 1); ++i) some += fmaxf(fmaf(-by_low, keep_q[i], fmaf(-by_high, keep_q[i], keep_p[i])), 0.f);
-                const double w = running_sum((double)some * p.one);
-                if (lane == 63) s.sums[v][wave] = w;
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        } else if (shows) {
+            over_kept(beta * q.one_q / p.one, [&](int v, float left, float) {
+                const double sum = running_sum((double)left * p.one);
+                if (lane == 63) s.sums[v][wave] = sum;
+            });
             __syncthreads();
             if (lane < segments)
                 for (int i = 0; i < kNodeWaves; ++i) part += s.sums[lane][i];
@@ -593,16 +598,19 @@ static size_t sample_rest_at(int V) { return align_up((size_t)2 * GHD_MAX_M * sa
 static size_t sample_first_at(int V) { return sample_rest_at(V) + align_up((size_t)GHD_MAX_M * sample_segments(V) * sizeof(Rest), 256); }
 static size_t sample_nodes_at(int V) { return sample_first_at(V) + align_up(GHD_MAX_M * sizeof(First), 256); }
 
-size_t accept_sampled_bytes(int M, int V) { return sample_nodes_at(V) + GHD_MAX_M * 8 + 256; }
+static size_t sample_kept_at(int V) { return sample_nodes_at(V) + align_up(GHD_MAX_M * 8 + 4, 256); }
+
+size_t accept_sampled_bytes(int M, int V) { return sample_kept_at(V) + kept_at(M, sample_segments(V), 0) * 4; }
 
 ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
 {
-    static_assert(kNodeThreads * kSide == kSegment && kKeep % kSide == 0 && kMaxSegments == 64, "a segment's tokens are dealt evenly, a lane has a segment of a row");
+    static_assert(kNodeThreads * kSide == kSegment && kSide == 8 && kMaxSegments == 64, "a segment's tokens are dealt evenly, a lane has a segment of a row");
     Segment* seg = (Segment*)ws;
     Rest* rest = (Rest*)((char*)ws + sample_rest_at(a.V));
     First* firsts = (First*)((char*)ws + sample_first_at(a.V));
     uint64_t* nodes = (uint64_t*)((char*)ws + sample_nodes_at(a.V));
     uint32_t* arrived = (uint32_t*)(nodes + GHD_MAX_M);
+    float* kept = (float*)((char*)ws + sample_kept_at(a.V));
     const int segments = sample_segments(a.V);
     hipLaunchKernelGGL(k_sample_rows, dim3(segments, a.M + (a.q_logits ? a.q_rows : 0)), dim3(kRowThreads), 0, st, a.logits,
                        a.tokens, a.parent, a.u, a.q_logits, a.M, a.V, a, seg, arrived);
@@ -612,15 +620,15 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
         hipLaunchKernelGGL(k_sample_first, dim3(a.M), dim3(64), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M, a.V, a, segments,
                            firsts);
         if ((s = check_launch())) return s;
-        hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, firsts, rest);
+        hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, firsts, rest, kept);
         if ((s = check_launch())) return s;
         hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
                            a.V, a, (const First*)firsts,
-                           (const Rest*)rest, segments, nodes, arrived);
+                           (const Rest*)rest, kept, segments, nodes, arrived);
     } else {
         hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
                            a.V, a, (const First*)nullptr,
-                           (const Rest*)nullptr, segments, nodes, arrived);
+                           (const Rest*)nullptr, kept, segments, nodes, arrived);
     }
     return check_launch();
 }
