@@ -11,6 +11,8 @@
 #include "sparse.h"
 #include "wave.h"
 
+#include <type_traits>
+
 namespace ghd {
 
 constexpr int kSegment = 4096;                   // logits of a row that a workgroup takes
@@ -490,16 +492,23 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                 }
                 to(v, left, left_q);
             };
-            constexpr int kAtOnce = 4, kStep = 2 * kSegment / 4;
-            for (int v0 = 0; v0 < segments; v0 += kAtOnce) {
-                floatx4 x[kAtOnce][4];
+            constexpr int kStep = 2 * kSegment / 4;
+            auto several = [&](int v0, auto count) {
+                constexpr int N = decltype(count)::value;
+                floatx4 x[N][4];
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
+                for (int i = 0; i < N; ++i)
 #pragma unroll
                     for (int f = 0; f < 4; ++f) x[i][f] = from[(size_t)min(v0 + i, segments - 1) * kStep + f * kNodeThreads];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
+                for (int i = 0; i < N; ++i)
                     if (v0 + i < segments) some(v0 + i, x[i]);
+            };
+            if (segments <= 2) {
+                several(0, std::integral_constant<int, 2>{});
+            } else {
+                for (int v0 = 0; v0 < segments; v0 += 8) several(v0, std::integral_constant<int, 8>{});
             }
         };
         bool shows = q.more;
