@@ -19,6 +19,7 @@ constexpr int kSegment = 4096;                   // logits of a row that a workg
 constexpr int kRowThreads = 256, kPerThread = kSegment / kRowThreads;
 constexpr int kNodeThreads = 512, kNodeWaves = kNodeThreads / 64, kSide = kSegment / kNodeThreads;
 constexpr int kMaxSegments = 64;                 // of the largest vocabulary, 262144
+constexpr int kAtOnce = 8;                       // segments whose kept weights a node's workgroup asks for
 constexpr double kLog2e = 1.4426950408889634;
 
 // Softmax weights of a row: 2^((l - m) c), c = log2 e / T.  NaN and minus infinity have none; where the maximum is
@@ -376,7 +377,7 @@ __device__ __forceinline__ void node_is_done(const SampleArgs& a, NodeShared& s,
     a.res[1] = s.token[at];
 }
 
-// One workgroup a node.
+// One workgroup a node.  DRAFTS: they have probabilities.
 template <bool DRAFTS>
 __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(const Segment* __restrict__ seg), SampleArgs a, const First* __restrict__ firsts,
                                                                const Rest* __restrict__ rest, float* kept, int segments, uint64_t* nodes, uint32_t* arrived)
@@ -476,39 +477,37 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
         }
         __syncthreads();
         // Weights in 32 bits, 0 of what was rejected, are there if a second child is; what is left may be less than those show: then
-        // they are worked out anew each time.  over_kept: of segment after segment the lane's part of p - by q, in units of the row's
-        // weights, and of q: eight tokens' in 32 bits, the factor in two parts.
+        // they are worked out anew each time.  In units of the target's weights what is left of a token is p - by q; `by` in two parts.
         float* const w = kept + kept_at(node, segments, 0);
+        struct Left {
+            float high, low;
+            __device__ __forceinline__ Left(double by) : high((float)by), low((float)(by - (double)high)) {}
+            __device__ __forceinline__ float operator()(float pw, float qw) const { return fmaxf(fmaf(-low, qw, fmaf(-high, qw, pw)), 0.f); }
+        };
+        // to(v, left, left_q): a thread's share of segment v, two times four neighbours of either row; eight segments are asked for at a time
         auto over_kept = [&](double by, auto to) {
-            const float by_high = (float)by, by_low = (float)(by - (double)by_high);
-            const floatx4* from = (const floatx4*)w + tid;
-            auto some = [&](int v, const floatx4 (&x)[4]) {
-                float left = 0.f, left_q = 0.f;
+            const Left left(by);
+            for (int v0 = 0; v0 < segments; v0 += kAtOnce) {
+                floatx4 has[kAtOnce][4];
+                const floatx4* from = (const floatx4*)(w + kept_at(0, segments, v0)) + tid;
 #pragma unroll
-                for (int e = 0; e < kSide; ++e) {
-                    const float pw = x[e / 4][e % 4], qw = x[2 + e / 4][e % 4];
-                    left += fmaxf(fmaf(-by_low, qw, fmaf(-by_high, qw, pw)), 0.f);
-                    left_q += qw;
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (v0 + i >= segments) continue;
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) has[i][f] = from[i * (2 * kSegment / 4) + f * kNodeThreads];
                 }
-                to(v, left, left_q);
-            };
-            constexpr int kStep = 2 * kSegment / 4;
-            auto several = [&](int v0, auto count) {
-                constexpr int N = decltype(count)::value;
-                floatx4 x[N][4];
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) x[i][f] = from[(size_t)min(v0 + i, segments - 1) * kStep + f * kNodeThreads];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (v0 + i < segments) some(v0 + i, x[i]);
-            };
-            if (segments <= 2) {
-                several(0, std::integral_constant<int, 2>{});
-            } else {
-                for (int v0 = 0; v0 < segments; v0 += 8) several(v0, std::integral_constant<int, 8>{});
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (v0 + i >= segments) continue;
+                    float sum = 0.f, sum_q = 0.f;
+#pragma unroll
+                    for (int e = 0; e < kSide; ++e) {
+                        sum += left(has[i][e / 4][e % 4], has[i][2 + e / 4][e % 4]);
+                        sum_q += has[i][2 + e / 4][e % 4];
+                    }
+                    to(v0 + i, sum, sum_q);
+                }
             }
         };
         bool shows = q.more;
@@ -579,13 +578,19 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
         } else if (tried == 1) {
             part = first.p;
         } else if (shows) {
-            over_kept(beta * q.one_q / p.one, [&](int v, float left, float) {
-                const double sum = running_sum((double)left * p.one);
+            const double by = beta * q.one_q / p.one;
+            over_kept(by, [&](int v, float left, float) {
+                const double sum = running_sum((double)left);
                 if (lane == 63) s.sums[v][wave] = sum;
             });
             __syncthreads();
             if (lane < segments)
                 for (int i = 0; i < kNodeWaves; ++i) part += s.sums[lane][i];
+            const Left left(by);
+            return finish(-1, draw_from_segments(a, s, part, segments, [&](int t) {
+                const float* at = w + kept_at(0, segments, t / kSegment) + t % kSegment;
+                return (double)left(at[0], at[kSegment]);
+            }));
         } else {
             for (int v = 0; v < segments; ++v) {
                 double w = 0.0;
@@ -631,9 +636,9 @@ ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st)
         if ((s = check_launch())) return s;
         hipLaunchKernelGGL(k_sample_rest, dim3(segments, a.M), dim3(kRowThreads), 0, st, a, firsts, rest, kept);
         if ((s = check_launch())) return s;
-        hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
-                           a.V, a, (const First*)firsts,
-                           (const Rest*)rest, kept, segments, nodes, arrived);
+        hipLaunchKernelGGL(k_sample_nodes<true>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens,
+                           a.parent, a.u, (const Segment*)seg, a.M, a.V, a, (const First*)firsts, (const Rest*)rest, kept, segments, nodes,
+                           arrived);
     } else {
         hipLaunchKernelGGL(k_sample_nodes<false>, dim3(a.M), dim3(kNodeThreads), 0, st, a.logits, a.tokens, a.parent, a.u, (const Segment*)seg, a.M,
                            a.V, a, (const First*)nullptr,
