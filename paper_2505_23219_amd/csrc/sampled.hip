@@ -476,8 +476,8 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
             s.q[tid] = is ? q_of(x) : 0.0;
         }
         __syncthreads();
-        // Weights in 32 bits, 0 of what was rejected, are there if a second child is; what is left may be less than those show: then
-        // they are worked out anew each time.  In units of the target's weights what is left of a token is p - by q; `by` in two parts.
+        // Weights in 32 bits, 0 of what was rejected, are there if a second child is; where less is left than
+        // those show, they are worked out anew each time, in 64 bits' range.  In units of the target's weights what is left of a token is p - by q; `by` in two parts.
         float* const w = kept + kept_at(node, segments, 0);
         struct Left {
             float high, low;
@@ -533,34 +533,38 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                 all_q = wave_sum(first.q);
                 asm volatile("" : "+v"(all), "+v"(all_q));
             } else {
-                shows = shows && rest_q > 1e-25 && alpha < 1e25;
-                double sp = 0.0, sq = 0.0;
-                if (shows) {
-                    over_kept(next * q.one_q / p.one, [&](int, float left, float left_q) {
-                        sp += (double)left;
-                        sq += (double)left_q;
-                    });
-                    sp *= p.one;
-                    sq *= q.one_q;
-                } else {
-                    for (int t = tid; t < a.V; t += kNodeThreads) {
-                        if (s.rejected(t)) continue;
-                        const double qt = q_of(t);
-                        sp += fmax(p_of(t) - next * qt, 0.0);
-                        sq += qt;
+                for (;;) {
+                    double sp = 0.0, sq = 0.0;
+                    if (shows) {
+                        over_kept(next * q.one_q / p.one, [&](int, float left, float left_q) {
+                            sp += (double)left;
+                            sq += (double)left_q;
+                        });
+                        sp *= p.one;
+                        sq *= q.one_q;
+                    } else {
+                        for (int t = tid; t < a.V; t += kNodeThreads) {
+                            if (s.rejected(t)) continue;
+                            const double qt = q_of(t);
+                            sp += fmax(p_of(t) - next * qt, 0.0);
+                            sq += qt;
+                        }
                     }
-                }
-                sp = running_sum(sp);
-                sq = running_sum(sq);
-                if (lane == 63) {
-                    s.part[0][wave] = sp;
-                    s.part[1][wave] = sq;
-                }
-                __syncthreads();
-                all = all_q = 0.0;
-                for (int v = 0; v < kNodeWaves; ++v) {
-                    all += s.part[0][v];
-                    all_q += s.part[1][v];
+                    sp = running_sum(sp);
+                    sq = running_sum(sq);
+                    if (lane == 63) {
+                        s.part[0][wave] = sp;
+                        s.part[1][wave] = sq;
+                    }
+                    __syncthreads();
+                    all = all_q = 0.0;
+                    for (int v = 0; v < kNodeWaves; ++v) {
+                        all += s.part[0][v];
+                        all_q += s.part[1][v];
+                    }
+                    if (!shows || (all > 1e-25 && all_q > 1e-25)) break;
+                    shows = false;
+                    __syncthreads();
                 }
             }
             if (all > 0.0) {

@@ -168,6 +168,46 @@ def test_little_left():
         _check((case[0], tokens, parent, u, None, None))
 
 
+@pytest.mark.parametrize("V", [5, 4096, 4097, 8193, 32768, 33000, 70001, 262144])
+@pytest.mark.parametrize("children", [2, 3, 19])
+def test_many_rejections(V, children):
+    """A root whose children are all rejected, their tokens once and twice and outside of the vocabulary; any workspace.
+
+    The token follows from sums of p - b q of tokens not rejected.  A weight is off by 2^-24 of itself, b and the difference as much again, and
+    up to eight of them are added up in 32 bits (three roundings each, at most): the running sum by less than 12 2^-24 of the
+    running sum of p + b q."""
+    children = min(children, V - 2)
+    M, g = children + 1, torch.Generator().manual_seed(V + children)
+    for turn in range(3):
+        logits, q = 1.5 * torch.randn(M, V, generator=g), torch.randn(M, V, generator=g)
+        tokens = torch.zeros(M, dtype=torch.int32)
+        tokens[1:] = torch.randperm(V, generator=g)[:children].int()
+        if V > 4096:                             # one in the last segment, in the first, at both ends
+            tokens[1], tokens[2] = V - 1, 0
+        if turn == 1 and children > 4:
+            tokens[3], tokens[4] = tokens[1], V
+        u = torch.full((M,), 0.99)
+        u[0] = (0.11, 0.77, 0.0)[turn]
+        at = tokens[1:].long().clamp(max=V - 1)
+        logits[0, at], q[0, at] = -30.0, q[0, at] + 4.0
+        p, qp = torch.softmax(logits[0].double(), 0), torch.softmax(q[0].double(), 0)
+        size, beta, alpha, gone = p.clone(), 0.0, 1.0, torch.zeros(V, dtype=torch.bool)
+        left, rest = p.clone(), 1.0
+        for x in tokens[1:].tolist():
+            if x >= V:
+                continue
+            beta += 1.0 / (alpha * rest)
+            gone[x] = True
+            left, size = (p - beta * qp).clamp(min=0).masked_fill(gone, 0), (p + beta * qp).masked_fill(gone, 0)
+            alpha, rest = 1.0 / left.sum().item(), qp.masked_fill(gone, 0).sum().item()
+        ws = torch.full((B.ghd_accept_sampled_workspace_bytes(M, V),), 255, dtype=torch.uint8, device="cuda")
+        got = _gpu((logits, tokens, [-1] + [0] * children, u, q, None), ws=ws)
+        assert got[0] == 1 and 0 <= got[1] < V and not gone[got[1]]
+        upto, off = left.cumsum(0), 12 * 2.0 ** -24 * size.cumsum(0)
+        goal, t = u[0].double() * left.sum(), got[1]
+        assert upto[t] + off[-1] >= goal and upto[t] - left[t] - off[-1] <= goal and left[t] > -off[-1], (t, goal, upto[t], left[t])
+
+
 def test_rows_of_drafts_are_clamped_and_a_parent_is_an_earlier_node():
     case = _case(10, 200, "random", "depths", 4)
     row = [r + 100 if i % 2 else r - 100 for i, r in enumerate(case[5])]
