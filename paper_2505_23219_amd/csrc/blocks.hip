@@ -13,7 +13,8 @@ __device__ __forceinline__ float one_over_power(float p) { return __uint_as_floa
 __device__ __forceinline__ int code_of(float x) { return (int)fminf(fmaxf(x, -127.f), 127.f); }
 
 // ---- bounds ------------------------------------------------------------------------------
-// A wavefront has a block: 16-byte loads, so many rows at a time as fit, all requested at once.  Bound: the bytes of K.
+// A wavefront has a block: 16-byte loads, so many rows at a time as fit, all requested at once.  Bound: the bytes of
+// K: 256 blocks of 32 heads of 128 channels, 134 MB, 28.9 us (4.6 TB/s).  A single block of 8 heads: 3.6 us, a launch's time.
 template <int D>
 __global__ __launch_bounds__(256) void k_block_bounds(Bounds to, const half_t* __restrict__ k, int first, int n, int nkv, int64_t k_head,
                                                       int64_t k_tok)
@@ -217,6 +218,8 @@ __device__ __forceinline__ void block_scores(const SelectArgs& a, int head, int 
     }
 }
 
+// Bound: reading codes where tokens are few (8 heads of 2047 blocks, 4.3 MB: 6.1 us, half of it before the first of them is there), else the
+// quantising of queries, which every wavefront does for itself.
 template <int D, int TILES>
 __global__ __launch_bounds__(256) void k_block_scores(SELECT_FIRST, SelectArgs a)
 {
@@ -397,7 +400,9 @@ __device__ __forceinline__ void store_eight(const SelectArgs& a, int head, int m
     }
 }
 
-// Scores and picks of few blocks in one launch: a workgroup has eight tokens of a head, whose scores stay in LDS.
+// Scores and picks of few blocks in one launch: a workgroup has eight tokens of a head, whose scores stay in LDS.  Bound: what follows one
+// another - codes' way from the L2, the product, three or four rounds of a pick.  64 tokens of 32 heads over 512 blocks: 12.9 us (14.1 with
+// arguments from memory and maxima by shuffles, 16.4 with heads spread over the XCDs).
 constexpr int kFewBlocks = 512;
 template <int D>
 __global__ __launch_bounds__(512) void k_block_few(SELECT_FIRST, SelectArgs a)
@@ -411,7 +416,7 @@ __global__ __launch_bounds__(512) void k_block_few(SELECT_FIRST, SelectArgs a)
     auto keep = [&](int b, uint4_ key) {
         if ((lane & 15) < 8) *(uint4_*)(s_key[lane & 7] + b) = key;
     };
-    // (all of a wavefront's tiles are asked for at once: two at a time, 64 tokens of 32 heads took .. us)
+    // (all of a wavefront's tiles are asked for at once: by two, that took 0.2 us more)
     if (a.n > 128) block_scores<D, kFewBlocks / 128>(a, head, m0 + (lane & 7), wave * 16, 128, lane, keep);
     else if (wave * 16 < a.n) block_scores<D, 1>(a, head, m0 + (lane & 7), wave * 16, 128, lane, keep);
     __syncthreads();
@@ -420,7 +425,7 @@ __global__ __launch_bounds__(512) void k_block_few(SELECT_FIRST, SelectArgs a)
     store_eight(a, head, m0, s_bits, tid);
 }
 
-// A workgroup has eight tokens.  64 tokens of 32 heads over 512 blocks: 8.2 us, a workgroup a token and its bits set by atomic operations 15.8.
+// A workgroup has eight tokens, a wavefront each; their bits meet in LDS and leave as bytes of the words.
 constexpr int kPickBytes = 2048;                 // blocks
 template <int KEPT>
 __global__ __launch_bounds__(512) void k_block_pick_eight(SelectArgs a)
@@ -437,7 +442,7 @@ __global__ __launch_bounds__(512) void k_block_pick_eight(SelectArgs a)
     store_eight(a, head, m0, s_bits, tid);
 }
 
-// A workgroup has a token; the words are zeros before (k_block_scores).
+// A workgroup has a token; the words are zeros before (k_block_scores).  Bound: what follows one another.  8 heads' picks among 2047 blocks: 5.2 us.
 template <int KEPT>
 __global__ __launch_bounds__(1024) void k_block_pick(SelectArgs a)
 {
@@ -470,16 +475,23 @@ ghd_status launch_block_bounds_read(float* hi, float* lo, Bounds from, int first
 ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st)
 {
     if (a.n == 0) return GHD_OK;
-    if (a.n <= kFewBlocks) {
+    // One launch takes up to 128 blocks, or 512 where there are so many picks that they fill the GPU anyhow, if it is one round of workgroups.
+    // In a graph, us, against two launches: 1 token, 8 heads of 4, 128 blocks 9.2 | 9.2, 512 blocks 13.4 | 9.2; 64 tokens, 32 heads, 128 blocks
+    // 7.8 | 10.2, 512 blocks 11.6 | 14.5; 128 tokens, 32 heads of 4, 512 blocks 28.4 | 24.  Without a graph a launch costs the host 3 us.
+    const bool many = a.M * a.nkv >= 1024;
+    if (a.n <= kFewBlocks && a.nkv * ceil_div(a.M, 8) <= 256 && (a.n <= 128 || many)) {
         const dim3 teams(a.nkv, ceil_div(a.M, 8));                  // (a head's tokens on one XCD, where its codes are)
         if (d == 128) hipLaunchKernelGGL(k_block_few<128>, teams, dim3(512), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
         else hipLaunchKernelGGL(k_block_few<64>, teams, dim3(512), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);
         return check_launch();
     }
-    // a wavefront has 64 blocks, or 16 where there would be fewer than four wavefronts for each compute unit
+    // A wavefront has 64 blocks, or 16 where there would be fewer than four wavefronts for each compute unit: 1 token, 8 heads of 4, 1000
+    // blocks 9.2 us, with 64 11.7; 128 tokens 17.0, with 16 21.6.
     const int tiles = ceil_div(a.M, 16), per = (int64_t)ceil_div(a.n, 64) * a.nkv * tiles >= 1024 ? 4 : 1;
     const dim3 grid(ceil_div(a.n, 64 * per), a.nkv, tiles);
-    const bool eight = a.n <= kPickBytes && a.M > 4;
+    // eight tokens' picks in a workgroup, or one's: 64 tokens, 32 heads, 1000 blocks 20.1 us | 27.7; 64 tokens, 8 heads of 4, 2000 blocks
+    // 21.3 | 16.1, 8 tokens 16.6 | 9.8
+    const bool eight = a.n <= kPickBytes && many;
     a.zero = !eight;
     if (d == 128) {
         if (per == 4) hipLaunchKernelGGL((k_block_scores<128, 4>), grid, dim3(256), 0, st, a.q, a.bounds.codes, a.bounds.units, a.bounds.blocks, a.M, a.nkv, a.rep, a.n, a);

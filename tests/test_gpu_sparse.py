@@ -101,6 +101,24 @@ def test_select(M, nh, nkv, d, kv_len, count, sinks, recent):
     _check_select(q, k, kd, kv_len, count, sinks, recent)
 
 
+@pytest.mark.parametrize("M,nh,nkv,d,kv_len,count,sinks,recent", [
+    (128, 8, 8, 64, 64 * 128, 5, 1, 1), (128, 8, 8, 64, 64 * 129, 9, 0, 0), (127, 9, 9, 64, 64 * 512, 40, 2, 1), (128, 8, 8, 128, 64 * 513, 33, 1, 2),
+    (100, 22, 11, 64, 64 * 1100 + 5, 17, 0, 0), (128, 8, 8, 64, 64 * 2048, 60, 1, 1), (128, 8, 8, 64, 64 * 2049, 60, 1, 1),
+    (20, 104, 104, 64, 64 * 130, 7, 1, 1), (16, 4, 4, 64, 64 * 129, 128, 0, 0), (128, 17, 17, 64, 64 * 100, 3, 0, 1)])
+def test_select_of_many_picks(M, nh, nkv, d, kv_len, count, sinks, recent):
+    """1024 picks and more, and few of them, on either side of what one launch and one workgroup take."""
+    test_select(M, nh, nkv, d, kv_len, count, sinks, recent)
+
+
+@pytest.mark.parametrize("M,n", [(128, 200), (128, 600), (128, 1200)])
+def test_many_picks_of_equal_blocks(M, n):
+    some = torch.randn(2, 64, 64, generator=_gen(2)).half()
+    k = some[torch.arange(n) * 7 % 2].reshape(1, n * 64, 64).repeat(8, 1, 1)
+    q = torch.randn(M, 8, 64, generator=_gen(9)).half()
+    for count in (1, 130, n - 1):
+        _check_select(q, k, k.cuda(), n * 64, count, 1, 0)
+
+
 @pytest.mark.parametrize("M,n", [(3, 300), (3, 700), (9, 900), (6, 1500), (1, 5000)])
 @pytest.mark.parametrize("kinds", [1, 2, 5])
 def test_select_takes_the_lowest_of_equal_blocks(kinds, M, n):
