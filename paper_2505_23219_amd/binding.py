@@ -739,12 +739,13 @@ def _here(name: str, t: torch.Tensor, dtype, shape, dev: int) -> int:
     return t.data_ptr()
 
 
-def _cache_at(name: str, t: torch.Tensor, heads: int, rows: int, cols: int, dev: int) -> int:
-    """Where a cache [heads, >= rows, >= cols] (any strides, the last axis side by side) on GPU `dev` lies."""
-    if (dev < 0 or t.get_device() != dev or t.dtype is not torch.float16 or t.dim() != 3 or t.stride(2) != 1 or t.shape[0] != heads
-            or t.shape[1] < rows or t.shape[2] < cols):
-        raise _misfit(name, t, "float16 on the GPU, at least (%d, %d, %d), its last axis side by side" % (heads, rows, cols))
-    return t.data_ptr()
+def _cache_at(name: str, t: torch.Tensor, heads: int, rows: int, cols: int, dev: int) -> tuple:
+    """Where a cache [heads, >= rows, >= cols] (any strides, the last axis side by side) on GPU `dev` lies, and its two strides."""
+    if dev >= 0 and t.get_device() == dev and t.dtype is torch.float16 and t.dim() == 3:
+        (n, r, c), (head, row, one) = t.shape, t.stride()
+        if one == 1 and n == heads and r >= rows and c >= cols:
+            return t.data_ptr(), head, row
+    raise _misfit(name, t, "float16 on the GPU, at least (%d, %d, %d), its last axis side by side" % (heads, rows, cols))
 
 
 def _stream_of(dev: int) -> int:
@@ -771,8 +772,7 @@ class BlockBounds:
 def ghd_block_bounds(bounds: BlockBounds, k_cache: torch.Tensor, block0: int, blocks: int) -> None:
     """Bounds of blocks block0 .. block0 + blocks - 1 from k_cache fp16 [nkv, rows, d]."""
     nkv, d, dev = bounds.nkv, bounds.d, k_cache.get_device()
-    k = _cache_at("k_cache", k_cache, nkv, (block0 + blocks) * GHD_BLOCK, d, dev)
-    head, tok, _ = k_cache.stride()
+    k, head, tok = _cache_at("k_cache", k_cache, nkv, (block0 + blocks) * GHD_BLOCK, d, dev)
     st = (_lib or lib()).ghd_block_bounds(_here("bounds", bounds.data, torch.uint8, None, dev), k, block0, blocks, nkv, d, bounds.capacity,
                                           head, tok, _stream_of(dev))
     if st:
@@ -784,14 +784,16 @@ def ghd_block_bounds_read(bounds: BlockBounds, block0: int, blocks: int, hi: Opt
     """What the bounds stand for: float [nkv, blocks, d], largest and smallest key of each channel."""
     shape, dev = (bounds.nkv, blocks, bounds.d), bounds.data.get_device()
     data = _here("bounds", bounds.data, torch.uint8, None, dev)
-    if hi is None and lo is None:
-        hi, lo = torch.empty((2,) + shape, dtype=torch.float32, device=bounds.data.device).unbind(0)
-    elif hi is None:
-        hi = torch.empty_like(lo)
-    elif lo is None:
-        lo = torch.empty_like(hi)
-    st = (_lib or lib()).ghd_block_bounds_read(_here("hi", hi, torch.float32, shape, dev), _here("lo", lo, torch.float32, shape, dev), data,
-                                               block0, blocks, bounds.nkv, bounds.d, bounds.capacity, _stream_of(dev))
+    if hi is None and lo is None:                # (the two are known to fit: no checks)
+        both = torch.empty((2,) + shape, dtype=torch.float32, device=bounds.data.device)
+        hi_ptr = both.data_ptr()
+        lo_ptr = hi_ptr + 4 * bounds.nkv * blocks * bounds.d
+        hi, lo = both.unbind(0)
+    else:
+        hi = torch.empty_like(lo) if hi is None else hi
+        lo = torch.empty_like(hi) if lo is None else lo
+        hi_ptr, lo_ptr = _here("hi", hi, torch.float32, shape, dev), _here("lo", lo, torch.float32, shape, dev)
+    st = (_lib or lib()).ghd_block_bounds_read(hi_ptr, lo_ptr, data, block0, blocks, bounds.nkv, bounds.d, bounds.capacity, _stream_of(dev))
     if st:
         _check(st, "ghd_block_bounds_read")
     return hi, lo
@@ -838,9 +840,8 @@ def ghd_sparse_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     if (parent is None) == (mask is None):
         raise ValueError("either parent or mask says which drafted tokens a token sees")
     q_ptr = _here("q", q, torch.float16, None, dev)
-    k, v = _cache_at("k_cache", k_cache, nkv, rows, d, dev), _cache_at("v_cache", v_cache, nkv, d, rows, dev)
-    k_head, k_tok, _ = k_cache.stride()
-    v_head, v_ch, _ = v_cache.stride()
+    k, k_head, k_tok = _cache_at("k_cache", k_cache, nkv, rows, d, dev)
+    v, v_head, v_ch = _cache_at("v_cache", v_cache, nkv, d, rows, dev)
     if out is None:
         out = torch.empty_like(q)
     if ws is None:
