@@ -517,8 +517,8 @@ ghd_status ghd_block_bounds_read(float *hi, float *lo, const void *bounds, int b
  *            the block (NULL is fine where there is no whole block)
  * A block's score for a token and a key head is the largest over the head's query heads of
  * s' s sum_c (max(Q_c, 0) HI_c + min(Q_c, 0) LO_c), where Q = rint(q / s') is the query held like a
- * key: up to the rounding of q the highest score that a key of the block can have.  It is exact in 32 bits: equal inputs
- * have equal selections.  A block that holds an infinity or NaN scores infinity; a query head that
+ * key: up to the rounding of q and the codes' end at 127 the highest score that a key of the block can have.  It is
+ * exact in 32 bits: equal inputs have equal selections.  A block that holds an infinity or NaN scores infinity; a query head that
  * does scores 0. */
 ghd_status ghd_block_select(uint64_t *sel_dev, const void *q, const void *bounds, int M, int kv_len, int nh,
                             int nkv, int d, int capacity, int count, int sinks, int recent, void *ws,

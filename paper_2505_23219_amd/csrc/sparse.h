@@ -1,7 +1,8 @@
 // Attention over blocks of the committed cache that each drafted token selects: layouts and launches.
 //
 // A block is 64 committed rows.  Its bounds: for every channel the largest and the smallest key as whole numbers HI and LO,
-// within -127 .. 127, of a unit that is a power of two; HI rounded up and LO down, so q.k <= sum_c (q > 0 ? q HI : q LO) unit.
+// within -127 .. 127, of a unit that is a power of two; HI rounded up and LO down, so q.k <= sum_c (q > 0 ? q HI : q LO) unit, but
+// for what ends at 127.
 // Scores are whole numbers times powers of two, exact in 32 bits: the order of the blocks does not depend on how they are summed.
 #pragma once
 #include "common.h"
