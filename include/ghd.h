@@ -528,7 +528,7 @@ size_t ghd_block_select_workspace_bytes(int M, int kv_len, int nkv);
 /* ghd_tree_attention (parent_dev) or ghd_masked_attention (mask_dev; exactly one of the two) over what each
  * token reads: rows of whole blocks by sel_dev - from ghd_block_select, or any other - , rows from
  * 64 (kv_len / 64) on, and drafted rows.  q, out fp16 [M, nh, d]; out may be q, and meets nothing else that the call
- * reads.  A token that sees no key gives zeros.  An infinity or NaN in a row reaches the tokens that
+ * reads.  |scale| <= 1e20.  A token that sees no key gives zeros.  An infinity or NaN in a row reaches the tokens that
  * see the row and no others (a call over such rows is many times slower).  Statistics and sums are 32
  * bits, probabilities are rounded to fp16.  The workspace's size falls neither with M nor with kv_len. */
 ghd_status ghd_sparse_attention(void *out, const void *q, const void *k_cache, const void *v_cache,

@@ -133,7 +133,7 @@ ghd_status ghd_sparse_attention(void* out, const void* q, const void* k_cache, c
 {
     const int n = kv_len / kBlock;
     if (!out || !q || !k_cache || !v_cache || (!sel_dev && n > 0) || (!parent_dev && !mask_dev)) return GHD_ERR_NULL;
-    if (!rows_ok(M, kv_len) || !heads_ok(nh, nkv, d) || (parent_dev && mask_dev) || !isfinite(scale)) return GHD_ERR_SHAPE;
+    if (!rows_ok(M, kv_len) || !heads_ok(nh, nkv, d) || (parent_dev && mask_dev) || !(fabsf(scale) <= 1e20f)) return GHD_ERR_SHAPE;
     // (a block's rows and a head's channels are read at 32-bit offsets)
     if (k_stride_tok < d || k_stride_head < 0 || v_stride_head < 0 || k_stride_tok > (1 << 24) || v_stride_ch > (1 << 22)) return GHD_ERR_SHAPE;
     const int64_t rows = (int64_t)kv_len + M;

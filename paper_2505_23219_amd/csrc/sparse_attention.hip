@@ -213,13 +213,16 @@ struct SparseState {
             for (int ct = 0; ct < D / 16; ++ct) o[ct] *= r;
             m = now;
         }
-        const float off = m == -INFINITY ? 0.f : -m;
+        // (products are rounded as the maximum was, so none passes it by more than 8: with one rounding for both, scores of 2^28 and more
+        // would be off from their maximum by so much that a power overflows)
+        const float off = m == -INFINITY ? 0.f : m;
         half2_ p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+#pragma clang fp contract(off)
             floatx2 x;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) x[u] = fast_exp2(fmaf(s[e >> 1][2 * (e & 1) + u], c, off));
+            for (int u = 0; u < 2; ++u) x[u] = fast_exp2(s[e >> 1][2 * (e & 1) + u] * c - off);
             p[e] = __builtin_convertvector(x, half2_);
         }
         const half8 all = {p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};

@@ -244,6 +244,25 @@ def test_scales(scale):
     _check(6, 4, 2, 64, 400, _selection(2, 6, 6, 3, 1), "random", scale=scale)
 
 
+@pytest.mark.parametrize("M,rep,d,kv_len", [(1, 1, 64, 700), (7, 4, 128, 700), (40, 1, 64, 1500), (100, 1, 128, 300), (128, 2, 64, 300)])
+@pytest.mark.parametrize("scale", [None, -3.0, 1e9])
+def test_the_largest_scores(M, rep, d, kv_len, scale):
+    """Queries and keys of 60000 with any signs: scores differ by 2^30 and more, so a row has the value of its best key, bit for bit."""
+    nkv, g = 2, _gen(M + d)
+    sign = lambda *n: (torch.randint(2, n, generator=g) * 2 - 1).half()
+    rows, n = -(-(kv_len + M) // 8) * 8, kv_len // 64
+    k, v = 60000 * sign(nkv, rows, d), torch.randn(nkv, d, rows, generator=g).half()
+    q = 60000 * sign(M, nkv * rep, d)
+    at = torch.randperm(kv_len, generator=g)[:M * rep].view(M, rep)
+    for h in range(nkv):                         # the key of a row's own signs, or of the opposite ones
+        k[h, at.view(-1)] = (q[:, h * rep:(h + 1) * rep].reshape(M * rep, d) * (-1 if scale is not None and scale < 0 else 1))
+    sel = torch.full((nkv, -(-M // 64), n), -1, dtype=torch.int64, device="cuda")
+    rel, _ = _relation("none", M, 1)
+    got = B.ghd_sparse_attention(q.cuda(), k.cuda(), v.cuda(), sel, kv_len, scale=scale, **rel).cpu()
+    for h in range(nkv):
+        assert torch.equal(got[:, h * rep:(h + 1) * rep], v[h][:, at].permute(1, 2, 0))
+
+
 def test_all_blocks_are_all_of_the_attention():
     for M, kv_len in ((1, 700), (24, 1000), (128, 200)):
         nh, d = 8, 128

@@ -73,7 +73,7 @@ nan, inf = float("nan"), float("inf")
     (_attend, NULL, dict(out=None)), (_attend, NULL, dict(q=None)), (_attend, NULL, dict(k=None)), (_attend, NULL, dict(v=None)),
     (_attend, NULL, dict(sel=None)), (_attend, NULL, dict(parent=None)), (_attend, SHAPE, dict(mask=FAR[9])), (_attend, SHAPE, dict(M=0)),
     (_attend, SHAPE, dict(M=129)), (_attend, SHAPE, dict(kv_len=(1 << 21) + 1)), (_attend, SHAPE, dict(kv_len=-64)),
-    (_attend, SHAPE, dict(nkv=3)), (_attend, SHAPE, dict(d=80)), (_attend, SHAPE, dict(scale=nan)), (_attend, SHAPE, dict(scale=inf)),
+    (_attend, SHAPE, dict(nkv=3)), (_attend, SHAPE, dict(d=80)), (_attend, SHAPE, dict(scale=nan)), (_attend, SHAPE, dict(scale=inf)), (_attend, SHAPE, dict(scale=-1.1e20)),
     (_attend, SHAPE, dict(kt=56)), (_attend, SHAPE, dict(vh=-8)), (_attend, CAPACITY, dict(vc=640)), (_attend, ALIGN, dict(vc=645)),
     (_attend, ALIGN, dict(kt=68)), (_attend, ALIGN, dict(out=FAR[0] + 8)), (_attend, ALIGN, dict(parent=FAR[7] + 2)),
     (_attend, ALIGN, dict(sel=FAR[6] + 4)), (_attend, ALIGN, dict(mask=FAR[9] + 4, parent=None)), (_attend, WORKSPACE, dict(ws=None)),
