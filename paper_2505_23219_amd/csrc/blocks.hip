@@ -304,7 +304,7 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
         }
     }
     uint32_t need = a.keep, in;                  // of the keys from low to high, of which there are `in`
-    int shift = max(0, 24 - (int)__builtin_clz((high - low) | 1));
+    int shift = pick_shift(low, high);
     for (;;) {
         each([&](uint32_t key, int) {
             if (key >= low && key <= high) atomicAdd(&s.hist[(key - low) >> shift], 1u);
@@ -327,7 +327,7 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
             }
         }
         team_sync<TEAM>();
-        const uint32_t from = low + (s.step << shift), to = from + ((1u << shift) - 1);
+        const uint32_t from = low + (s.step << shift), to = pick_step_end(from, high, shift);
         each([&](uint32_t key, int b) {
             if (key > to && key <= high) take(b);
         });

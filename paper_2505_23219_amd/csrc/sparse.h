@@ -39,6 +39,18 @@ struct SelectArgs {
     bool zero;                       // (the launch's) the words have to be zeros when the picks begin
     int lo, hi, keep;                // blocks [0, lo) and [hi, n) are taken, and `keep` of those between
 };
+// A pick cuts the keys from low to high into at most 256 steps of 2^shift keys.
+__host__ __device__ static inline int pick_shift(uint32_t low, uint32_t high)
+{
+    const int bits = 32 - __builtin_clz((high - low) | 1);
+    return bits > 8 ? bits - 8 : 0;
+}
+// The last key of the step that begins at `from`: the highest step ends at `high`.  (Where infinite scores meet ones below zero a step is 2^24
+// keys, and the highest may reach beyond 32 bits.)
+__host__ __device__ static inline uint32_t pick_step_end(uint32_t from, uint32_t high, int shift)
+{
+    return (high - from) >> shift ? from + ((1u << shift) - 1) : high;
+}
 static inline size_t select_bytes(int M, int n, int nkv) { return align_up((size_t)nkv * M * ((n + 3) & ~3) * 4, 256) + 256; }
 ghd_status launch_block_select(SelectArgs a, int d, hipStream_t st);
 

@@ -230,4 +230,8 @@ void ghd_debug_sparse_attention(int M, int kv_len, int nh, int nkv, int d, int64
 /* Halves of blocks that a list of `count` blocks, the last of them `last_block`, gives the wavefronts. */
 int ghd_debug_sparse_halves(int count, int last_block, int total) { return sparse_halves(count, last_block, total); }
 
+/* How a pick cuts a range of keys, and the last key of a step of it. */
+int ghd_debug_pick_shift(uint32_t low, uint32_t high) { return pick_shift(low, high); }
+uint32_t ghd_debug_pick_step_end(uint32_t from, uint32_t high, int shift) { return pick_step_end(from, high, shift); }
+
 }  // extern "C"
