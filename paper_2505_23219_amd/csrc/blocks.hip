@@ -347,13 +347,16 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, PickShared<TEAM
         return;
     }
     if (in <= S::kRanked) {
+        // (as many as were counted, unless another call writes to this workspace meanwhile: then nothing is taken that is no block)
         each([&](uint32_t key, int b) {
             if (key < low || key > high) return;
             const uint32_t to = atomicAdd(&s.n, 1u);
+            if (to >= S::kRanked) return;
             s.key[to] = key;
             s.at[to] = b;
         });
         team_sync<TEAM>();
+        in = min(in, s.n);
         if (tid >= (int)in) return;
         const uint32_t key = s.key[tid];
         const int at = s.at[tid];

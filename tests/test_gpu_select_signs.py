@@ -52,3 +52,19 @@ def test_scores_below_zero(M, nh, nkv, d, n, count, sinks, recent):
 def test_scores_of_both_signs(M, nh, nkv, d, n, count):
     """Picks that go down to the scores below zero."""
     _check(M, nh, nkv, d, n, count, 0, 0, mixed=True)
+
+
+@pytest.mark.parametrize("M,nkv,n", [(3, 2, 100), (128, 8, 300), (2, 1, 700), (1, 1, 4300), (128, 8, 700)])
+def test_bounds_that_were_never_given(M, nkv, n):
+    """Blocks whose bounds hold anything: which of them a token reads says nothing, but it reads `count` blocks."""
+    g, d = T._gen(n), 64
+    bounds = B.BlockBounds(nkv, d, n * 64)
+    bounds.data.copy_(torch.randint(0, 256, (bounds.data.numel(),), dtype=torch.uint8, generator=g))
+    units = bounds.data[nkv * n * 2 * d:].view(torch.int32)
+    odd = torch.tensor([0xff800000, 0xffffffff, 0x7fffffff, 0x7f800000, 0xff7fffff, 0x80000000]).int()
+    units[::3] = odd[torch.randint(0, 6, (len(units[::3]),), generator=g)].cuda()
+    q = torch.randn(M, nkv, d, generator=g).half().cuda()
+    for count in (1, 2, 20, n - 1):
+        sel = B.ghd_block_select(q, bounds, n * 64, count, sinks=1, recent=0).cpu()
+        bits = torch.stack([sel[:, i // 64] >> (i % 64) & 1 for i in range(M)])
+        assert (bits.sum(2) == count).all() and (bits[:, :, 0] == 1).all()
