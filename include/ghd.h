@@ -559,7 +559,9 @@ ghd_status ghd_accept_sampled(const float *logits, const int32_t *tokens_dev, co
                               const float *u_dev, const float *q_logits, const int32_t *q_row_dev, int q_rows,
                               int M, int V, float temperature, float q_temperature, int32_t *res_dev, void *ws,
                               size_t ws_bytes, void *stream);
+/* The second: for calls without q_logits, which keep no weights for rejections: 400 KB at the most. */
 size_t ghd_accept_sampled_workspace_bytes(int M, int V);
+size_t ghd_accept_sampled_undrawn_workspace_bytes(int M, int V);
 
 #ifdef __cplusplus
 }

@@ -124,6 +124,7 @@ def lib() -> C.CDLL:
             "ghd_sparse_attention_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
             "ghd_accept_sampled": (C.c_int32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp, sz, vp]),
             "ghd_accept_sampled_workspace_bytes": (sz, [i32, i32]),
+            "ghd_accept_sampled_undrawn_workspace_bytes": (sz, [i32, i32]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -148,7 +149,7 @@ EXPORTS = ["ghd_status_str", "ghd_last_hip_error", "ghd_tree_validate", "ghd_tre
            "ghd_attention_q4_workspace_bytes", "ghd_commit_path_q4", "ghd_kv_read_q4",
            "ghd_block_bounds_bytes", "ghd_block_bounds", "ghd_block_bounds_read", "ghd_block_select",
            "ghd_block_select_workspace_bytes", "ghd_sparse_attention", "ghd_sparse_attention_workspace_bytes",
-           "ghd_accept_sampled", "ghd_accept_sampled_workspace_bytes"]
+           "ghd_accept_sampled", "ghd_accept_sampled_workspace_bytes", "ghd_accept_sampled_undrawn_workspace_bytes"]
 
 
 def status_str(status: int) -> str:
@@ -862,6 +863,11 @@ def ghd_accept_sampled_workspace_bytes(M: int, V: int) -> int:
     return lib().ghd_accept_sampled_workspace_bytes(M, V)
 
 
+def ghd_accept_sampled_undrawn_workspace_bytes(M: int, V: int) -> int:
+    """For calls without q_logits."""
+    return lib().ghd_accept_sampled_undrawn_workspace_bytes(M, V)
+
+
 def ghd_accept_sampled(logits: torch.Tensor, tokens: torch.Tensor, parent: torch.Tensor, u: torch.Tensor, temperature: float = 1.0,
                        q_logits: Optional[torch.Tensor] = None, q_row: Optional[torch.Tensor] = None,
                        q_temperature: Optional[float] = None, res: Optional[torch.Tensor] = None,
@@ -874,7 +880,8 @@ def ghd_accept_sampled(logits: torch.Tensor, tokens: torch.Tensor, parent: torch
     if res is None:
         res = torch.zeros(2 + M, dtype=torch.int32, device=logits.device)
     if ws is None:
-        ws = workspace(L.ghd_accept_sampled_workspace_bytes(M, V), logits.device)
+        need = L.ghd_accept_sampled_undrawn_workspace_bytes if q_logits is None else L.ghd_accept_sampled_workspace_bytes
+        ws = workspace(need(M, V), logits.device)
     dev, q_rows = logits.get_device(), 0 if q_logits is None else q_logits.shape[0]
     st = L.ghd_accept_sampled(_here("logits", logits, torch.float32, None, dev), _here("tokens", tokens, torch.int32, (M,), dev),
                               _here("parent", parent, torch.int32, (M,), dev), _here("u", u, torch.float32, (M,), dev),

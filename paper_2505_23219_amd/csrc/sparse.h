@@ -82,7 +82,7 @@ struct SampleArgs {
     int M, V, q_rows;
     float temperature, q_temperature;
 };
-size_t accept_sampled_bytes(int M, int V);
+size_t accept_sampled_bytes(int M, int V, bool drafts);   // drafts: they have probabilities
 ghd_status launch_accept_sampled(const SampleArgs& a, void* ws, hipStream_t st);
 
 }  // namespace ghd

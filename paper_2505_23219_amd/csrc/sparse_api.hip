@@ -179,7 +179,12 @@ ghd_status ghd_sparse_attention(void* out, const void* q, const void* k_cache, c
 
 size_t ghd_accept_sampled_workspace_bytes(int M, int V)
 {
-    return M < 1 || M > GHD_MAX_M || V < 1 || V > 262144 ? 0 : accept_sampled_bytes(M, V);
+    return M < 1 || M > GHD_MAX_M || V < 1 || V > 262144 ? 0 : accept_sampled_bytes(M, V, true);
+}
+
+size_t ghd_accept_sampled_undrawn_workspace_bytes(int M, int V)
+{
+    return M < 1 || M > GHD_MAX_M || V < 1 || V > 262144 ? 0 : accept_sampled_bytes(M, V, false);
 }
 
 ghd_status ghd_accept_sampled(const float* logits, const int32_t* tokens_dev, const int32_t* parent_dev, const float* u_dev,
@@ -197,10 +202,10 @@ ghd_status ghd_accept_sampled(const float* logits, const int32_t* tokens_dev, co
     if (!at_word(logits, 4) || !at_word(q_logits, 4) || !at_word(tokens_dev, 4) || !at_word(parent_dev, 4) || !at_word(u_dev, 4) ||
         !at_word(q_row_dev, 4) || !at_word(res_dev, 4))
         return GHD_ERR_ALIGN;
-    if (!ws || ws_bytes < accept_sampled_bytes(M, V)) return GHD_ERR_WORKSPACE;
+    const size_t used = accept_sampled_bytes(M, V, q_logits != nullptr), row = (size_t)V * 4, ints = (size_t)M * 4;
+    if (!ws || ws_bytes < used) return GHD_ERR_WORKSPACE;
     if (!at16(ws)) return GHD_ERR_ALIGN;
     // (the result is written when all else has been read: it may lie where an input is)
-    const size_t used = accept_sampled_bytes(M, V), row = (size_t)V * 4, ints = (size_t)M * 4;
     if (meet(ws, used, res_dev, ints + 8) || meet(ws, used, logits, M * row) || meet(ws, used, q_logits, q_rows * row) || meet(ws, used, tokens_dev, ints) ||
         meet(ws, used, parent_dev, ints) || meet(ws, used, u_dev, ints) || meet(ws, used, q_row_dev, ints))
         return GHD_ERR_SHAPE;

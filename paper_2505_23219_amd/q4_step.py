@@ -119,7 +119,7 @@ def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: 
     tree = torch.tensor(parent, dtype=torch.int32, device=table.device)
     res = torch.empty(2 + M, dtype=torch.int32, device=table.device)
     amax = torch.empty(M, dtype=torch.int32, device=table.device)
-    room = B.workspace(B.ghd_accept_sampled_workspace_bytes(M, stack.shape.V), table.device) if temperature > 0 else None
+    room = B.workspace(B.ghd_accept_sampled_undrawn_workspace_bytes(M, stack.shape.V), table.device) if temperature > 0 else None
     written: List[int] = []
     kv_len = steps = 0
     root = first
