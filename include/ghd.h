@@ -554,7 +554,7 @@ size_t ghd_sparse_attention_workspace_bytes(int M, int kv_len, int nh, int nkv, 
  *            written when all has been read, and may lie where an input does
  * NaN and -infinity among logits have the probability 0; where a row holds infinity its infinities share all of it.  The next
  * token is -1 where no token has a probability.  Tokens outside of the vocabulary are rejected.
- * Weights are 24 bits, their arguments and sums 64.  V <= 262144, q_rows <= GHD_MAX_M. */
+ * Weights, and what rejections leave of each, are 24 bits, their arguments and sums 64.  V <= 262144, q_rows <= GHD_MAX_M. */
 ghd_status ghd_accept_sampled(const float *logits, const int32_t *tokens_dev, const int32_t *parent_dev,
                               const float *u_dev, const float *q_logits, const int32_t *q_row_dev, int q_rows,
                               int M, int V, float temperature, float q_temperature, int32_t *res_dev, void *ws,

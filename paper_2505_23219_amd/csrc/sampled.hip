@@ -6,7 +6,7 @@
 // few nodes that the walk can come to, and of those k_sample_rest sums up what a first rejection leaves, over the segments again,
 // and keeps the weights where there may be others.
 //
-// Weights exp((l - m) / T) have arguments in 64 bits and 24 bits themselves; sums are 64 bits.  So a sum over a row is off by some
+// Weights exp((l - m) / T) have arguments in 64 bits and 24 bits themselves, and so has what rejections leave of each; sums are 64 bits.  So a sum over a row is off by some
 // 2^-24 / sqrt(V) of its largest terms, by random roundings of single weights, and what 64 bits would accept or draw is
 // what is accepted or drawn but where a random number lies as close to a border: of 17500 calls over 32000 to 131072 tokens two drew
 // another token, a neighbour.
@@ -490,8 +490,9 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
             __device__ __forceinline__ Left(double by) : high((float)by), low((float)(by - (double)high)) {}
             __device__ __forceinline__ float operator()(float pw, float qw) const { return fmaxf(fmaf(-low, qw, fmaf(-high, qw, pw)), 0.f); }
         };
-        // to(v, left, left_q): a thread's share of segment v, two times four neighbours of either row; eight segments are asked for at a time
-        auto over_kept = [&](double by, auto to) {
+        // to(v, left, left_q): a thread's share of segment v, two times four neighbours of either row, q's if it is to be summed; eight segments are
+        // asked for at a time
+        auto over_kept = [&](double by, bool sum_q_too, auto to) {
             const Left left(by);
             for (int v0 = 0; v0 < segments; v0 += kAtOnce) {
                 floatx4 has[kAtOnce][4];
@@ -506,12 +507,12 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                     if (v0 + i >= segments) continue;
-                    float sum = 0.f, sum_q = 0.f;
+                    double sum = 0.0, sum_q = 0.0;
 #pragma unroll
-                    for (int e = 0; e < kSide; ++e) {
-                        sum += left(has[i][e / 4][e % 4], has[i][2 + e / 4][e % 4]);
-                        sum_q += has[i][2 + e / 4][e % 4];
-                    }
+                    for (int e = 0; e < kSide; ++e) sum += (double)left(has[i][e / 4][e % 4], has[i][2 + e / 4][e % 4]);
+                    if (sum_q_too)
+#pragma unroll
+                        for (int e = 0; e < kSide; ++e) sum_q += (double)has[i][2 + e / 4][e % 4];
                     to(v0 + i, sum, sum_q);
                 }
             }
@@ -539,12 +540,16 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                 all_q = wave_sum(first.q);
                 asm volatile("" : "+v"(all), "+v"(all_q));
             } else {
+                // What is left of q follows from what was: off by 2^-53 of the whole for each rejection, 2^-36 of a thousandth at the most.  Where less
+                // is left it is summed up.
+                const double without = rest_q - s.q[k];
+                const bool follows = without > 1e-3;
                 for (;;) {
                     double sp = 0.0, sq = 0.0;
                     if (shows) {
-                        over_kept(next * q.one_q / p.one, [&](int, float left, float left_q) {
-                            sp += (double)left;
-                            sq += (double)left_q;
+                        over_kept(next * q.one_q / p.one, !follows, [&](int, double left, double left_q) {
+                            sp += left;
+                            sq += left_q;
                         });
                         sp *= p.one;
                         sq *= q.one_q;
@@ -557,7 +562,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                         }
                     }
                     sp = running_sum(sp);
-                    sq = running_sum(sq);
+                    if (!follows) sq = running_sum(sq);
                     if (lane == 63) {
                         s.part[0][wave] = sp;
                         s.part[1][wave] = sq;
@@ -568,6 +573,7 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
                         all += s.part[0][v];
                         all_q += s.part[1][v];
                     }
+                    if (follows) all_q = without;
                     if (!shows || (all > 1e-25 && all_q > 1e-25)) break;
                     shows = false;
                     __syncthreads();
@@ -589,8 +595,8 @@ __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(cons
             part = first.p;
         } else if (shows) {
             const double by = beta * q.one_q / p.one;
-            over_kept(by, [&](int v, float left, float) {
-                const double sum = running_sum((double)left);
+            over_kept(by, false, [&](int v, double left, double) {
+                const double sum = running_sum(left);
                 if (lane == 63) s.sums[v][wave] = sum;
             });
             __syncthreads();
