@@ -114,7 +114,8 @@ def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: 
            generator: Optional[torch.Generator] = None) -> Tuple[List[int], int, float]:
     """At least `count` tokens behind `first`: (tokens, steps, seconds).  parent: the tree of every step;
     draft(written) -> the tokens of its nodes 1 .. M - 1 (none for a tree of one node).  Greedily, or, with a
-    temperature above 0, as sampled token by token from softmax(logits / temperature) with numbers of `generator`."""
+    temperature above 0, as sampled token by token from softmax(logits / temperature) with numbers of `generator`.  Raises
+    FloatingPointError where no token has a probability (logits that are no numbers)."""
     M = len(parent)
     tree = torch.tensor(parent, dtype=torch.int32, device=table.device)
     res = torch.empty(2 + M, dtype=torch.int32, device=table.device)
@@ -136,6 +137,8 @@ def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: 
         stack.commit(res, M, kv_len)
         r = res.tolist()
         taken, root = r[0], r[1]
+        if root < 0:
+            raise FloatingPointError("no token has a probability behind the %d that were written" % len(written))
         path = nodes[torch.tensor(r[2:2 + taken], device=table.device)].tolist()
         written += path[1:] + [root]
         kv_len += taken
