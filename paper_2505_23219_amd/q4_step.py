@@ -116,6 +116,8 @@ def decode(stack: Q4Stack, table: torch.Tensor, first: int, count: int, parent: 
     draft(written) -> the tokens of its nodes 1 .. M - 1 (none for a tree of one node).  Greedily, or, with a
     temperature above 0, as sampled token by token from softmax(logits / temperature) with numbers of `generator`.  Raises
     FloatingPointError where no token has a probability (logits that are no numbers)."""
+    if not 0 <= temperature < float("inf"):
+        raise ValueError("temperature has to be 0 (greedy) or above and finite, not %s" % temperature)
     M = len(parent)
     tree = torch.tensor(parent, dtype=torch.int32, device=table.device)
     res = torch.empty(2 + M, dtype=torch.int32, device=table.device)

@@ -1,4 +1,4 @@
-"""The 4-bit decoding loop ends where no token can be sampled (the library's calls replaced by plain ones)."""
+"""What the 4-bit decoding loop refuses, and that it ends where no token can be sampled (the library's calls replaced by plain ones)."""
 import math
 from types import SimpleNamespace
 
@@ -45,6 +45,12 @@ def test_a_token_that_cannot_be_drawn_ends_it(plain):
         q4_step.decode(_Stack(3), table, 1, 5, [-1], temperature=0.5)
     with pytest.raises(FloatingPointError, match="behind the 0"):
         q4_step.decode(_Stack(0), table, 1, 5, [-1], temperature=2.0)
+
+
+@pytest.mark.parametrize("temperature", [-1.0, -1e-30, math.nan, math.inf, -math.inf])
+def test_temperatures_that_are_none(plain, temperature):
+    with pytest.raises(ValueError, match="temperature"):
+        q4_step.decode(_Stack(99), torch.zeros(10, 4), 1, 5, [-1], temperature=temperature)
 
 
 def test_greedy_as_before(plain):
