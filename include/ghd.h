@@ -489,7 +489,9 @@ ghd_status ghd_kv_read_q4(void *k_out, void *v_out, const ghd_kv *kv_host, int L
  * drafted token read a part of it: bounds are kept of the keys of every block of 64
  * committed rows, a token's queries are scored against them, and the attention reads the
  * blocks that a token has selected, the committed rows behind the last whole block, and the drafted
- * rows that the token sees.  The cache is the one of ghd_tree_attention, with nkv key heads:
+ * rows that the token sees.  Queries come rotated, and the drafted rows' keys and values are in the cache: ghd_verify_layer and
+ * ghd_verify_stack do both for an attention of their own, so a step with these calls brings them itself.  The cache is
+ * the one of ghd_tree_attention, with nkv key heads:
  * nh % nkv == 0, query head h reads key head h / (nh / nkv).  nh <= 1024, nkv <= 256, d in {64, 128},
  * kv_len <= 2^21, k_stride_tok <= 2^24 and v_stride_ch <= 2^22 for the attention.  Blocks are counted from row 0; kv_len / 64 are whole.
  *
@@ -506,7 +508,9 @@ ghd_status ghd_block_bounds(void *bounds, const void *k_cache, int block0, int b
                             int capacity, int64_t k_stride_head, int64_t k_stride_tok, void *stream);
 
 /* What the bounds of blocks [block0, block0 + blocks) stand for: hi, lo float [nkv, blocks, d], 16-byte
- * aligned: HI s and LO s; infinity and minus infinity for a block that holds an infinity or NaN. */
+ * aligned: HI s and LO s; infinity and minus infinity for a block that holds an infinity or NaN.  For programs that
+ * choose blocks by a rule of their own (ghd_sparse_attention takes any selection) or look at what was chosen;
+ * ghd_block_select does not need it. */
 ghd_status ghd_block_bounds_read(float *hi, float *lo, const void *bounds, int block0, int blocks, int nkv,
                                  int d, int capacity, void *stream);
 

@@ -239,7 +239,9 @@ __host__ __device__ __forceinline__ size_t kept_at(int node, int segments, int s
 
 // What is left of a segment when the first child of a node is rejected: then beta is 1.  Where there are other children, the weights against
 // the rows' maxima are kept, 0 for the rejected token: another rejection goes over all of them in one workgroup.
-// Bound: a launch's time (64 nodes of 32000: 3.1 us), the exponentials of two rows (a chain of 128 nodes, 131072: 8.0 us).
+// Bound: a launch's time (64 nodes of 32000: 3.1 us).  A chain of 128 nodes, 131072 tokens: 8.0 us, of which the exponentials, one node's in 32
+// workgroups, are half at most: every rejected node's 32 workgroups first work out whether the walk can come there, and rows are asked for
+// behind that.
 __global__ __launch_bounds__(kRowThreads) void k_sample_rest(SampleArgs a, First* firsts, Rest* __restrict__ rest, float* __restrict__ kept)
 {
     __shared__ Reach s_reach;
@@ -381,8 +383,8 @@ __device__ __forceinline__ void node_is_done(const SampleArgs& a, NodeShared& s,
 }
 
 // One workgroup a node.  DRAFTS: they have probabilities.  Bound: what follows one another.  64 nodes, 32000 tokens: 8.0 us, with draft
-// probabilities 6.7 where no second child is rejected.  Each that is takes a pass over the kept weights: 2 us, and 256 KB at the
-// 100 to 150 GB/s that one compute unit gets from the L2 (32000 tokens 3.8 us a rejection, 131072 11).  In registers up to 32768 tokens'
+// probabilities 6.7 where no second child is rejected.  Each that is takes a pass over the kept weights: 2 us at 8000 tokens,
+// 3.9 at 32000 (256 KB), 9.2 at 131072 (1 MB), read and summed up by one compute unit.  In registers up to 32768 tokens'
 // weights took 10% less of many rejections, and 15% more at 8000 tokens.
 template <bool DRAFTS>
 __global__ __launch_bounds__(kNodeThreads) void k_sample_nodes(SAMPLE_FIRST(const Segment* __restrict__ seg), SampleArgs a, const First* __restrict__ firsts,

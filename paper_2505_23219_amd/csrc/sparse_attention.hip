@@ -472,8 +472,8 @@ __global__ __launch_bounds__(RT == 1 ? 256 : 512, RT == 1 ? 3 : 2) void k_sparse
 }
 
 // ---- more rows ----------------------------------------------------------------------------
-// What a compute unit reads from the L2 has a bound of its own (some 35 GB/s here), so above 32 rows a block of keys is read once for all rows of
-// a workgroup: straight to LDS, four blocks of 64 keys on their way, while eight wavefronts - four groups of rows, each RT tiles of
+// Wavefronts that read keys by themselves read them once for each tile or two of rows, so above 32 rows a block of keys is read once for all rows
+// of a workgroup: straight to LDS, four blocks of 64 keys on their way, while eight wavefronts - four groups of rows, each RT tiles of
 // 16, by halves of a block - take their operands from there.
 constexpr int kStages = 4;
 template <int D>
@@ -535,9 +535,11 @@ struct StagedBlock {
     }
 };
 
-// Bound: the bytes' way into the LDS.  64 tokens, 32 heads, lists of up to 48 blocks: 19.3 us, without the products 19.7 of 23.3 (of an earlier
-// state); 128 tokens, 40 heads, up to 96 blocks: 42.5 us, without them 42.4 of 47.7.  Loads past the L2: 46.2 of 48.3, but 23.8 against 22.9
-// for the tree; 256 rows in four wavefronts of 512 registers: 63.
+// Bound: the loads, but by what is not known.  64 tokens, 32 heads, lists of up to 48 blocks: 19.3 us, without the products 19.7 of 23.3 (of an
+// earlier state); 128 tokens, 40 heads, up to 96 blocks: 42.5 us, without them 42.4 of 47.7: a workgroup's 17 blocks of 32 KB come at
+// 13 GB/s, with 96 KB on their way, where attn_staged (attention_impl.h) has twice that inside its step's launch.  All 131 blocks of those tokens
+// take 52.8 us with the join, 3.2 TB/s; ghd_tree_attention's 49.4.  Loads past the L2: 46.2 of 48.3, but 23.8 against 22.9 for the tree,
+// so none has them; 256 rows in four wavefronts of 512 registers: 63.
 template <int D, int RT>
 __global__ __launch_bounds__(512, 2) void k_sparse_staged(SPARSE_FIRST, SparseArgs a, SparseCut cut)
 {
